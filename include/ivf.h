@@ -410,6 +410,133 @@ int ivf_cache_hotness(ivf_index* index, float* hotness);
  */
 int ivf_schedule(ivf_index* index, const float* q, int32_t nq, int32_t micro, int32_t* order, float* ms_gpu);
 
+/*
+ * Answering from retrieved passages: the operators of the language model's step behind a retrieval.  The
+ * queries of a micro-batch (ivf_schedule) are answered from passages that they share, and the beams of a beam
+ * search share their whole prompt, so keys and values lie in a paged cache of which a group of sequences can
+ * share a prefix.  These calls need no index.  All pointers are device pointers, work is enqueued on `stream`
+ * (a hipStream_t, NULL for the default stream) without waiting, nothing is allocated, and calls may be captured
+ * into a graph.  What the arrays on the device hold can change from call to call and from replay to replay.
+ *
+ * ivf_kv_cache: the keys and values of one layer.  Token slot t is place t % page of page t / page:
+ *   element e of head h is at  (t / page) * page_stride + (t % page) * token_stride + h * head_stride + e
+ * of k and of v, so pages can hold tokens one after the other or heads one after the other.  Strides count
+ * elements and are multiples of 8; k and v are 16-byte aligned; dtype is IVF_F16 or IVF_BF16; page is a
+ * power of two.
+ *
+ * ivf_kv_step: the sequences of one step, for all layers.
+ *   q_off     [n_seq + 1] first new token of each sequence, ascending from 0 to n_tokens
+ *   len       [n_seq] keys that the sequence has of its own, those of its new tokens included: its new tokens
+ *             are the last q_off[s + 1] - q_off[s] of them
+ *   table     [n_seq][table_stride] entry i names the slots of the sequence's own keys i * page ..: slots
+ *             entry * page and on.  `page` here is a power of two of at most the cache's: with page = 1 the table
+ *             names every slot by itself, and a beam's past moves by its table row alone (ivf_beam_step)
+ *   group_off [n_groups + 1] or NULL (n_groups = 0): sequences group_off[g] .. group_off[g + 1] share the
+ *             prefix g of prefix_len[g] keys, in the slots that row g of prefix_table names by entries of
+ *             prefix_page slots.  A prefix comes before the own keys.  Sequences outside all groups have none
+ *   max_q, max_len, max_prefix  the most new tokens, own keys and prefix keys of any sequence as far as the
+ *             caller knows (0: unknown).  They size the launch: lengths beyond them are still computed
+ *             right, but slower
+ * Key j of a sequence is key j of its prefix, or own key j - prefix_len; new token i has position
+ * prefix_len + len - (new tokens) + i.  Entries outside the cache and lengths outside the tables are not
+ * followed out of bounds: such keys are never written, and when read hold what some other slot holds.
+ */
+typedef struct ivf_kv_cache {
+    void* k;
+    void* v;
+    int64_t n_pages, page_stride, token_stride, head_stride;
+    int32_t page, n_heads, d, dtype;
+} ivf_kv_cache;
+
+typedef struct ivf_kv_step {
+    const int32_t* q_off;
+    const int32_t* len;
+    const int32_t* table;
+    int64_t table_stride;
+    const int32_t* group_off;
+    const int32_t* prefix_len;
+    const int32_t* prefix_table;
+    int64_t prefix_stride;
+    int32_t n_seq, n_tokens, page, max_q, max_len;
+    int32_t n_groups, prefix_page, max_prefix;
+} ivf_kv_step;
+
+/* One element vector of d for every head of every token: element e of head h of token t is at
+ * t * token_stride + h * head_stride + e.  Strides are multiples of 8, data is 16-byte aligned. */
+typedef struct ivf_rows {
+    void* data;
+    int64_t token_stride, head_stride;
+} ivf_rows;
+
+/*
+ * Appends the new tokens' keys and values (n_tokens x cache->n_heads x d each, of the cache's type) to the
+ * cache, each in the slot of its place, and rotates keys and, with q given, queries by position on the way.
+ *   rotary     [n_positions][rot] float32: cosines of the rot / 2 angles of a position, then their sines; or
+ *              NULL with rot = 0: nothing is rotated.  rot is a multiple of 16 of at most d; the elements from
+ *              rot on are copied.  A pair (a, b) becomes (a c - b s, b c + a s) in 32 bits, rounded once
+ *   interleaved  0: pairs are elements (f, f + rot / 2); 1: elements (2 f, 2 f + 1)
+ *   positions  [n_tokens] the positions to rotate by (taken into 0 .. n_positions - 1), or NULL: the tokens'
+ *              positions in their sequences
+ *   q, q_out   n_tokens x n_q_heads x d each, or both NULL with n_q_heads = 0; q_out may be q
+ * d is a multiple of 16 of at most 1024.  Tokens whose place is not in the table or whose entry is not in the
+ * cache are not written (their queries are rotated).  Two tokens must not share a slot.
+ */
+int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_rows* k, const ivf_rows* v,
+                  const float* rotary, int32_t n_positions, int32_t rot, int32_t interleaved, const int32_t* positions,
+                  const ivf_rows* q, const ivf_rows* q_out, int32_t n_q_heads, void* stream);
+
+/*
+ * Attention of the new tokens over the cache: out = softmax(scale * q . k) v over the keys that a token sees, in
+ * 32 bits, rounded once.  A token at position p sees key j when j <= p and, with window > 0, p - j < window or j <
+ * sinks.  A token that sees nothing gets zeros.  The keys of a prefix are read once for all tokens of its group.
+ *   q, out     n_tokens x n_q_heads x d, of the cache's type; query head h reads key head
+ *              h / (n_q_heads / cache->n_heads)
+ *   lse        [n_tokens][n_q_heads] float32: the logarithm of the sum of the exponentials (-INF: nothing
+ *              seen), or NULL
+ *   scale      > 0
+ *   workspace  device, 16-byte aligned, at least what ivf_attend_workspace() says for the same arguments; its
+ *              contents need not be kept, and calls that may overlap need one each
+ * d is 64, 96, 128 or 256.  Keys and values in slots that a token does not see never reach its result, whatever
+ * they hold; probabilities are rounded to the cache's type before the product with the values.
+ */
+int ivf_attend_workspace(const ivf_kv_step* step, const ivf_kv_cache* cache, int32_t n_q_heads, int32_t window, int32_t sinks,
+                         size_t* bytes);
+int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_rows* q, int32_t n_q_heads, const ivf_rows* out,
+               float* lse, float scale, int32_t window, int32_t sinks, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One step of a beam search for n_prompts prompts of beams_in beams: of all continuations of a prompt's beams
+ * by one token of the vocabulary the beams_out best become the new beams, and rows of per-beam states move.
+ * Row r = prompt * beams_in + beam:
+ *   logits     row r at r * row_stride (elements of dtype), `vocab` entries; logarithm of the softmax in 32 bits:
+ *              (x - max) - log(sum of exp(x - max)).  -INF and NaN entries are no continuations (and count
+ *              for nothing in the sum)
+ *   scores_in  [rows] the beams' scores; a continuation's score is score + log-softmax.  A beam at -INF
+ *              offers nothing
+ *   done_in    [rows] or NULL: a beam whose byte is not zero offers only the token `eos`, at its own score
+ * Order: larger score, then lower beam, then larger logit, then lower token.
+ *   scores_out, parent, token, done_out   [n_prompts][beams_out], best first: the score, the row it continues, the
+ *              token, and 1 where the parent was done or the token is eos.  Where a prompt has fewer
+ *              continuations: score -INF, parent = its first row, token -1, done 1
+ *   states     host array of n_states: row prompt * beams_out + i of `to` becomes row parent of `from`
+ *              (row_bytes, and strides in bytes); `to` must not overlap `from`
+ *   workspace  as in ivf_attend; its size is ivf_beam_workspace()
+ * beams_in and beams_out are at most IVF_MAX_BEAMS, n_states at most IVF_MAX_BEAM_STATES; logits are IVF_F32,
+ * IVF_F16 or IVF_BF16.
+ */
+#define IVF_MAX_BEAMS 64
+#define IVF_MAX_BEAM_STATES 8
+typedef struct ivf_beam_state {
+    const void* from;
+    void* to;
+    int64_t row_bytes, from_stride, to_stride;
+} ivf_beam_state;
+int ivf_beam_workspace(int32_t n_prompts, int32_t beams_in, int32_t vocab, int32_t beams_out, size_t* bytes);
+int ivf_beam_step(const void* logits, int64_t row_stride, int dtype, int32_t n_prompts, int32_t beams_in, int32_t vocab,
+                  const float* scores_in, const uint8_t* done_in, int32_t eos, int32_t beams_out, float* scores_out,
+                  int32_t* parent, int32_t* token, uint8_t* done_out, const ivf_beam_state* states, int32_t n_states,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
 /* Number of host threads used for the scan of C_miss (default: hardware threads, at most 64). */
 int ivf_set_host_threads(ivf_index* index, int32_t n);
 

@@ -18,6 +18,7 @@ IVF_F32, IVF_F16, IVF_BF16 = 0, 1, 2
 IVF_PLACE_DEVICE, IVF_PLACE_HOST = 0, 1
 IVF_PREFETCH_RESET = 1
 IVF_MAX_K = 112
+IVF_MAX_BEAMS, IVF_MAX_BEAM_STATES = 64, 8
 DTYPE_CODE = {"f32": IVF_F32, "f16": IVF_F16, "bf16": IVF_BF16}
 
 EXPORTS = [
@@ -26,7 +27,7 @@ EXPORTS = [
     "ivf_prefetch_ways", "ivf_resident", "ivf_batched_scores", "ivf_get_layout", "ivf_profile_enable", "ivf_profile_read",
     "ivf_profile_reset", "ivf_set_host_threads", "ivf_set_pipeline_depth", "ivf_synchronize",
     "ivf_set_batch_mode", "ivf_limit_batch_memory", "ivf_cache_configure", "ivf_cache_end_round", "ivf_cache_hotness",
-    "ivf_schedule", "ivf_host_scan", "ivf_host_scan_capacity", "ivf_prefetch_amount", "ivf_prefetch_plan", "ivf_cache_plan", "ivf_strerror", "ivf_last_error",
+    "ivf_schedule", "ivf_kv_append", "ivf_attend", "ivf_attend_workspace", "ivf_beam_step", "ivf_beam_workspace", "ivf_host_scan", "ivf_host_scan_capacity", "ivf_prefetch_amount", "ivf_prefetch_plan", "ivf_cache_plan", "ivf_strerror", "ivf_last_error",
 ]
 
 
@@ -52,6 +53,28 @@ class Profile(C.Structure):
     _fields_ = [("calls", C.c_uint64), ("ms_coarse", C.c_double), ("ms_select", C.c_double),
                 ("ms_scan", C.c_double), ("ms_merge", C.c_double), ("scan_bytes", C.c_uint64),
                 ("scan_rows", C.c_uint64)]
+
+
+class KvCacheArg(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("page_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("page", C.c_int32), ("n_heads", C.c_int32),
+                ("d", C.c_int32), ("dtype", C.c_int32)]
+
+
+class KvStepArg(C.Structure):
+    _fields_ = [("q_off", C.c_void_p), ("len", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64),
+                ("group_off", C.c_void_p), ("prefix_len", C.c_void_p), ("prefix_table", C.c_void_p), ("prefix_stride", C.c_int64),
+                ("n_seq", C.c_int32), ("n_tokens", C.c_int32), ("page", C.c_int32), ("max_q", C.c_int32), ("max_len", C.c_int32),
+                ("n_groups", C.c_int32), ("prefix_page", C.c_int32), ("max_prefix", C.c_int32)]
+
+
+class RowsArg(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class BeamStateArg(C.Structure):
+    _fields_ = [("from_", C.c_void_p), ("to", C.c_void_p), ("row_bytes", C.c_int64), ("from_stride", C.c_int64),
+                ("to_stride", C.c_int64)]
 
 
 class IvfError(RuntimeError):
@@ -100,6 +123,12 @@ def load():
     L.ivf_cache_end_round.argtypes = [vp, C.POINTER(CacheStats)]
     L.ivf_cache_hotness.argtypes = [vp, vp]
     L.ivf_schedule.argtypes = [vp, vp, i32, i32, vp, C.POINTER(C.c_float)]
+    step, cache, rows = C.POINTER(KvStepArg), C.POINTER(KvCacheArg), C.POINTER(RowsArg)
+    L.ivf_kv_append.argtypes = [step, cache, rows, rows, vp, i32, i32, i32, vp, rows, rows, i32, vp]
+    L.ivf_attend_workspace.argtypes = [step, cache, i32, i32, i32, C.POINTER(sz)]
+    L.ivf_attend.argtypes = [step, cache, rows, i32, rows, vp, C.c_float, i32, i32, vp, sz, vp]
+    L.ivf_beam_workspace.argtypes = [i32, i32, i32, i32, C.POINTER(sz)]
+    L.ivf_beam_step.argtypes = [vp, i64, ci, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, C.POINTER(BeamStateArg), i32, vp, sz, vp]
     L.ivf_strerror.argtypes = [ci]
     L.ivf_strerror.restype = C.c_char_p
     L.ivf_last_error.restype = C.c_char_p
@@ -457,3 +486,215 @@ def ivf_cache_plan(hotness, offsets, row_bytes, resident_off, buffer_used, buffe
                             int(buffer_bytes), float(fraction), _ptr(evicted), C.byref(n_ev), moves, C.byref(n_mv)))
     mv = [(m.cluster, m.via_staging, m.from_byte, m.to_byte, m.bytes) for m in moves[:n_mv.value]]
     return evicted[:n_ev.value], mv, used.value
+
+
+# ---- answering from retrieved passages -------------------------------------------------------------
+_codes = None
+
+
+def _code(dtype):
+    global _codes
+    if _codes is None:
+        t = _torch()
+        _codes = {t.float32: IVF_F32, t.float16: IVF_F16, t.bfloat16: IVF_BF16}
+    code = _codes.get(dtype)
+    if code is None:
+        raise TypeError(f"{dtype}: float32, float16 or bfloat16 expected")
+    return code
+
+
+def _i32(a, shape, what):
+    """A contiguous int32 CUDA tensor of this shape (None in it: any size)."""
+    t = _torch()
+    if a.dtype is not t.int32:
+        raise TypeError(f"{what} must be int32")
+    if not a.is_cuda or not a.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous CUDA tensor")
+    if len(a.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, a.shape)):
+        raise ValueError(f"{what} has shape {tuple(a.shape)}, expected {tuple(shape)}")
+    return a.data_ptr()
+
+
+def _rows(a, n_tokens, n_heads, d, dtype, what):
+    """[n_tokens, heads, d] with the elements of a head side by side."""
+    if a.dtype is not dtype:
+        raise TypeError(f"{what} is {a.dtype}, the cache {dtype}")
+    shape, stride = a.shape, a.stride()
+    if not a.is_cuda or len(shape) != 3 or shape[0] != n_tokens or shape[2] != d or (n_heads is not None and shape[1] != n_heads):
+        raise ValueError(f"{what} has shape {tuple(shape)}, expected CUDA [{n_tokens}, {n_heads or 'heads'}, {d}]")
+    if stride[2] != 1 and d > 1:
+        raise ValueError(f"the elements of a head of {what} must lie side by side")
+    return RowsArg(a.data_ptr(), stride[0], stride[1])
+
+
+class KvCache:
+    """The paged cache of one layer: k and v [n_pages, page, heads, d], views of any page, token and head order
+    (a cache of head-major pages is passed as `pages.transpose(1, 2)`)."""
+
+    def __init__(self, k, v):
+        if k.dtype is not v.dtype or k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError("k and v must have the same type, shape and strides")
+        if not (k.is_cuda and v.is_cuda) or k.dim() != 4 or k.stride(3) != 1:
+            raise ValueError("expected CUDA tensors [n_pages, page, heads, d] with the elements of a head side by side")
+        self.k, self.v, self.dtype = k, v, k.dtype
+        (pages, page, self.heads, self.d), st = k.shape, k.stride()
+        self.arg = KvCacheArg(k.data_ptr(), v.data_ptr(), pages, st[0], st[1], st[2], page, self.heads, self.d, _code(k.dtype))
+        self.ref = C.byref(self.arg)
+
+
+class KvStep:
+    """The sequences of one step, for the calls of all layers.  q_off [sequences + 1], lens [sequences] and table
+    [sequences, entries] are int32 CUDA tensors; a table entry names `page` slots.  With group_off [groups + 1]
+    the sequences of a group share the prefix of prefix_lens [groups] keys in the rows of prefix_table [groups,
+    entries], whose entries name prefix_page slots (default: page).  max_q, max_len and max_prefix are what the
+    program knows of the lengths (0: nothing).  The tensors' contents may change between calls."""
+
+    def __init__(self, q_off, lens, table, page, n_tokens, max_q=0, max_len=0, group_off=None, prefix_lens=None, prefix_table=None,
+                 prefix_page=None, max_prefix=0):
+        n = lens.shape[0]
+        a = KvStepArg(_i32(q_off, (n + 1,), "q_off"), _i32(lens, (n,), "lens"), _i32(table, (n, None), "table"), table.shape[1])
+        a.n_seq, a.n_tokens, a.page, a.max_q, a.max_len = n, n_tokens, page, max_q, max_len
+        if group_off is not None:
+            if prefix_lens is None or prefix_table is None:
+                raise ValueError("group_off, prefix_lens and prefix_table go together")
+            g = prefix_lens.shape[0]
+            a.group_off, a.prefix_len = _i32(group_off, (g + 1,), "group_off"), _i32(prefix_lens, (g,), "prefix_lens")
+            a.prefix_table, a.prefix_stride = _i32(prefix_table, (g, None), "prefix_table"), prefix_table.shape[1]
+            a.n_groups, a.prefix_page, a.max_prefix = g, page if prefix_page is None else prefix_page, max_prefix
+        self.arg, self.n_tokens = a, n_tokens
+        self._keep = (q_off, lens, table, group_off, prefix_lens, prefix_table)
+        self.ref = C.byref(a)
+
+
+def _workspace(n, stream):
+    """n bytes that are free again, in stream order, once the call's kernels have run."""
+    t = _torch()
+    w = t.empty(n, dtype=t.uint8, device="cuda")
+    if stream is not None:
+        w.record_stream(stream)
+    return w
+
+
+def _on(stream):
+    return (_torch().cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def ivf_kv_append(step, cache, k, v, rotary=None, positions=None, q=None, q_out=None, interleaved=False, stream=None):
+    """Appends the new tokens' k and v [tokens, heads, d] to the cache; with rotary [positions, rot] float32 (cosines,
+    then sines) keys and q [tokens, query heads, d] are rotated.  Returns q_out (default: a new tensor)."""
+    n, d, t = step.n_tokens, cache.d, _torch()
+    kr, vr = _rows(k, n, cache.heads, d, cache.dtype, "k"), _rows(v, n, cache.heads, d, cache.dtype, "v")
+    qr = qo = rp = pp = None
+    hq = n_pos = rot = 0
+    if q is not None:
+        if q_out is None:
+            q_out = t.empty(q.shape, dtype=q.dtype, device=q.device)
+            if stream is not None:
+                q_out.record_stream(stream)
+        hq = q.shape[1]
+        qr, qo = _rows(q, n, hq, d, cache.dtype, "q"), _rows(q_out, n, hq, d, cache.dtype, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if rotary is not None:
+        if rotary.dtype is not t.float32 or not rotary.is_cuda or not rotary.is_contiguous() or rotary.dim() != 2:
+            raise ValueError("rotary must be a contiguous float32 CUDA tensor [positions, rot]")
+        n_pos, rot = rotary.shape
+        rp = rotary.data_ptr()
+    if positions is not None:
+        pp = _i32(positions, (n,), "positions")
+    status = load().ivf_kv_append(step.ref, cache.ref, kr, vr, rp, n_pos, rot, 1 if interleaved else 0, pp, qr, qo, hq, _on(stream))
+    if status != 0:
+        _check(status)
+    return q_out
+
+
+def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0, workspace=None, stream=None):
+    """Attention of the new tokens q [tokens, query heads, d] over the cache; returns out (default: a new tensor).
+    lse: float32 [tokens, query heads] or None.  scale: default d ** -0.5.  workspace: a uint8 CUDA tensor of
+    at least ivf_attend_workspace() bytes, default one for this call."""
+    n, d, t = step.n_tokens, cache.d, _torch()
+    if out is None:
+        out = t.empty(q.shape, dtype=q.dtype, device=q.device)
+        if stream is not None:
+            out.record_stream(stream)
+    hq = q.shape[1]
+    qr, qo = _rows(q, n, hq, d, cache.dtype, "q"), _rows(out, n, hq, d, cache.dtype, "out")
+    lp = None
+    if lse is not None:
+        if lse.dtype is not t.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape != (n, hq):
+            raise ValueError("lse must be a contiguous float32 CUDA tensor [tokens, query heads]")
+        lp = lse.data_ptr()
+    if workspace is None:
+        need = ivf_attend_workspace(step, cache, hq, window, sinks)
+        if need:
+            workspace = _workspace(need, stream)
+    wp, wn = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    status = load().ivf_attend(step.ref, cache.ref, qr, hq, qo, lp, d ** -0.5 if scale is None else scale, window, sinks, wp, wn,
+                               _on(stream))
+    if status != 0:
+        _check(status)
+    return out
+
+
+def ivf_attend_workspace(step, cache, n_q_heads, window=0, sinks=0):
+    """Bytes of workspace of ivf_attend with these arguments."""
+    n = C.c_size_t(0)
+    status = load().ivf_attend_workspace(step.ref, cache.ref, n_q_heads, window, sinks, C.byref(n))
+    if status != 0:
+        _check(status)
+    return n.value
+
+
+def ivf_beam_workspace(n_prompts, beams_in, vocab, beams_out):
+    """Bytes of workspace of ivf_beam_step with these sizes."""
+    n = C.c_size_t(0)
+    status = load().ivf_beam_workspace(n_prompts, beams_in, vocab, beams_out, C.byref(n))
+    if status != 0:
+        _check(status)
+    return n.value
+
+
+def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), workspace=None, stream=None):
+    """One step of a beam search.  logits [prompts, beams, vocab] (float32, float16 or bfloat16, rows evenly spaced),
+    scores [prompts, beams] float32, done [prompts, beams] bool or uint8, or None.  states: pairs (from, to) of
+    CUDA tensors with a row per beam, before and after (prompts * beams and prompts * beams_out rows, each row
+    contiguous).  Returns scores, parents (row of logits), tokens and done, each [prompts, beams_out]."""
+    t = _torch()
+    if logits.dim() != 3 or not logits.is_cuda or logits.stride(2) != 1:
+        raise ValueError("logits must be a CUDA tensor [prompts, beams, vocab] with contiguous rows")
+    p, b, vocab = logits.shape
+    stride = logits.stride(1) if b > 1 else logits.stride(0)
+    if p > 1 and logits.stride(0) != b * stride:
+        raise ValueError("the rows of logits must be evenly spaced")
+    if p * b == 1:
+        stride = vocab
+    if scores.dtype is not t.float32 or not scores.is_cuda or not scores.is_contiguous() or scores.shape != (p, b):
+        raise ValueError("scores must be a contiguous float32 CUDA tensor [prompts, beams]")
+    dp = None
+    if done is not None:
+        if done.dtype not in (t.bool, t.uint8) or not done.is_cuda or not done.is_contiguous() or done.shape != (p, b):
+            raise ValueError("done must be a contiguous bool or uint8 CUDA tensor [prompts, beams]")
+        dp = done.data_ptr()
+    n = b if beams_out is None else beams_out
+    args = (BeamStateArg * max(1, len(states)))()
+    for i, (src, dst) in enumerate(states):
+        if src.dtype is not dst.dtype or not (src.is_cuda and dst.is_cuda):
+            raise ValueError("a state and its destination must be CUDA tensors of the same type")
+        if src.shape[0] != p * b or dst.shape[0] != p * n or src.shape[1:] != dst.shape[1:] or not (src[0].is_contiguous() and dst[0].is_contiguous()):
+            raise ValueError("a state has a contiguous row per beam, before and after")
+        e, size = src[0].numel(), src.element_size()
+        args[i] = BeamStateArg(src.data_ptr(), dst.data_ptr(), e * size, src.stride(0) * size, (dst.stride(0) if p * n > 1 else e) * size)
+    need = ivf_beam_workspace(p, b, vocab, n)
+    score, parent = t.empty(p, n, dtype=t.float32, device="cuda"), t.empty(p, n, dtype=t.int32, device="cuda")
+    token, out = t.empty(p, n, dtype=t.int32, device="cuda"), t.empty(p, n, dtype=t.bool, device="cuda")
+    if workspace is None:
+        workspace = _workspace(need, stream)
+    if stream is not None:
+        for x in (score, parent, token, out):
+            x.record_stream(stream)
+    status = load().ivf_beam_step(logits.data_ptr(), stride, _code(logits.dtype), p, b, vocab, scores.data_ptr(), dp, eos, n,
+                                  score.data_ptr(), parent.data_ptr(), token.data_ptr(), out.data_ptr(), args, len(states),
+                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(), _on(stream))
+    if status != 0:
+        _check(status)
+    return score, parent, token, out

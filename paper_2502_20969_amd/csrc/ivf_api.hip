@@ -24,7 +24,7 @@ using namespace ivf;
 // ---- errors -----------------------------------------------------------------------------------
 static thread_local std::string g_last_error;
 
-static int fail(int status, const char* fmt, ...) {
+int ivf::fail(int status, const char* fmt, ...) {
     char buf[512];
     va_list ap;
     va_start(ap, fmt);
@@ -33,14 +33,6 @@ static int fail(int status, const char* fmt, ...) {
     g_last_error = buf;
     return status;
 }
-
-#define HIP_TRY(expr)                                                                       \
-    do {                                                                                    \
-        hipError_t e_ = (expr);                                                             \
-        if (e_ != hipSuccess)                                                               \
-            return fail(e_ == hipErrorOutOfMemory ? IVF_ENOMEM : IVF_EHIP, "%s: %s", #expr, \
-                        hipGetErrorString(e_));                                             \
-    } while (0)
 
 extern "C" const char* ivf_strerror(int status) {
     switch (status) {

@@ -9,6 +9,17 @@
 
 namespace ivf {
 
+// sets the calling thread's error text and returns `status` (ivf_api.hip)
+int fail(int status, const char* fmt, ...);
+
+#define HIP_TRY(expr)                                                                       \
+    do {                                                                                    \
+        hipError_t e_ = (expr);                                                             \
+        if (e_ != hipSuccess)                                                               \
+            return fail(e_ == hipErrorOutOfMemory ? IVF_ENOMEM : IVF_EHIP, "%s: %s", #expr, \
+                        hipGetErrorString(e_));                                             \
+    } while (0)
+
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;   // empty slot of a candidate list
 constexpr int kMaxKPrime = 128;            // candidates kept per list: k + slack <= 128
 constexpr int kScanWaves = 4;              // scan workgroup: 4 wavefronts, two workgroups per compute unit

@@ -1,0 +1,122 @@
+"""What the calls of the paged cache, its attention and the beam step refuse, before any work is enqueued (no GPU)."""
+import ctypes as C
+
+import pytest
+
+import paper_2502_20969_amd as P
+from paper_2502_20969_amd.binding import BeamStateArg, KvCacheArg, KvStepArg, RowsArg
+
+OK = 1 << 20            # an aligned address that no test lets a kernel see
+
+
+def _cache(**kw):
+    a = KvCacheArg(OK, OK, 10, 16 * 2 * 64, 2 * 64, 64, 16, 2, 64, P.IVF_BF16)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def _step(**kw):
+    a = KvStepArg(OK, OK, OK, 4)
+    a.n_seq, a.n_tokens, a.page = 2, 3, 16
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def _rows(data=OK, t=128, h=64):
+    return RowsArg(data, t, h)
+
+
+BAD_CACHE = [dict(k=None), dict(v=None), dict(k=OK + 8), dict(v=OK + 2), dict(n_pages=0), dict(n_heads=0), dict(d=0), dict(page=0), dict(page=12),
+             dict(page=-16), dict(page_stride=2044), dict(token_stride=4), dict(head_stride=7), dict(dtype=P.IVF_F32), dict(dtype=9)]
+BAD_STEP = [dict(q_off=None), dict(len=None), dict(table=None), dict(table_stride=0), dict(n_seq=0), dict(n_tokens=0), dict(page=3), dict(page=32),
+            dict(page=0), dict(max_q=-1), dict(max_len=-1), dict(max_prefix=-1), dict(n_groups=-1), dict(n_groups=1), dict(n_groups=1, group_off=OK, prefix_len=OK),
+            dict(n_groups=1, group_off=OK, prefix_len=OK, prefix_table=OK, prefix_stride=4, prefix_page=0),
+            dict(n_groups=1, group_off=OK, prefix_len=OK, prefix_table=OK, prefix_stride=0, prefix_page=16)]
+
+
+def _append(step=None, cache=None, k=None, v=None, rotary=OK, n_pos=10, rot=64, q=None, q_out=None, hq=0):
+    return P.load().ivf_kv_append(step or _step(), cache or _cache(), k or _rows(), v or _rows(), rotary, n_pos, rot, 0, None, q, q_out, hq, None)
+
+
+def _attend(step=None, cache=None, q=None, out=None, hq=4, scale=0.125, window=0, sinks=0, ws=OK, nbytes=1 << 40):
+    return P.load().ivf_attend(step or _step(), cache or _cache(), q or _rows(), hq, out or _rows(), None, scale, window, sinks, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw", BAD_CACHE)
+def test_caches(kw):
+    n = C.c_size_t()
+    assert _append(cache=_cache(**kw)) == -1
+    assert _attend(cache=_cache(**kw)) == -1
+    assert P.load().ivf_attend_workspace(_step(), _cache(**kw), 4, 0, 0, C.byref(n)) == -1
+
+
+@pytest.mark.parametrize("kw", BAD_STEP)
+def test_steps(kw):
+    n = C.c_size_t()
+    assert _append(step=_step(**kw)) == -1
+    assert _attend(step=_step(**kw)) == -1
+    assert P.load().ivf_attend_workspace(_step(**kw), _cache(), 4, 0, 0, C.byref(n)) == -1
+
+
+@pytest.mark.parametrize("rows", [RowsArg(None, 128, 64), RowsArg(OK + 4, 128, 64), RowsArg(OK, 132, 64), RowsArg(OK, 128, 60)])
+def test_rows(rows):
+    assert _append(k=rows) == -1 and _append(v=rows) == -1
+    assert _append(q=rows, q_out=_rows(), hq=2) == -1 and _append(q=_rows(), q_out=rows, hq=2) == -1
+    assert _attend(q=rows) == -1 and _attend(out=rows) == -1
+
+
+def test_appends():
+    L = P.load()
+    assert _append(q=_rows(), hq=2) == -1 and _append(hq=2) == -1 and _append(q=_rows(), q_out=_rows(), hq=0) == -1 and _append(hq=-1) == -1
+    assert _append(rot=24) == -1 and _append(rot=80) == -1 and _append(rot=-16) == -1 and _append(rot=0) == -1
+    assert _append(rotary=None) == -1 and _append(n_pos=0) == -1
+    assert _append(cache=_cache(d=72)) == -1
+    assert _append(cache=_cache(d=1040), rot=0, rotary=None) == -5
+    assert L.ivf_kv_append(None, _cache(), _rows(), _rows(), None, 0, 0, 0, None, None, None, 0, None) == -1
+    assert L.ivf_kv_append(_step(), None, _rows(), _rows(), None, 0, 0, 0, None, None, None, 0, None) == -1
+    assert L.ivf_kv_append(_step(), _cache(), None, _rows(), None, 0, 0, 0, None, None, None, 0, None) == -1
+    assert b"k is NULL" in L.ivf_last_error()
+
+
+def test_attention():
+    L = P.load()
+    n = C.c_size_t()
+    for d in (32, 80, 112, 512):
+        assert _attend(cache=_cache(d=d)) == -5
+    assert _attend(hq=3) == -1 and _attend(hq=0) == -1 and _attend(window=-1) == -1 and _attend(sinks=-1) == -1
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert _attend(scale=scale) == -1
+    assert _attend(ws=OK + 4) == -1
+    assert L.ivf_attend_workspace(_step(), _cache(), 4, 0, 0, None) == -1
+    assert L.ivf_attend(None, _cache(), _rows(), 4, _rows(), None, 1.0, 0, 0, OK, 1 << 40, None) == -1
+    assert L.ivf_attend(_step(), None, _rows(), 4, _rows(), None, 1.0, 0, 0, OK, 1 << 40, None) == -1
+    assert L.ivf_attend(_step(), _cache(), None, 4, _rows(), None, 1.0, 0, 0, OK, 1 << 40, None) == -1
+    assert L.ivf_attend_workspace(_step(), _cache(), 4, 0, 0, C.byref(n)) == 0
+    if n.value:
+        assert _attend(nbytes=n.value - 1) == -1 and _attend(ws=None) == -1
+        assert b"workspace" in L.ivf_last_error()
+
+
+def test_beam_steps():
+    L = P.load()
+    n = C.c_size_t()
+    for sizes in ((0, 2, 10, 2), (1, 0, 10, 2), (1, 2, 0, 2), (1, 2, 10, 0)):
+        assert L.ivf_beam_workspace(*sizes, C.byref(n)) == -1
+    assert L.ivf_beam_workspace(1, 65, 10, 2, C.byref(n)) == -5 and L.ivf_beam_workspace(1, 2, 10, 65, C.byref(n)) == -5
+    assert L.ivf_beam_workspace(2 ** 30, 64, 10, 2, C.byref(n)) == -5
+    assert L.ivf_beam_workspace(1, 2, 10, 2, None) == -1
+    assert L.ivf_beam_workspace(3, 2, 10, 2, C.byref(n)) == 0
+
+    def call(logits=OK, stride=10, dtype=0, p=3, scores=OK, out=OK, parent=OK, token=OK, fin=OK, states=None, n_states=0, ws=OK, nbytes=n.value):
+        return L.ivf_beam_step(logits, stride, dtype, p, 2, 10, scores, None, 2, 2, out, parent, token, fin, states, n_states, ws, nbytes, None)
+
+    for kw in (dict(logits=None), dict(scores=None), dict(out=None), dict(parent=None), dict(token=None), dict(fin=None), dict(stride=9), dict(dtype=3),
+               dict(dtype=-1), dict(logits=OK + 2), dict(logits=OK + 1, dtype=1), dict(n_states=-1), dict(n_states=1), dict(ws=None), dict(ws=OK + 8),
+               dict(nbytes=n.value - 1), dict(p=0)):
+        assert call(**kw) == -1, kw
+    states = (BeamStateArg * 9)(*[BeamStateArg(OK, OK, 8, 8, 8)] * 9)
+    assert call(states=states, n_states=9) == -5
+    for bad in (BeamStateArg(None, OK, 8, 8, 8), BeamStateArg(OK, None, 8, 8, 8), BeamStateArg(OK, OK, 0, 8, 8), BeamStateArg(OK, OK, 8, -8, 8), BeamStateArg(OK, OK, 8, 8, 4)):
+        assert call(states=(BeamStateArg * 1)(bad), n_states=1) == -1
