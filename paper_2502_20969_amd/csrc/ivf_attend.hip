@@ -1,81 +1,512 @@
 // Attention of a step's new tokens over the paged cache.
+//
+//   out = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q . k_j) over the keys j that the token sees
+//
+// in one pass over the keys with a running maximum m: w_j is taken as 2^(x_j - m), x_j = q . k_j scale log2(e), and what
+// was summed is scaled by 2^(m - m') when m rises to m'.  Sums over disjoint sets of keys are joined by the same rule, so
+// the keys of a long sequence are split over workgroups and those of a prefix are read for all tokens of its group at
+// once, whose sequences then add their own keys.
+//
+// Rows.  The new tokens of a sequence (of a group, for its prefix) times the query heads that share a key head are the
+// rows of one product, row r = token r / G, head r % G: 32 of them to a wavefront.  Scores are formed transposed,
+// S^T = K Q^T by 32 x 32 x 16 MFMAs (lane l holds 16 of 32 keys of row l % 32), so that a row's maximum and sum stay
+// inside a lane but for one exchange with lane l ^ 32, and the weights are already where O^T += V^T P^T wants them: the
+// order of keys inside a product is free, and V is read from LDS transposed in the order in which S^T came out.
+//
+// Keys and values go from memory to LDS directly, without passing registers, 16 bytes a lane; the chunks of a row are
+// permuted on the way so that both kinds of LDS reads are spread over the banks.  The tables' entries are fetched into
+// LDS in the same way ahead of the tiles they name.
 #include "ivf_answer.h"
 #include "ivf_device.h"
 #include <algorithm>
+#include <math.h>
 
 namespace ivf {
 using namespace dev;
+
+enum { kConcat, kOwn, kPrefix };     // keys of a pass: prefix and own, own only, prefix only
 
 struct AttendArgs {
     CacheView cache;
     StepView step;
     ivf_rows q, out;
     float* lse;
-    float scale;
-    int hq, group, window, sinks;        // group: query heads per key head
+    float scale_log2;                // scale * log2(e)
+    int hq, hkv, group, window, sinks;       // group: query heads per key head
+    // partial sums [token][query head][parts]: O [d] unnormalised, and (m, l); m NaN: the row's result is complete
+    float* part_o;
+    float2* part_ml;
+    int parts;                       // 0: one pass over all keys, no partial sums
+    // this pass
+    int mode, part0, n_part;         // its range of partial sums
+    int n_split, n_tile;             // workgroups that share a row's keys; workgroups that share a unit's rows
+    int rows_lo, rows_hi;            // units with more than rows_lo and at most rows_hi rows
 };
 
-// One wavefront per token and query head, 64 keys at a time: a lane takes the product with one key, then the lanes
-// take the elements of the values.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void attend_rows_kernel(AttendArgs a) {
-    constexpr int kPer = (D + 63) / 64;
-    const int lane = threadIdx.x, h = blockIdx.y, kvh = h / a.group;
-    __shared__ float s_q[D];
-    for (int t = blockIdx.x; t < a.step.n_tokens; t += gridDim.x) {
-        int lo = 0, hi = a.step.n_seq;                     // the last sequence that begins at or before t
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.step.q_off[mid] <= t) lo = mid; else hi = mid;
-        }
-        const int s = lo, g = group_of(a.step, s), plen = prefix_of(a.step, g);
-        const int n = own_len(a.step, s);
-        const int pos = plen + n - (a.step.q_off[s + 1] - t);
-        const T* q = (const T*)a.q.data + t * a.q.token_stride + h * a.q.head_stride;
-        __syncthreads();
-        for (int e = lane; e < D; e += 64) s_q[e] = (float)q[e] * a.scale;
-        __syncthreads();
-        float m = -INFINITY, l = 0.f, o[kPer] = {};
-        const int end = min(pos + 1, plen + n);
-        const int low = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-        for (int j0 = 0; j0 < end; j0 += 64) {
-            if (j0 + 64 <= low && j0 >= a.sinks) continue;
-            const int j = j0 + lane;
-            const bool sees = j < end && (j >= low || j < a.sinks);
-            int64_t off = 0;
-            float x = -INFINITY;
-            if (sees) {
-                const int64_t slot = j < plen ? slot_in(a.step.prefix_table + g * a.step.prefix_stride, a.step.prefix_entries, a.step.prefix_shift, j)
-                                              : slot_in(a.step.table + s * a.step.table_stride, a.step.own_entries, a.step.shift, j - plen);
-                off = slot_offset(a.cache, slot) + kvh * a.cache.head_stride;
-                const T* k = (const T*)a.cache.k + off;
-                x = 0.f;
-                for (int e = 0; e < D; ++e) x += s_q[e] * (float)k[e];
-            }
-            float top = x;
-            for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-            if (__ballot(sees) == 0) continue;
-            const float m2 = fmaxf(m, top);
-            const float keep = m2 == -INFINITY ? 1.f : expf(m - m2);
-            const float p = sees ? expf(x - m2) : 0.f;
-            float sum = p;
-            for (int w = 32; w >= 1; w >>= 1) sum += __shfl_xor(sum, w);
-            l = l * keep + sum;
-            m = m2;
-            for (int i = 0; i < kPer; ++i) o[i] *= keep;
-            for (uint64_t left = __ballot(sees); left; left &= left - 1) {
-                const int from = __builtin_ctzll(left);
-                const float pj = __shfl(p, from);
-                const T* v = (const T*)a.cache.v + __shfl((long long)off, from);
-                for (int i = 0; i < kPer; ++i)
-                    if (i * 64 + lane < D) o[i] += pj * (float)v[i * 64 + lane];
-            }
-        }
-        T* out = (T*)a.out.data + t * a.out.token_stride + h * a.out.head_stride;
-        for (int i = 0; i < kPer; ++i)
-            if (i * 64 + lane < D) out[i * 64 + lane] = (T)(l == 0.f ? 0.f : o[i] / l);
-        if (a.lse && lane == 0) a.lse[(int64_t)t * a.hq + h] = l == 0.f ? -INFINITY : m + logf(l);
+// ---- memory to LDS ------------------------------------------------------------------------------
+// The loads are written as assembly so that the compiler, which cannot know which of them a read from LDS depends on,
+// does not wait for all of them; they have no register outputs, and are waited for by count.
+extern __shared__ __align__(16) unsigned char s_mem[];
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+// lane l's 16 (4) bytes at g go to LDS address `to` + 16 l (4 l); `to` is the same in all lanes
+__device__ __forceinline__ void fetch16(const void* g, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(g), "s"(to) : "memory");
+}
+__device__ __forceinline__ void fetch4(const void* g, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(g), "s"(to) : "memory");
+}
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory"); }
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// ---- types ------------------------------------------------------------------------------------------
+typedef short s4_t __attribute__((ext_vector_type(4)));
+typedef short s8_t __attribute__((ext_vector_type(8)));
+typedef float f16v_t __attribute__((ext_vector_type(16)));
+typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s4_t* lds_s4;
+
+template <typename T> struct Half;
+template <> struct Half<_Float16> {
+    static constexpr uint32_t kExponent = 0x7C00u;
+    // weights reach from 2^-22 of the largest down to f16's smallest numbers only if the largest lies high
+    static constexpr float kLift = 7.f;
+    static __device__ __forceinline__ f16v_t mfma(s8_t a, s8_t b, f16v_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8_t, a), __builtin_bit_cast(h8_t, b), c, 0, 0, 0);
     }
+};
+template <> struct Half<__bf16> {
+    static constexpr uint32_t kExponent = 0x7F80u;
+    static constexpr float kLift = 0.f;
+    static __device__ __forceinline__ f16v_t mfma(s8_t a, s8_t b, f16v_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8_t, a), __builtin_bit_cast(b8_t, b), c, 0, 0, 0);
+    }
+};
+
+// A maximum rises only when the new one is 2^kSlack above it: until then weights of up to 2^kSlack are summed, which
+// costs no precision, and the sums need not be scaled for every small rise.
+constexpr float kSlack = 8.f;
+
+// NARROW: the workgroup has one tile of 32 rows, its wavefronts take the tiles of keys in turn, each with LDS of its own.
+// Otherwise every wavefront has 32 rows of its own and all share the tiles.
+template <int D, bool NARROW>
+struct Shape {
+    static constexpr int kChunks = D <= 64 ? 8 : D <= 128 ? 16 : 32;       // 16-byte chunks of a staged row
+    static constexpr int kPitch = kChunks * 16;
+    static constexpr int kKeys = NARROW || D > 128 ? 32 : 64;              // keys of a tile
+    static constexpr int kWaves = NARROW && D > 128 ? 2 : 4;
+    static constexpr int kStages = NARROW && D <= 64 ? 4 : 2;
+    static constexpr int kAhead = kStages - 1;                             // tiles on their way while one is worked on
+    static constexpr int kTileBytes = kKeys * kPitch * 2;                  // keys, then values
+    static constexpr int kRowsPerLoad = 64 / kChunks;
+    static constexpr int kWaveRows = NARROW ? kKeys : kKeys / kWaves;      // rows of a tile that a wavefront fetches
+    static constexpr int kLoads = kWaveRows / kRowsPerLoad;                // loads for its keys, and as many for its values
+    static constexpr int kRows = NARROW ? 32 : 32 * kWaves;                // rows of a workgroup
+    static constexpr int kEntrySlots = kAhead > 1 ? 8 : 4;                 // tiles whose table entries are kept
+    static constexpr int kStageBytes = (NARROW ? kWaves : 1) * kStages * kTileBytes;
+    static constexpr int kLds = kStageBytes + kWaves * kEntrySlots * 256;
+    static_assert(2 * kAhead < kEntrySlots, "an entry's place is not taken before its tile is fetched");
+    static_assert(!NARROW || (size_t)kWaves * 32 * D * 4 + kWaves * 32 * 8 <= (size_t)kStageBytes, "room to join the wavefronts");
+};
+
+// chunk c of row r of a tile lies at place c ^ place_swap(r)
+template <int CHUNKS> __device__ __forceinline__ int place_swap(int row) {
+    return CHUNKS == 8 ? row & 7 : (row & 3) << 2 | (row >> 2 & 3);
+}
+
+template <typename T, int D, bool NARROW>
+__global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) void attend_kernel(AttendArgs a) {
+    using S = Shape<D, NARROW>;
+    using H = Half<T>;
+    constexpr int kKeySteps = D / 16, kBlocks = D / 32, kKeyTiles = S::kKeys / 32;
+    const int lane = lane_id(), wave = wave_id(), half = lane >> 5;
+    const int G = a.group;
+    int at = blockIdx.x;
+    const int kvh = at % a.hkv; at /= a.hkv;
+    const int tile0 = a.n_tile - 1 - at % a.n_tile; at /= a.n_tile;        // the rows that see most first
+    const int split = at % a.n_split, unit = at / a.n_split;
+
+    // the unit: its tokens and keys
+    const bool by_group = a.mode == kPrefix;
+    int s0 = unit, s1 = unit + 1, g;
+    if (by_group) {
+        g = unit;
+        s0 = min(max(a.step.group_off[g], 0), a.step.n_seq);
+        s1 = min(max(a.step.group_off[g + 1], s0), a.step.n_seq);
+    } else {
+        g = group_of(a.step, unit);
+    }
+    const int t0 = token_of(a.step, s0), t1 = token_of(a.step, s1);
+    const int rows = (t1 - t0) * G;
+    if (rows <= a.rows_lo || rows > a.rows_hi) return;
+    const int plen = prefix_of(a.step, g);
+    if (by_group && plen == 0) return;
+    const int own = by_group ? 0 : own_len(a.step, unit);
+    const int kb = a.mode == kOwn ? plen : 0, ke = plen + own;
+    const int32_t* ptab = a.step.prefix_table + (int64_t)max(g, 0) * a.step.prefix_stride;
+    const int32_t* otab = a.step.table + (int64_t)s0 * a.step.table_stride;
+
+    // position of a token: where its sequence's keys end, less the tokens behind it
+    auto position = [&](int t) {
+        int seq = unit;
+        if (by_group) {
+            int lo = s0, hi = s1;                   // the last sequence that begins at or before t
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.step.q_off[mid] <= t) lo = mid; else hi = mid;
+            }
+            seq = lo;
+        }
+        return plen + own_len(a.step, seq) - (token_of(a.step, seq + 1) - t);
+    };
+
+    unsigned char* stage = s_mem + (NARROW ? wave * S::kStages * S::kTileBytes : 0);
+    const uint32_t stage_at = __builtin_amdgcn_readfirstlane(lds_address(stage));
+    const int32_t* entries = (const int32_t*)(s_mem + S::kStageBytes + wave * S::kEntrySlots * 256);
+    const uint32_t entries_at = __builtin_amdgcn_readfirstlane(lds_address(entries));
+
+    for (int tile = tile0; tile * S::kRows < rows; tile += a.n_tile) {
+        // rows of the workgroup and of this lane
+        const int row_first = tile * S::kRows, row_last = min(rows, row_first + S::kRows) - 1;
+        const int row = row_first + (NARROW ? 0 : wave * 32) + (lane & 31);
+        const bool mine = row < rows;
+        const int tok = t0 + (mine ? row : rows - 1) / G, head = kvh * G + (mine ? row : rows - 1) % G;
+        const int pos = mine ? position(tok) : -1;
+        const int lim = min(pos, ke - 1);                                  // sees keys kb .. lim that are at or above low, or sinks
+        const int low = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+        // over the workgroup's rows (positions rise inside a sequence; over a group, all rows are looked at)
+        int most = -1, least = 0x7FFFFFFF;
+        if (by_group) {
+            for (int r = row_first + lane; r <= row_last; r += 64) {
+                const int p = position(t0 + r / G);
+                most = max(most, p);
+                least = min(least, p);
+            }
+            for (int w = 32; w >= 1; w >>= 1) { most = max(most, __shfl_xor(most, w)); least = min(least, __shfl_xor(least, w)); }
+        } else {
+            most = position(t0 + row_last / G);
+            least = position(t0 + row_first / G);
+        }
+        most = __builtin_amdgcn_readfirstlane(most);
+        least = __builtin_amdgcn_readfirstlane(least);
+        // over the wavefront's rows: up to where all see all, and from where on
+        int all_to = mine ? lim : 0x7FFFFFFF, all_from = mine ? low : 0;
+        for (int w = 16; w >= 1; w >>= 1) { all_to = min(all_to, __shfl_xor(all_to, w)); all_from = max(all_from, __shfl_xor(all_from, w)); }
+        all_to = __builtin_amdgcn_readfirstlane(all_to);
+        all_from = __builtin_amdgcn_readfirstlane(all_from);
+
+        // the tiles of keys that some row sees: [0, n_sink) and [n_low, n_end) of the grid that begins at kb
+        const int end = min(ke, most + 1);
+        const int n_end = end > kb ? (end - kb + S::kKeys - 1) / S::kKeys : 0;
+        int n_low = 0, n_sink = 0;
+        if (a.window > 0) {
+            n_low = min(n_end, max(0, max(0, least - a.window + 1) - kb) / S::kKeys);
+            n_sink = min(n_low, a.sinks > kb ? (min(a.sinks, end) - kb + S::kKeys - 1) / S::kKeys : 0);
+        }
+        const int seen = n_sink + n_end - n_low;
+        const int per = (seen + a.n_split - 1) / a.n_split;
+        const int v0 = min(seen, split * per), v1 = min(seen, v0 + per);
+        // of these the wavefront takes n
+        const int n = NARROW ? (v1 - v0 - wave + S::kWaves - 1) / S::kWaves : v1 - v0;
+        auto first_key = [&](int i) {
+            const int v = v0 + (NARROW ? wave + i * S::kWaves : i);
+            return kb + (v < n_sink ? v : v - n_sink + n_low) * S::kKeys;
+        };
+
+        // the rows of Q as the second operand: lane l, row l % 32, elements 16 s + 8 (l / 32) and on
+        s8_t q[kKeySteps];
+        {
+            const T* src = (const T*)a.q.data + tok * a.q.token_stride + head * a.q.head_stride + half * 8;
+#pragma unroll
+            for (int s = 0; s < kKeySteps; ++s) q[s] = mine ? *(const s8_t*)(src + s * 16) : s8_t{};
+        }
+
+        // fetching: lane l keeps the entry of row l of the wavefront's part of a tile
+        const int fetch_row = lane & (S::kWaveRows - 1);
+        auto key_of = [&](int i) { return min(first_key(i) + (NARROW ? 0 : wave * S::kWaveRows) + fetch_row, ke - 1); };
+        auto fetch_entries = [&](int i) {
+            const int key = key_of(i);
+            const int32_t* e = key < plen ? ptab + (key >> a.step.prefix_shift) : otab + ((key - plen) >> a.step.shift);
+            fetch4(e, entries_at + (i & (S::kEntrySlots - 1)) * 256);
+        };
+        auto fetch_tile = [&](int i) {
+            const int key = key_of(i);
+            const bool pre = key < plen;
+            const int shift = pre ? a.step.prefix_shift : a.step.shift;
+            const int64_t limit = (pre ? a.step.prefix_entries : a.step.own_entries) - 1;
+            int64_t e = max(entries[(i & (S::kEntrySlots - 1)) * 64 + lane], 0);
+            if (e > limit) e = limit;
+            const int64_t slot = (e << shift) + ((pre ? key : key - plen) & ((1 << shift) - 1));
+            const int64_t off = (slot_offset(a.cache, slot) + kvh * a.cache.head_stride) * 2;
+            const int lo = (int)off, hi = (int)(off >> 32);
+            const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes + (NARROW ? 0 : wave * S::kWaveRows * S::kPitch);
+#pragma unroll
+            for (int u = 0; u < S::kLoads; ++u) {
+                const int r = u * S::kRowsPerLoad + lane / S::kChunks;
+                const int chunk = (lane % S::kChunks) ^ place_swap<S::kChunks>((NARROW ? 0 : wave * S::kWaveRows) + r);
+                const int64_t o = (int64_t)((uint64_t)(uint32_t)__shfl(hi, r) << 32 | (uint32_t)__shfl(lo, r)) + chunk * 16;
+                if (D % 64 == 0 || chunk < D / 8) {
+                    fetch16((const char*)a.cache.k + o, to + u * 1024);
+                    fetch16((const char*)a.cache.v + o, to + S::kKeys * S::kPitch + u * 1024);
+                }
+            }
+        };
+
+        f16v_t o[kBlocks] = {};
+        float m = -INFINITY, l = 0.f;
+
+        // one tile: scores, weights, products
+        auto compute = [&](int i, auto full_tag) __attribute__((always_inline)) {
+            constexpr bool FULL = decltype(full_tag)::value;
+            const int j0 = first_key(i);
+            const unsigned char* ks = stage + (i % S::kStages) * S::kTileBytes;
+            const unsigned char* vs = ks + S::kKeys * S::kPitch;
+            f16v_t x[kKeyTiles];
+#pragma unroll
+            for (int t = 0; t < kKeyTiles; ++t) {
+                x[t] = f16v_t{};
+                const int r = t * 32 + (lane & 31);
+#pragma unroll
+                for (int s = 0; s < kKeySteps; ++s) {
+                    const s8_t k = *(const s8_t*)(ks + r * S::kPitch + (((2 * s + half) ^ place_swap<S::kChunks>(r)) << 4));
+                    x[t] = H::mfma(k, q[s], x[t]);
+                }
+            }
+            auto sees = [&](int j) { return j <= lim && (j >= low || j < a.sinks); };
+            if (!FULL) {
+#pragma unroll
+                for (int t = 0; t < kKeyTiles; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = j0 + t * 32 + (r & 3) + 8 * (r >> 2) + 4 * half;
+                        x[t][r] = sees(j) ? x[t][r] : -INFINITY;
+                    }
+            }
+            float top = x[0][0];
+#pragma unroll
+            for (int t = 0; t < kKeyTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, x[t][r]);
+            top = fmaxf(top, xor_lane<32>(top)) * a.scale_log2;
+            if (__ballot(top > m + kSlack) != 0) {
+                const float m2 = fmaxf(m, top);
+                const float f = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m2);
+                m = m2;
+                l *= f;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) o[b] *= f;
+            }
+            const float minus = (m == -INFINITY ? 0.f : -m) + H::kLift;
+            s8_t p[kKeyTiles * 2];
+            float sum = 0.f;
+#pragma unroll
+            for (int t = 0; t < kKeyTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], a.scale_log2, minus));
+                    sum += w;
+                    p[t * 2 + r / 8][r % 8] = __builtin_bit_cast(short, (T)w);
+                }
+            l += sum;
+            // V transposed, the keys in the order of p: lane l, element l % 32 of a block of 32, keys 16 s + 4 (l / 32) .. + 4 and
+            // eight behind those
+            auto value = [&](int s, int b) __attribute__((always_inline)) {
+                s8_t v;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int r = 16 * s + 8 * u + 4 * half + (lane & 15) / 4;
+                    const int chunk = 4 * b + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+                    const unsigned char* at = vs + r * S::kPitch + ((chunk ^ place_swap<S::kChunks>(r)) << 4) + (lane & 1) * 8;
+                    const s4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[u * 4 + e] = y[e];
+                }
+                return v;
+            };
+            if (!FULL) {
+                // a value that is not finite times the weight zero of a row that does not see it would be NaN
+                uint32_t odd = 0;
+                for (int s = 0; s < kKeyTiles * 2; ++s)
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) {
+                        const s8_t v = value(s, b);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) odd |= ((uint16_t)v[e] & H::kExponent) == H::kExponent;
+                    }
+                if (__ballot(odd != 0) != 0) {
+                    // key by key: the product for all rows, kept by those that see the key
+                    for (int jj = 0; jj < S::kKeys; ++jj) {
+                        const int s = jj >> 4, e = (jj & 3) + 4 * (jj >> 3 & 1);
+                        const bool here = (jj >> 2 & 1) == half, keep = sees(j0 + jj);
+                        s8_t w{};
+#pragma unroll
+                        for (int u = 0; u < kKeyTiles * 2; ++u)
+#pragma unroll
+                            for (int i8 = 0; i8 < 8; ++i8)
+                                if (u == s && i8 == e && here) w[i8] = p[u][i8];
+#pragma unroll
+                        for (int b = 0; b < kBlocks; ++b) {
+                            s8_t v = value(s, b);
+#pragma unroll
+                            for (int i8 = 0; i8 < 8; ++i8) v[i8] = i8 == e && here ? v[i8] : (short)0;
+                            const f16v_t y = H::mfma(v, w, f16v_t{});
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) o[b][r] += keep ? y[r] : 0.f;
+                        }
+                    }
+                    return;
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < kKeyTiles * 2; ++s)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) o[b] = H::mfma(value(s, b), p[s], o[b]);
+        };
+
+        if (n > 0) {
+#pragma unroll
+            for (int i = 0; i < 2 * S::kAhead; ++i)
+                if (i < n) fetch_entries(i);
+            wait_loads<0>();
+#pragma unroll
+            for (int i = 0; i < S::kAhead; ++i)
+                if (i < n) fetch_tile(i);
+        }
+        for (int i = 0; i < n; ++i) {
+            // tile i has arrived: kAhead - 1 younger ones may be on their way
+            if (S::kAhead > 1 && i + S::kAhead <= n) wait_loads<(S::kAhead - 1) * 2 * S::kLoads>();
+            else wait_loads<0>();
+            if (!NARROW) barrier();      // for every wavefront, and the tile before has been read
+            if (i + S::kAhead < n) fetch_tile(i + S::kAhead);
+            if (i + 2 * S::kAhead < n) fetch_entries(i + 2 * S::kAhead);
+            const int j0 = first_key(i);
+            if (!NARROW && row - (lane & 31) >= rows) continue;            // no rows: this wavefront only fetches
+            const bool full = j0 + S::kKeys - 1 <= all_to && (j0 >= all_from || j0 + S::kKeys <= a.sinks);
+            if (full) compute(i, std::true_type{});
+            else compute(i, std::false_type{});
+        }
+        l += xor_lane<32>(l);
+
+        // what is left to do with the sums
+        const bool last = a.mode == kConcat && a.n_split == 1;             // they are complete
+        auto finish = [&](int t, int h, float mm, float ll) {              // by one lane per row
+            if (a.lse && last) a.lse[(int64_t)t * a.hq + h] = ll > 0.f || ll != ll ? (mm + __builtin_amdgcn_logf(ll) - H::kLift) * 0.6931471805599453f : -INFINITY;
+            if (a.parts == 0) return;
+            float2* ml = a.part_ml + ((int64_t)t * a.hq + h) * a.parts;
+            ml[a.part0 + split] = make_float2(last ? NAN : mm, ll);
+            if (split == 0) {
+                for (int i = a.n_split; i < a.n_part; ++i) ml[a.part0 + i] = make_float2(-INFINITY, 0.f);
+                if (a.mode == kOwn && plen == 0)                           // no prefix pass comes by here
+                    for (int i = 0; i < a.part0; ++i) ml[i] = make_float2(-INFINITY, 0.f);
+            }
+        };
+        if (!NARROW) {
+            if (mine) {
+                if (half == 0) finish(tok, head, m, l);
+                const float f = last ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f;
+                T* out = (T*)a.out.data + tok * a.out.token_stride + head * a.out.head_stride;
+                float* part = last ? nullptr : a.part_o + (((int64_t)tok * a.hq + head) * a.parts + a.part0 + split) * D;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        const int d = 32 * b + 2 * r + 4 * half;
+                        if (last) {
+                            s4_t y;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) y[e] = __builtin_bit_cast(short, (T)(o[b][r + e] * f));
+                            *(s4_t*)(out + d) = y;
+                        } else if (v1 > v0) {
+                            *(float4*)(part + d) = make_float4(o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]);
+                        }
+                    }
+            }
+            barrier();                   // the tiles have been read before the next rows' are fetched
+        } else {
+            // the wavefronts' sums are joined through LDS: [wavefront][row][D], and [wavefront][row] (m, l)
+            __syncthreads();
+            float* so = (float*)s_mem;
+            float2* sm = (float2*)(s_mem + (size_t)S::kWaves * 32 * D * 4);
+            if (half == 0) sm[wave * 32 + (lane & 31)] = make_float2(m, l);
+            __syncthreads();
+            float mm = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < S::kWaves; ++w) mm = fmaxf(mm, sm[w * 32 + (lane & 31)].x);
+            const float f = m == -INFINITY ? (m != m ? m : 0.f) : __builtin_amdgcn_exp2f(m - mm);
+            if (mine) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4)
+                        *(float4*)(so + ((size_t)wave * 32 + (lane & 31)) * D + 32 * b + 2 * r + 4 * half) =
+                            make_float4(o[b][r] * f, o[b][r + 1] * f, o[b][r + 2] * f, o[b][r + 3] * f);
+            }
+            __syncthreads();
+            const int count = row_last - row_first + 1;
+            for (int c = threadIdx.x; c < count * (D / 4); c += S::kWaves * 64) {
+                const int r = c / (D / 4), d = c % (D / 4) * 4;
+                const int t = t0 + (row_first + r) / G, h = kvh * G + (row_first + r) % G;
+                float top = -INFINITY, sum = 0.f;
+                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < S::kWaves; ++w) top = fmaxf(top, sm[w * 32 + r].x);
+#pragma unroll
+                for (int w = 0; w < S::kWaves; ++w) {
+                    const float2 p = sm[w * 32 + r];
+                    sum += p.x == -INFINITY ? p.y : p.y * __builtin_amdgcn_exp2f(p.x - top);
+                    const float4 z = *(const float4*)(so + ((size_t)w * 32 + r) * D + d);
+                    y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+                }
+                if (d == 0) finish(t, h, top, sum);
+                if (last) {
+                    const float g1 = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                    s4_t z = {__builtin_bit_cast(short, (T)(y.x * g1)), __builtin_bit_cast(short, (T)(y.y * g1)),
+                              __builtin_bit_cast(short, (T)(y.z * g1)), __builtin_bit_cast(short, (T)(y.w * g1))};
+                    *(s4_t*)((T*)a.out.data + t * a.out.token_stride + h * a.out.head_stride + d) = z;
+                } else if (v1 > v0) {
+                    *(float4*)(a.part_o + (((int64_t)t * a.hq + h) * a.parts + a.part0 + split) * D + d) = y;
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Joins a row's partial sums: one wavefront per token and query head.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+    constexpr int kPer = (D + 63) / 64;
+    const int64_t row = (int64_t)blockIdx.x * 4 + wave_id();
+    const int lane = lane_id();
+    if (row >= (int64_t)a.step.n_tokens * a.hq) return;
+    const float2* ml = a.part_ml + row * a.parts;
+    float top = -INFINITY;
+    bool done = false;
+    for (int i = lane; i < a.parts; i += 64) { const float x = ml[i].x; done |= x != x; top = fmaxf(top, x); }
+    if (__ballot(done)) return;
+    for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+    float sum = 0.f, o[kPer] = {};
+    for (int i = 0; i < a.parts; ++i) {
+        const float2 p = ml[i];
+        if (p.x == -INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(p.x - top);
+        sum += p.y * f;
+        const float* src = a.part_o + (row * a.parts + i) * D;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (e * 64 + lane < D) o[e] += src[e * 64 + lane] * f;
+    }
+    const int t = (int)(row / a.hq), h = (int)(row % a.hq);
+    T* out = (T*)a.out.data + t * a.out.token_stride + h * a.out.head_stride;
+    const float f = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+        if (e * 64 + lane < D) out[e * 64 + lane] = (T)(o[e] * f);
+    if (a.lse && lane == 0)
+        a.lse[row] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum) - Half<T>::kLift) * 0.6931471805599453f : -INFINITY;
 }
 
 static int check_heads(const ivf_kv_cache* cache, int n_q_heads, int window, int sinks) {
@@ -87,16 +518,100 @@ static int check_heads(const ivf_kv_cache* cache, int n_q_heads, int window, int
     return IVF_OK;
 }
 
-template <typename T>
-static hipError_t launch_attend(const AttendArgs& a, int d, hipStream_t s) {
-    const dim3 grid(std::min(a.step.n_tokens, 1 << 20), a.hq), block(64);
-    switch (d) {
-    case 64: hipLaunchKernelGGL((attend_rows_kernel<T, 64>), grid, block, 0, s, a); break;
-    case 96: hipLaunchKernelGGL((attend_rows_kernel<T, 96>), grid, block, 0, s, a); break;
-    case 128: hipLaunchKernelGGL((attend_rows_kernel<T, 128>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((attend_rows_kernel<T, 256>), grid, block, 0, s, a); break;
+// How a call is cut into passes.
+struct AttendPlan {
+    bool shared;                     // the prefix in a pass of its own
+    bool narrow, wide;               // kernels that the own (or all) keys need
+    bool prefix_narrow;
+    int split_narrow, split_wide, split_prefix;
+    int tiles_narrow, tiles_wide, tiles_prefix;      // workgroups along a unit's rows
+    int parts, part_own, n_own;
+};
+
+constexpr int kNarrowRows = 32, kWideRows = 128, kAllRows = 0x7FFFFFFF;
+
+static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv, int group, int window, int sinks) {
+    AttendPlan p{};
+    const int64_t rows = (int64_t)sv.n_tokens * group;
+    auto known = [](int hint, int64_t cap) { return hint > 0 ? std::min<int64_t>(hint, cap) : cap; };
+    const int64_t len = known(st->max_len, sv.own_cap), pre = sv.n_groups > 0 ? known(st->max_prefix, sv.prefix_cap) : 0;
+    const int64_t most_q = known(st->max_q, sv.n_tokens);
+    p.shared = pre > 0 && sv.n_seq > sv.n_groups && rows < (int64_t)sv.n_seq * kWideRows;
+    const int64_t keys_all = p.shared ? len : len + pre;
+    // keys that a row reads: of a window a tile more
+    auto read_keys = [&](int64_t keys) { return window > 0 ? std::min<int64_t>(keys, (int64_t)window + std::min<int64_t>(sinks, keys) + most_q + 64) : keys; };
+    const int64_t keys = read_keys(keys_all);
+    p.wide = sv.n_seq == 1 ? rows > kNarrowRows : most_q * group > kNarrowRows;
+    p.narrow = sv.n_seq == 1 ? !p.wide : true;
+    auto split = [](int64_t units, int64_t want, int64_t keys, int64_t least) {
+        const int64_t most = (keys + least - 1) / least;
+        return (int)std::max<int64_t>(1, std::min<int64_t>({(want + units - 1) / units, most, 64}));
+    };
+    p.tiles_narrow = 1;
+    // (unknown: twice what sequences of equal lengths would need)
+    const int64_t tile_rows = st->max_q > 0 || sv.n_seq == 1 ? most_q * group : std::min(rows, 2 * rows / sv.n_seq);
+    p.tiles_wide = (int)std::max<int64_t>(1, (tile_rows + kWideRows - 1) / kWideRows);
+    if (p.narrow) p.split_narrow = split((int64_t)sv.n_seq * hkv, 4096, keys, 512);
+    if (p.wide) p.split_wide = split(hkv * ((rows + kWideRows - 1) / kWideRows + sv.n_seq - 1), 512, keys, 512);
+    p.n_own = std::max(p.split_narrow, p.split_wide);
+    if (p.shared) {
+        const int64_t group_rows = rows / sv.n_groups;
+        p.prefix_narrow = group_rows <= kNarrowRows;
+        const int tile = p.prefix_narrow ? kNarrowRows : kWideRows;
+        p.tiles_prefix = (int)std::max<int64_t>(1, (group_rows + tile - 1) / tile);
+        p.split_prefix = split((int64_t)sv.n_groups * hkv * p.tiles_prefix, p.prefix_narrow ? 2048 : 512, read_keys(pre), p.prefix_narrow ? 512 : 256);
+        p.part_own = p.split_prefix;
     }
+    p.parts = p.shared || p.n_own > 1 ? p.part_own + p.n_own : 0;
+    return p;
+}
+
+static size_t plan_bytes(const AttendPlan& p, int64_t rows, int d) { return (size_t)(rows * p.parts) * ((size_t)d * 4 + 8); }
+
+template <typename T, int D, bool NARROW>
+static hipError_t launch_pass(AttendArgs a, int64_t units, hipStream_t s) {
+    using S = Shape<D, NARROW>;
+    const int64_t grid = units * a.n_split * a.n_tile * a.hkv;
+    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+    static const hipError_t allowed = hipFuncSetAttribute((const void*)attend_kernel<T, D, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+    if (allowed != hipSuccess) return allowed;
+    hipLaunchKernelGGL((attend_kernel<T, D, NARROW>), dim3((unsigned)grid), dim3(S::kWaves * 64), S::kLds, s, a);
     return hipGetLastError();
+}
+
+template <typename T, int D>
+static hipError_t launch_attend(AttendArgs a, const AttendPlan& p, hipStream_t s) {
+    const int64_t rows = (int64_t)a.step.n_tokens * a.hq;
+    hipError_t e;
+    a.parts = p.parts;
+    if (p.shared) {
+        a.mode = kPrefix; a.part0 = 0; a.n_part = a.n_split = p.split_prefix; a.n_tile = p.tiles_prefix; a.rows_lo = 0; a.rows_hi = kAllRows;
+        if ((e = p.prefix_narrow ? launch_pass<T, D, true>(a, a.step.n_groups, s) : launch_pass<T, D, false>(a, a.step.n_groups, s))) return e;
+    }
+    a.mode = p.shared ? kOwn : kConcat; a.part0 = p.part_own; a.n_part = p.n_own;
+    if (p.wide) {
+        a.n_split = p.split_wide; a.n_tile = p.tiles_wide; a.rows_lo = p.narrow ? kNarrowRows : 0; a.rows_hi = kAllRows;
+        if ((e = launch_pass<T, D, false>(a, a.step.n_seq, s))) return e;
+    }
+    if (p.narrow) {
+        a.n_split = p.split_narrow; a.n_tile = p.tiles_narrow; a.rows_lo = 0; a.rows_hi = p.wide ? kNarrowRows : kAllRows;
+        if ((e = launch_pass<T, D, true>(a, a.step.n_seq, s))) return e;
+    }
+    if (p.parts > 0) {
+        hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+template <typename T>
+static hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int d, hipStream_t s) {
+    switch (d) {
+    case 64: return launch_attend<T, 64>(a, p, s);
+    case 96: return launch_attend<T, 96>(a, p, s);
+    case 128: return launch_attend<T, 128>(a, p, s);
+    default: return launch_attend<T, 256>(a, p, s);
+    }
 }
 
 }  // namespace ivf
@@ -110,26 +625,31 @@ extern "C" int ivf_attend_workspace(const ivf_kv_step* step, const ivf_kv_cache*
     if (rc) return rc;
     if ((rc = check_heads(cache, n_q_heads, window, sinks))) return rc;
     if (!bytes) return fail(IVF_EINVAL, "bytes is NULL");
-    *bytes = 0;
+    const AttendPlan p = plan_attend(step, sv, cache->n_heads, n_q_heads / cache->n_heads, window, sinks);
+    *bytes = plan_bytes(p, (int64_t)sv.n_tokens * n_q_heads, cache->d);
     return IVF_OK;
 }
 
 extern "C" int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_rows* q, int32_t n_q_heads,
                           const ivf_rows* out, float* lse, float scale, int32_t window, int32_t sinks, void* workspace,
                           size_t workspace_bytes, void* stream) {
-    size_t need = 0;
-    int rc = ivf_attend_workspace(step, cache, n_q_heads, window, sinks, &need);
-    if (rc) return rc;
     AttendArgs a{};
-    if ((rc = make_views(step, cache, &a.cache, &a.step))) return rc;
+    int rc = make_views(step, cache, &a.cache, &a.step);
+    if (rc) return rc;
+    if ((rc = check_heads(cache, n_q_heads, window, sinks))) return rc;
     if ((rc = check_rows(q, "q")) || (rc = check_rows(out, "out"))) return rc;
     if (!(scale > 0.f) || scale > 1e30f) return fail(IVF_EINVAL, "scale must be positive");
     if (((uintptr_t)workspace & 15u) != 0) return fail(IVF_EINVAL, "workspace must be 16-byte aligned");
+    a.q = *q; a.out = *out; a.lse = lse; a.scale_log2 = scale * 1.4426950408889634f;
+    a.hq = n_q_heads; a.hkv = cache->n_heads; a.group = n_q_heads / cache->n_heads; a.window = window; a.sinks = sinks;
+    const AttendPlan p = plan_attend(step, a.step, a.hkv, a.group, window, sinks);
+    const int64_t rows = (int64_t)a.step.n_tokens * n_q_heads;
+    const size_t need = plan_bytes(p, rows, cache->d);
     if (workspace_bytes < need || (need > 0 && !workspace))
         return fail(IVF_EINVAL, "this call needs %zu bytes of workspace (got %zu)", need, workspace ? workspace_bytes : (size_t)0);
-    a.q = *q; a.out = *out; a.lse = lse; a.scale = scale;
-    a.hq = n_q_heads; a.group = n_q_heads / cache->n_heads; a.window = window; a.sinks = sinks;
-    HIP_TRY(cache->dtype == IVF_F16 ? launch_attend<_Float16>(a, cache->d, (hipStream_t)stream)
-                                    : launch_attend<__bf16>(a, cache->d, (hipStream_t)stream));
+    a.part_o = (float*)workspace;
+    a.part_ml = (float2*)((float*)workspace + (size_t)(rows * p.parts) * cache->d);
+    HIP_TRY(cache->dtype == IVF_F16 ? launch_attend<_Float16>(a, p, cache->d, (hipStream_t)stream)
+                                    : launch_attend<__bf16>(a, p, cache->d, (hipStream_t)stream));
     return IVF_OK;
 }
