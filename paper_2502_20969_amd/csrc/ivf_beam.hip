@@ -6,6 +6,13 @@
 namespace ivf {
 using namespace dev;
 
+// Workgroup `part` of a row goes over a share of its vocabulary, tile by tile, and leaves its k best logits, sorted, and
+// (maximum, sum); the workgroup of a prompt joins the parts of its rows, picks, and moves the states' rows.
+struct BeamMove {
+    const uint8_t* from;
+    uint8_t* to;
+    int64_t row_bytes, from_stride, to_stride;
+};
 struct BeamArgs {
     const void* logits;
     int64_t row_stride;
@@ -14,10 +21,18 @@ struct BeamArgs {
     float* scores_out;
     int32_t *parent, *token;
     uint8_t* done_out;
-    unsigned long long* keys;     // [rows][k] the row's best logits, best first, packed with their tokens; 0 = none
-    float* lse;                   // [rows][2] maximum, and logarithm of the sum
-    int prompts, beams, vocab, k, eos;
+    unsigned long long* keys;     // [rows][parts][k] best logits, best first, packed with their tokens; 0 = none
+    float2* sums;                 // [rows][parts] maximum, and sum of exp(x - maximum)
+    int prompts, beams, vocab, k, eos, parts, share;     // share: tokens of a part
+    BeamMove moves[IVF_MAX_BEAM_STATES];
+    int n_moves;
 };
+
+constexpr int kBeamThreads = 256;
+constexpr int kBeamElems = 32;                           // logits of a thread's part of a tile
+constexpr int kBeamTile = kBeamThreads * kBeamElems;
+constexpr int kBeamPool = 512;                           // candidates ranked at once
+constexpr float kLog2e = 1.4426950408889634f;
 
 // A logit and its token as one word: larger is better, equal logits by lower token.  No continuation: 0.
 __device__ __forceinline__ unsigned long long pack_logit(float x, uint32_t token) {
@@ -31,104 +46,314 @@ __device__ __forceinline__ float logit_of(unsigned long long key) {
     return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
-__device__ __forceinline__ unsigned long long block_max(unsigned long long x, unsigned long long* s) {
+__device__ __forceinline__ float wave_max(float x) {
+    for (int w = 32; w >= 1; w >>= 1) x = fmaxf(x, __shfl_xor(x, w));
+    return x;
+}
+__device__ __forceinline__ unsigned long long wave_max(unsigned long long x) {
     for (int w = 32; w >= 1; w >>= 1) x = max(x, (unsigned long long)__shfl_xor((long long)x, w));
-    __syncthreads();
-    if (lane_id() == 0) s[wave_id()] = x;
-    __syncthreads();
-    for (int i = 0; i < 4; ++i) x = max(x, s[i]);
     return x;
 }
 
-// One workgroup per row: the maximum, the sum, then the k best, one pass over the row each.
-template <typename T>
-__global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a) {
-    __shared__ unsigned long long s_best[4];
-    __shared__ float s_sum[4];
-    const int row = blockIdx.x, tid = threadIdx.x;
-    const T* x = (const T*)a.logits + row * a.row_stride;
-    unsigned long long last = ~0ull;
-    float top = 0.f;
-    for (int i = 0; i < a.k; ++i) {
-        unsigned long long best = 0;
-        for (int t = tid; t < a.vocab; t += 256) {
-            const unsigned long long key = pack_logit((float)x[t], t);
-            if (key < last) best = max(best, key);
-        }
-        last = block_max(best, s_best);
-        if (i == 0) top = logit_of(last);
-        if (tid == 0) a.keys[(int64_t)row * a.k + i] = last;
-        if (last == 0) {
-            for (int j = i + 1 + tid; j < a.k; j += 256) a.keys[(int64_t)row * a.k + j] = 0;
-            break;
-        }
+// 16 bytes of logits from any element
+template <typename T> struct Logits;
+template <> struct Logits<float> {
+    static constexpr int kPer = 4;
+    static __device__ __forceinline__ float get(const uint4& v, int e) { return __uint_as_float((&v.x)[e]); }
+};
+template <> struct Logits<_Float16> {
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ float get(const uint4& v, int e) {
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)((&v.x)[e / 2] >> (16 * (e & 1))));
     }
-    float sum = 0.f;
-    for (int t = tid; t < a.vocab; t += 256) {
-        const float v = (float)x[t];
-        if (v > -INFINITY) sum += v == top ? 1.f : expf(v - top);
+};
+template <> struct Logits<__bf16> {
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ float get(const uint4& v, int e) {
+        const uint32_t w = (&v.x)[e / 2];
+        return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
     }
-    sum = group_sum<64>(sum);
-    if (lane_id() == 0) s_sum[wave_id()] = sum;
-    __syncthreads();
-    if (tid == 0) {
-        a.lse[row * 2] = top;
-        a.lse[row * 2 + 1] = logf(s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]);
+};
+typedef u4_t u4_half_t __attribute__((aligned(2)));
+
+// The k best words of pool[0 .. n) to best[0 .. k), best first, by counting; best past n is 0.  All threads call it.
+__device__ __forceinline__ void rank_pool(const unsigned long long* pool, int n, unsigned long long* best, int k) {
+    for (int i = threadIdx.x; i < k; i += kBeamThreads)
+        if (i >= n) best[i] = 0;
+    for (int i = threadIdx.x; i < n; i += kBeamThreads) {
+        const unsigned long long mine = pool[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += pool[j] > mine;
+        if (rank < k) best[rank] = mine;
     }
 }
 
-// One wavefront per prompt: k times the best candidate of the rows' lists, a lane per row.
-__global__ __launch_bounds__(64) void beam_pick_kernel(BeamArgs a) {
-    const int prompt = blockIdx.x, b = threadIdx.x, row0 = prompt * a.beams, row = row0 + b;
-    const bool mine = b < a.beams;
-    const bool done = mine && a.done_in && a.done_in[row];
-    const float run = mine ? a.scores_in[row] : -INFINITY;
-    int at = 0;
-    for (int i = 0; i < a.k; ++i) {
-        float score = -INFINITY;
-        int token = -1;
-        if (mine && at < a.k) {
-            if (done) {
-                if (at == 0) { score = run; token = a.eos; }
-            } else {
-                const unsigned long long key = a.keys[(int64_t)row * a.k + at];
-                const float v = logit_of(key), top = a.lse[row * 2];
-                if (key) { score = run + ((v == top ? 0.f : v - top) - a.lse[row * 2 + 1]); token = (int)~(uint32_t)key; }
+// Bound by reading the logits once: two tiles of 16-byte loads are on their way at a time (the one behind is requested
+// before one is worked on).  A thread keeps its own maximum and sum.  What may belong to the k best is rare: in the
+// first tile what reaches a value that k of the threads' maxima reach, later what is better than the k-th best so far;
+// it goes to a pool in LDS and is ranked by counting.
+template <typename T>
+__global__ __launch_bounds__(kBeamThreads) void beam_part_kernel(BeamArgs a) {
+    constexpr int kPer = Logits<T>::kPer, kLoads = kBeamElems / kPer;
+    __shared__ unsigned long long s_pool[kBeamPool + kBeamThreads];
+    __shared__ unsigned long long s_best[IVF_MAX_BEAMS];
+    __shared__ float s_edge[4];
+    __shared__ float2 s_sum[4];
+    __shared__ int s_count;
+    const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x, k = a.k;
+    if (a.done_in && a.done_in[row]) return;               // its only continuation needs no logits
+    const int begin = part * a.share, end = min(a.vocab, begin + a.share);
+    const T* x = (const T*)a.logits + row * a.row_stride;
+    const int tiles = (end - begin + kBeamTile - 1) / kBeamTile;
+    auto request = [&](int tile, uint4 (&raw)[kLoads]) __attribute__((always_inline)) {
+        const int t0 = begin + tile * kBeamTile + tid * kPer;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int t = t0 + i * kBeamThreads * kPer;
+            if (t + kPer <= end) {
+                const u4_t v = *(const u4_half_t*)(x + t);
+                raw[i] = make_uint4(v.x, v.y, v.z, v.w);
+            } else {                                       // the last few, one by one; none is taken for -inf below
+                uint32_t w[4] = {0, 0, 0, 0};
+                for (int e = 0; e < kPer; ++e) {
+                    if (t + e >= end) break;
+                    if (kPer == 4) w[e] = __float_as_uint((float)x[t + e]);
+                    else w[e / 2] |= (uint32_t)((const uint16_t*)x)[t + e] << (16 * (e & 1));
+                }
+                raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
-        if (!(score > -INFINITY)) token = -1;
-        float best = token >= 0 || (done && at == 0 && score > -INFINITY) ? score : -INFINITY;
-        float top = best;
-        for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-        const uint64_t at_top = __ballot(best == top && best > -INFINITY);
-        const int from = at_top ? __builtin_ctzll(at_top) : 0;
-        const int o = prompt * a.k + i;
-        if (b == from) {
-            a.scores_out[o] = at_top ? score : -INFINITY;
-            a.parent[o] = row0 + from;
-            a.token[o] = at_top ? token : -1;
-            a.done_out[o] = !at_top || done || token == a.eos;
-            ++at;
+    };
+    float m = -INFINITY, sum = 0.f;
+    unsigned long long least = 0;                          // the k-th best so far; 0: fewer
+    int have = 0;
+    uint4 next[kLoads];
+    if (tiles > 0) request(0, next);
+    for (int tile = 0; tile < tiles; ++tile) {
+        uint4 raw[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) raw[i] = next[i];
+        if (tile + 1 < tiles) request(tile + 1, next);
+        const int t0 = begin + tile * kBeamTile + tid * kPer;
+        auto token = [&](int i, int e) { return t0 + i * kBeamThreads * kPer + e; };
+        auto value = [&](int i, int e) __attribute__((always_inline)) {      // -inf where there is none, and for NaN
+            const float v = fmaxf(Logits<T>::get(raw[i], e), -INFINITY);
+            return token(i, e) < end ? v : -INFINITY;
+        };
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) top = fmaxf(top, value(i, e));
+        if (top > -INFINITY) {
+            const float m2 = fmaxf(m, top);
+            if (m2 == INFINITY) {                          // infinite logits share the probability
+                if (m < INFINITY) sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) sum += value(i, e) == INFINITY ? 1.f : 0.f;
+            } else {
+                float add = 0.f;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) add += __builtin_amdgcn_exp2f((value(i, e) - m2) * kLog2e);
+                sum = sum * __builtin_amdgcn_exp2f((m - m2) * kLog2e) + add;
+            }
+            m = m2;
         }
+        // what has to be reached: above `least`, or in the first tile at least `edge`, which k values reach if so many threads
+        // have any
+        float edge = -INFINITY;
+        if (tile == 0) {
+            float left = top;
+            // wavefronts whose threads all have a first load take part, in equal shares
+            const int waves = max(1, min(4, (end - begin) / (64 * kPer)));
+            const int need = (k + waves - 1) / waves;
+            for (int i = 0; i < need; ++i) {
+                edge = wave_max(left);
+                const uint64_t at = __ballot(left == edge);
+                if (lane_id() == __builtin_ctzll(at)) left = -INFINITY;
+            }
+            if (wave_id() >= waves) edge = INFINITY;
+            if (lane_id() == 0) s_edge[wave_id()] = edge;
+            __syncthreads();
+            edge = fminf(fminf(s_edge[0], s_edge[1]), fminf(s_edge[2], s_edge[3]));
+        }
+        auto passes = [&](float v, int t) { return v >= edge && pack_logit(v, t) > least; };
+        int mine = 0;
+        if (top >= edge && pack_logit(top, 0) > least) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) mine += passes(value(i, e), token(i, e));
+        }
+        if (tid == 0) s_count = have;
+        __syncthreads();
+        // room for them is taken one after the other; more than the pool holds (masses of equal values) go in by single
+        // elements, ranked in between
+        int at = mine ? atomicAdd(&s_count, mine) : 0;
+        __syncthreads();
+        const int total = s_count;
+        if (total == have) continue;
+        if (total <= kBeamPool) {
+            if (mine) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) {
+                        const float v = value(i, e);
+                        if (passes(v, token(i, e))) s_pool[at++] = pack_logit(v, token(i, e));
+                    }
+            }
+            __syncthreads();
+            rank_pool(s_pool, total, s_best, k);
+            have = min(total, k);
+            __syncthreads();
+            least = have == k ? s_best[k - 1] : 0;
+            for (int i = tid; i < have; i += kBeamThreads) s_pool[i] = s_best[i];
+            __syncthreads();
+        } else {
+            for (int i = 0; i < kLoads; ++i)
+                for (int e = 0; e < kPer; ++e) {
+                    float v = -INFINITY;                   // element (i, e), without indexing registers
+#pragma unroll
+                    for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+                        for (int w = 0; w < kPer; ++w) if (u == i && w == e) v = value(u, w);
+                    if (tid == 0) s_count = have;
+                    __syncthreads();
+                    if (passes(v, token(i, e))) s_pool[atomicAdd(&s_count, 1)] = pack_logit(v, token(i, e));
+                    __syncthreads();
+                    const int n = s_count;
+                    if (n == have) continue;
+                    rank_pool(s_pool, n, s_best, k);
+                    have = min(n, k);
+                    __syncthreads();
+                    least = have == k ? s_best[k - 1] : 0;
+                    for (int j = tid; j < have; j += kBeamThreads) s_pool[j] = s_best[j];
+                    __syncthreads();
+                }
+        }
+    }
+    unsigned long long* out = a.keys + (int64_t)blockIdx.x * k;
+    for (int i = tid; i < k; i += kBeamThreads) out[i] = i < have ? s_pool[i] : 0;
+    const float wm = wave_max(m);
+    float ws = m == -INFINITY ? 0.f : m == wm ? sum : wm == INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f((m - wm) * kLog2e);
+    ws = group_sum<64>(ws);
+    if (lane_id() == 0) s_sum[wave_id()] = make_float2(wm, ws);
+    __syncthreads();
+    if (tid == 0) {
+        const float bm = fmaxf(fmaxf(s_sum[0].x, s_sum[1].x), fmaxf(s_sum[2].x, s_sum[3].x));
+        float bs = 0.f;
+        for (int w = 0; w < 4; ++w)
+            bs += s_sum[w].x == bm ? s_sum[w].y : s_sum[w].x == -INFINITY || bm == INFINITY ? 0.f : s_sum[w].y * __builtin_amdgcn_exp2f((s_sum[w].x - bm) * kLog2e);
+        a.sums[blockIdx.x] = make_float2(bm, bs);
     }
 }
 
-struct BeamMove {
-    const uint8_t* from;
-    uint8_t* to;
-    int64_t row_bytes, from_stride, to_stride;
-};
-struct BeamMoves { BeamMove m[IVF_MAX_BEAM_STATES]; };
+__device__ __forceinline__ void move_row(const BeamMove& m, int64_t from_row, int64_t to_row, int i0, int step) {
+    const uint8_t* from = m.from + from_row * m.from_stride;
+    uint8_t* to = m.to + to_row * m.to_stride;
+    const bool wide = (((uintptr_t)from | (uintptr_t)to) & 15u) == 0, words = (((uintptr_t)from | (uintptr_t)to) & 3u) == 0;
+    int64_t done = 0;
+    if (wide) {
+        const int64_t n = m.row_bytes / 16;
+        for (int64_t i = i0; i < n; i += step) ((uint4*)to)[i] = ((const uint4*)from)[i];
+        done = n * 16;
+    } else if (words) {
+        const int64_t n = m.row_bytes / 4;
+        for (int64_t i = i0; i < n; i += step) ((uint32_t*)to)[i] = ((const uint32_t*)from)[i];
+        done = n * 4;
+    }
+    for (int64_t i = done + i0; i < m.row_bytes; i += step) to[i] = from[i];
+}
 
-// Rows of the states to their new places, one workgroup per row and state.
-__global__ __launch_bounds__(256) void beam_move_kernel(BeamMoves moves, const int32_t* parent) {
-    const BeamMove& m = moves.m[blockIdx.y];
-    const uint8_t* from = m.from + parent[blockIdx.x] * m.from_stride;
-    uint8_t* to = m.to + (int64_t)blockIdx.x * m.to_stride;
-    const bool wide = (((uintptr_t)from | (uintptr_t)to) & 15u) == 0;
-    const int64_t n = wide ? m.row_bytes / 16 : 0;
-    for (int64_t i = threadIdx.x; i < n; i += 256) ((uint4*)to)[i] = ((const uint4*)from)[i];
-    for (int64_t i = n * 16 + threadIdx.x; i < m.row_bytes; i += 256) to[i] = from[i];
+// One workgroup per prompt.  A wavefront joins the parts of a row, a lane per part: k times the best of the lists' heads.
+// Then one wavefront picks from the rows, a lane per row, in the same way; at last all move the states' rows, where they
+// are small.  Latency bounds it.
+constexpr int kPickThreads = 512;
+__global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
+    __shared__ float s_score[IVF_MAX_BEAMS * IVF_MAX_BEAMS];
+    __shared__ int32_t s_token[IVF_MAX_BEAMS * IVF_MAX_BEAMS];
+    __shared__ int32_t s_parent[IVF_MAX_BEAMS];
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    const int prompt = blockIdx.x, lane = lane_id(), wave = wave_id(), k = a.k, row0 = prompt * a.beams;
+    unsigned long long* lists = (unsigned long long*)s_raw + (size_t)wave * a.parts * k;
+    for (int b = wave; b < a.beams; b += kPickThreads / 64) {
+        const int64_t row = row0 + b;
+        const float run = a.scores_in[row];
+        const bool done = a.done_in && a.done_in[row];
+        float* score = s_score + b * k;
+        int32_t* token = s_token + b * k;
+        if (done || !(run > -INFINITY)) {
+            if (lane < k) { score[lane] = done && lane == 0 ? run : -INFINITY; token[lane] = a.eos; }
+            continue;
+        }
+        for (int i = lane; i < a.parts * k; i += 64) lists[i] = a.keys[row * a.parts * k + i];
+        const float2 ps = lane < a.parts ? a.sums[row * a.parts + lane] : make_float2(-INFINITY, 0.f);
+        const float top = wave_max(ps.x);
+        const float sum = group_sum<64>(ps.x == top ? ps.y : ps.x == -INFINITY || top == INFINITY ? 0.f : ps.y * __builtin_amdgcn_exp2f((ps.x - top) * kLog2e));
+        const float lse = logf(sum);
+        __builtin_amdgcn_wave_barrier();
+        int at = 0;
+        unsigned long long mine = 0;                       // the lane's result: the best of rank `lane`
+        unsigned long long head = lane < a.parts ? lists[lane * k] : 0;
+        for (int i = 0; i < k; ++i) {
+            const unsigned long long best = wave_max(head);
+            if (lane == i) mine = best;
+            if (best == 0) break;
+            if (head == best) { ++at; head = at < k ? lists[lane * k + at] : 0; }
+        }
+        if (lane < k) {
+            const float v = logit_of(mine);
+            score[lane] = mine ? run + ((v == top ? 0.f : v - top) - lse) : -INFINITY;
+            token[lane] = (int32_t)~(uint32_t)mine;
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {
+        const bool mine = lane < a.beams;
+        int at = 0;
+        float head = mine ? s_score[lane * k] : -INFINITY;
+        for (int i = 0; i < k; ++i) {
+            const float top = wave_max(head);
+            const uint64_t reach = __ballot(head == top && top > -INFINITY);
+            const int from = reach ? __builtin_ctzll(reach) : 0;
+            if (lane == from) {
+                const int o = prompt * k + i;
+                const int token = reach ? s_token[lane * k + at] : -1;
+                const bool done = reach && a.done_in && a.done_in[row0 + from];
+                a.scores_out[o] = top;
+                a.parent[o] = row0 + from;
+                a.token[o] = token;
+                a.done_out[o] = !reach || done || token == a.eos;
+                s_parent[i] = row0 + from;
+                if (reach) { ++at; head = at < k ? s_score[lane * k + at] : -INFINITY; }
+            }
+        }
+    }
+    __syncthreads();
+    for (int j = wave; j < k * a.n_moves; j += kPickThreads / 64)
+        move_row(a.moves[j % a.n_moves], s_parent[j / a.n_moves], (int64_t)prompt * k + j / a.n_moves, lane, 64);
+}
+
+// Large states: a workgroup per row and state.
+__global__ __launch_bounds__(256) void beam_move_kernel(BeamArgs a) {
+    move_row(a.moves[blockIdx.y], a.parent[blockIdx.x], blockIdx.x, threadIdx.x, 256);
+}
+
+struct BeamPlan { int parts, share; };
+
+// Parts of a row: enough workgroups for the chip (four of them fit a compute unit), tiles of their own, few enough for a wavefront
+// to join, whose lists (448 entries) fit LDS.
+static BeamPlan plan_beams(int64_t rows, int vocab, int k) {
+    const int tiles = (vocab + kBeamTile - 1) / kBeamTile;
+    const int64_t want = std::max<int64_t>(1, 2048 / rows);
+    const int parts = (int)std::min<int64_t>({want, tiles, 64, std::max(1, 448 / k)});
+    const int per = (tiles + parts - 1) / parts;
+    return BeamPlan{(tiles + per - 1) / per, per * kBeamTile};
 }
 
 static int check_beams(int n_prompts, int beams_in, int vocab, int beams_out) {
@@ -149,7 +374,8 @@ extern "C" int ivf_beam_workspace(int32_t n_prompts, int32_t beams_in, int32_t v
     if (rc) return rc;
     if (!bytes) return fail(IVF_EINVAL, "bytes is NULL");
     const size_t rows = (size_t)n_prompts * beams_in;
-    *bytes = rows * beams_out * 8 + rows * 8;
+    const BeamPlan p = plan_beams((int64_t)rows, vocab, beams_out);
+    *bytes = rows * p.parts * ((size_t)beams_out * 8 + 8);
     return IVF_OK;
 }
 
@@ -166,24 +392,35 @@ extern "C" int ivf_beam_step(const void* logits, int64_t row_stride, int dtype, 
     if (((uintptr_t)logits & (dtype == IVF_F32 ? 3u : 1u)) != 0) return fail(IVF_EINVAL, "logits must be aligned to their elements");
     if (n_states < 0 || (n_states > 0 && !states)) return fail(IVF_EINVAL, "states is NULL or n_states negative");
     if (n_states > IVF_MAX_BEAM_STATES) return fail(IVF_ELIMIT, "%d states: at most %d", n_states, IVF_MAX_BEAM_STATES);
-    BeamMoves moves{};
+    BeamArgs a{};
+    int64_t moved = 0;
     for (int i = 0; i < n_states; ++i) {
         const ivf_beam_state& s = states[i];
         if (!s.from || !s.to) return fail(IVF_EINVAL, "state %d: NULL", i);
         if (s.row_bytes < 1 || s.from_stride < 0 || s.to_stride < s.row_bytes) return fail(IVF_EINVAL, "state %d: row_bytes or strides", i);
-        moves.m[i] = BeamMove{(const uint8_t*)s.from, (uint8_t*)s.to, s.row_bytes, s.from_stride, s.to_stride};
+        a.moves[i] = BeamMove{(const uint8_t*)s.from, (uint8_t*)s.to, s.row_bytes, s.from_stride, s.to_stride};
+        moved += s.row_bytes * beams_out;
     }
     if (!workspace || ((uintptr_t)workspace & 15u) != 0) return fail(IVF_EINVAL, "workspace must be given and 16-byte aligned");
     if (workspace_bytes < need) return fail(IVF_EINVAL, "this call needs %zu bytes of workspace (got %zu)", need, workspace_bytes);
-    const int rows = n_prompts * beams_in;
-    BeamArgs a{logits, row_stride, scores_in, done_in, scores_out, parent, token, done_out, (unsigned long long*)workspace,
-               (float*)((unsigned long long*)workspace + (size_t)rows * beams_out), n_prompts, beams_in, vocab, beams_out, eos};
+    const int64_t rows = (int64_t)n_prompts * beams_in;
+    const BeamPlan p = plan_beams(rows, vocab, beams_out);
+    a.logits = logits; a.row_stride = row_stride; a.scores_in = scores_in; a.done_in = done_in; a.scores_out = scores_out;
+    a.parent = parent; a.token = token; a.done_out = done_out;
+    a.keys = (unsigned long long*)workspace;
+    a.sums = (float2*)(a.keys + rows * p.parts * beams_out);
+    a.prompts = n_prompts; a.beams = beams_in; a.vocab = vocab; a.k = beams_out; a.eos = eos; a.parts = p.parts; a.share = p.share;
+    // states above 64 KB a prompt are moved by workgroups of their own
+    const bool apart = moved > 65536;
+    a.n_moves = apart ? 0 : n_states;
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == IVF_F32) hipLaunchKernelGGL(beam_rows_kernel<float>, dim3(rows), dim3(256), 0, s, a);
-    else if (dtype == IVF_F16) hipLaunchKernelGGL(beam_rows_kernel<_Float16>, dim3(rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(beam_rows_kernel<__bf16>, dim3(rows), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(beam_pick_kernel, dim3(n_prompts), dim3(64), 0, s, a);
-    if (n_states > 0) hipLaunchKernelGGL(beam_move_kernel, dim3(n_prompts * beams_out, n_states), dim3(256), 0, s, moves, parent);
+    const dim3 grid((unsigned)(rows * p.parts)), block(kBeamThreads);
+    if (dtype == IVF_F32) hipLaunchKernelGGL(beam_part_kernel<float>, grid, block, 0, s, a);
+    else if (dtype == IVF_F16) hipLaunchKernelGGL(beam_part_kernel<_Float16>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(beam_part_kernel<__bf16>, grid, block, 0, s, a);
+    const size_t lds = (size_t)kPickThreads / 64 * p.parts * beams_out * 8;
+    hipLaunchKernelGGL(beam_pick_kernel, dim3(n_prompts), dim3(kPickThreads), lds, s, a);
+    if (apart) hipLaunchKernelGGL(beam_move_kernel, dim3(n_prompts * beams_out, n_states), dim3(256), 0, s, a);
     HIP_TRY(hipGetLastError());
     return IVF_OK;
 }
