@@ -86,6 +86,8 @@ template <> struct Half<__bf16> {
     }
 };
 
+__device__ __forceinline__ float other_half(float x) { return __uint_as_float(xor_lane_u32<32>(__float_as_uint(x))); }
+
 // A maximum rises only when the new one is 2^kSlack above it: until then weights of up to 2^kSlack are summed, which
 // costs no precision, and the sums need not be scaled for every small rise.
 constexpr float kSlack = 8.f;
@@ -168,6 +170,20 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
     const int32_t* entries = (const int32_t*)(s_mem + S::kStageBytes + wave * S::kEntrySlots * 256);
     const uint32_t entries_at = __builtin_amdgcn_readfirstlane(lds_address(entries));
 
+    // where a lane's pieces of a tile lie: of keys row l % 32, chunk 2 s + l / 32; of values see `value`.  Tiles of 32 keys, and
+    // steps of 16, follow at multiples of the pitch
+    int key_place[kKeySteps], value_place[2][kBlocks];
+#pragma unroll
+    for (int s = 0; s < kKeySteps; ++s)
+        key_place[s] = (lane & 31) * S::kPitch + (((2 * s + half) ^ place_swap<S::kChunks>(lane & 31)) << 4);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            const int r = 8 * u + 4 * half + (lane & 15) / 4, chunk = 4 * b + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+            value_place[u][b] = (S::kKeys + r) * S::kPitch + ((chunk ^ place_swap<S::kChunks>(r)) << 4) + (lane & 1) * 8;
+        }
+
     for (int tile = tile0; tile * S::kRows < rows; tile += a.n_tile) {
         // rows of the workgroup and of this lane
         const int row_first = tile * S::kRows, row_last = min(rows, row_first + S::kRows) - 1;
@@ -192,12 +208,6 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         }
         most = __builtin_amdgcn_readfirstlane(most);
         least = __builtin_amdgcn_readfirstlane(least);
-        // over the wavefront's rows: up to where all see all, and from where on
-        int all_to = mine ? lim : 0x7FFFFFFF, all_from = mine ? low : 0;
-        for (int w = 16; w >= 1; w >>= 1) { all_to = min(all_to, __shfl_xor(all_to, w)); all_from = max(all_from, __shfl_xor(all_from, w)); }
-        all_to = __builtin_amdgcn_readfirstlane(all_to);
-        all_from = __builtin_amdgcn_readfirstlane(all_from);
-
         // the tiles of keys that some row sees: [0, n_sink) and [n_low, n_end) of the grid that begins at kb
         const int end = min(ke, most + 1);
         const int n_end = end > kb ? (end - kb + S::kKeys - 1) / S::kKeys : 0;
@@ -209,10 +219,17 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         const int seen = n_sink + n_end - n_low;
         const int per = (seen + a.n_split - 1) / a.n_split;
         const int v0 = min(seen, split * per), v1 = min(seen, v0 + per);
-        // of these the wavefront takes n
-        const int n = NARROW ? (v1 - v0 - wave + S::kWaves - 1) / S::kWaves : v1 - v0;
+        // those whose keys all rows see come first: [inner0, inner1) of them
+        const int all_low = a.window > 0 ? max(0, most - a.window + 1) : 0;
+        const int inner_to = (min(least, ke - 1) + 1 - kb) / S::kKeys, inner_from = all_low > kb ? (all_low - kb + S::kKeys - 1) / S::kKeys : 0;
+        const int inner0 = min(v1, max(v0, n_sink + max(inner_from - n_low, 0)));
+        const int inner1 = min(v1, max(inner0, n_sink + inner_to - n_low)), inner = inner1 - inner0;
+        // of these tiles the wavefront takes n, the first n_full of them inner ones
+        auto mine_of = [&](int count) { return NARROW ? (count - wave + S::kWaves - 1) / S::kWaves : count; };
+        const int n = mine_of(v1 - v0), n_full = mine_of(inner);
         auto first_key = [&](int i) {
-            const int v = v0 + (NARROW ? wave + i * S::kWaves : i);
+            const int c = NARROW ? wave + i * S::kWaves : i;
+            const int v = c < inner ? inner0 + c : v0 + c - inner < inner0 ? v0 + c - inner : v0 + c;
             return kb + (v < n_sink ? v : v - n_sink + n_low) * S::kKeys;
         };
 
@@ -258,25 +275,21 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         f16v_t o[kBlocks] = {};
         float m = -INFINITY, l = 0.f;
 
-        // one tile: scores, weights, products
+        // one tile: scores, weights, products; `full`: every row sees all its keys
         auto compute = [&](int i, auto full_tag) __attribute__((always_inline)) {
-            constexpr bool FULL = decltype(full_tag)::value;
+            constexpr bool full = decltype(full_tag)::value;
             const int j0 = first_key(i);
-            const unsigned char* ks = stage + (i % S::kStages) * S::kTileBytes;
-            const unsigned char* vs = ks + S::kKeys * S::kPitch;
+            const unsigned char* tile_at = stage + (i % S::kStages) * S::kTileBytes;
             f16v_t x[kKeyTiles];
 #pragma unroll
-            for (int t = 0; t < kKeyTiles; ++t) {
-                x[t] = f16v_t{};
-                const int r = t * 32 + (lane & 31);
+            for (int t = 0; t < kKeyTiles; ++t) x[t] = f16v_t{};
 #pragma unroll
-                for (int s = 0; s < kKeySteps; ++s) {
-                    const s8_t k = *(const s8_t*)(ks + r * S::kPitch + (((2 * s + half) ^ place_swap<S::kChunks>(r)) << 4));
-                    x[t] = H::mfma(k, q[s], x[t]);
-                }
-            }
+            for (int s = 0; s < kKeySteps; ++s)
+#pragma unroll
+                for (int t = 0; t < kKeyTiles; ++t)
+                    x[t] = H::mfma(*(const s8_t*)(tile_at + key_place[s] + t * 32 * S::kPitch), q[s], x[t]);
             auto sees = [&](int j) { return j <= lim && (j >= low || j < a.sinks); };
-            if (!FULL) {
+            if (!full) {
 #pragma unroll
                 for (int t = 0; t < kKeyTiles; ++t)
 #pragma unroll
@@ -290,7 +303,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             for (int t = 0; t < kKeyTiles; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) top = fmaxf(top, x[t][r]);
-            top = fmaxf(top, xor_lane<32>(top)) * a.scale_log2;
+            top = fmaxf(top, other_half(top)) * a.scale_log2;
             if (__ballot(top > m + kSlack) != 0) {
                 const float m2 = fmaxf(m, top);
                 const float f = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m2);
@@ -301,64 +314,76 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             }
             const float minus = (m == -INFINITY ? 0.f : -m) + H::kLift;
             s8_t p[kKeyTiles * 2];
-            float sum = 0.f;
+            float sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < kKeyTiles; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], a.scale_log2, minus));
-                    sum += w;
+                    sum[r & 1] += w;
                     p[t * 2 + r / 8][r % 8] = __builtin_bit_cast(short, (T)w);
                 }
-            l += sum;
+            l += sum[0] + sum[1];
             // V transposed, the keys in the order of p: lane l, element l % 32 of a block of 32, keys 16 s + 4 (l / 32) .. + 4 and
             // eight behind those
             auto value = [&](int s, int b) __attribute__((always_inline)) {
                 s8_t v;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int r = 16 * s + 8 * u + 4 * half + (lane & 15) / 4;
-                    const int chunk = 4 * b + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
-                    const unsigned char* at = vs + r * S::kPitch + ((chunk ^ place_swap<S::kChunks>(r)) << 4) + (lane & 1) * 8;
-                    const s4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)at);
+                    const s4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(tile_at + value_place[u][b] + s * 16 * S::kPitch));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[u * 4 + e] = y[e];
                 }
                 return v;
             };
-            if (!FULL) {
-                // a value that is not finite times the weight zero of a row that does not see it would be NaN
-                uint32_t odd = 0;
+            bool odd = false;
+            if (!full) {
+                uint32_t any = 0;
+#pragma unroll 1
                 for (int s = 0; s < kKeyTiles * 2; ++s)
 #pragma unroll
                     for (int b = 0; b < kBlocks; ++b) {
                         const s8_t v = value(s, b);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) odd |= ((uint16_t)v[e] & H::kExponent) == H::kExponent;
+                        for (int e = 0; e < 8; ++e) any |= ((uint16_t)v[e] & H::kExponent) == H::kExponent;
                     }
-                if (__ballot(odd != 0) != 0) {
-                    // key by key: the product for all rows, kept by those that see the key
-                    for (int jj = 0; jj < S::kKeys; ++jj) {
-                        const int s = jj >> 4, e = (jj & 3) + 4 * (jj >> 3 & 1);
-                        const bool here = (jj >> 2 & 1) == half, keep = sees(j0 + jj);
-                        s8_t w{};
+                odd = __ballot(any != 0) != 0;
+            }
+            if (__builtin_expect(odd, 0)) {
+                // A value that is not finite, times the weight zero of a row that does not see it, would be NaN: such values are left
+                // out of the product, and counted instead for the rows that see them, the three kinds in one number
 #pragma unroll
-                        for (int u = 0; u < kKeyTiles * 2; ++u)
+                for (int s = 0; s < kKeyTiles * 2; ++s)
 #pragma unroll
-                            for (int i8 = 0; i8 < 8; ++i8)
-                                if (u == s && i8 == e && here) w[i8] = p[u][i8];
+                    for (int b = 0; b < kBlocks; ++b) {
+                        s8_t v = value(s, b);
 #pragma unroll
-                        for (int b = 0; b < kBlocks; ++b) {
-                            s8_t v = value(s, b);
+                        for (int e = 0; e < 8; ++e) v[e] = ((uint16_t)v[e] & H::kExponent) == H::kExponent ? (short)0 : v[e];
+                        o[b] = H::mfma(v, p[s], o[b]);
+                    }
+                auto of = [](float x) { return __builtin_bit_cast(short, (T)x); };
 #pragma unroll
-                            for (int i8 = 0; i8 < 8; ++i8) v[i8] = i8 == e && here ? v[i8] : (short)0;
-                            const f16v_t y = H::mfma(v, w, f16v_t{});
+                for (int b = 0; b < kBlocks; ++b) {
+                    f16v_t y{};
+#pragma unroll 1
+                    for (int s = 0; s < kKeyTiles * 2; ++s) {
+                        s8_t v = value(s, b), w;
 #pragma unroll
-                            for (int r = 0; r < 16; ++r) o[b][r] += keep ? y[r] : 0.f;
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t bits = (uint16_t)v[e];
+                            v[e] = (bits & H::kExponent) != H::kExponent ? (short)0
+                                   : (bits & 0x7FFFu) != H::kExponent ? of(16384.f) : bits >> 15 ? of(128.f) : of(1.f);
+                            w[e] = sees(j0 + 16 * s + (e & 3) + 8 * (e >> 2) + 4 * half) ? of(1.f) : (short)0;
                         }
+                        y = H::mfma(v, w, y);
                     }
-                    return;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int n = (int)y[r];           // NaN, -inf and +inf by digits of 128
+                        if (n != 0) o[b][r] += n >= 16384 || ((n & 127) && n >= 128) ? NAN : n >= 128 ? -INFINITY : INFINITY;
+                    }
                 }
+                return;
             }
 #pragma unroll
             for (int s = 0; s < kKeyTiles * 2; ++s)
@@ -375,20 +400,25 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             for (int i = 0; i < S::kAhead; ++i)
                 if (i < n) fetch_tile(i);
         }
-        for (int i = 0; i < n; ++i) {
+        auto arrive = [&](int i) __attribute__((always_inline)) {
             // tile i has arrived: kAhead - 1 younger ones may be on their way
             if (S::kAhead > 1 && i + S::kAhead <= n) wait_loads<(S::kAhead - 1) * 2 * S::kLoads>();
             else wait_loads<0>();
             if (!NARROW) barrier();      // for every wavefront, and the tile before has been read
             if (i + S::kAhead < n) fetch_tile(i + S::kAhead);
             if (i + 2 * S::kAhead < n) fetch_entries(i + 2 * S::kAhead);
-            const int j0 = first_key(i);
-            if (!NARROW && row - (lane & 31) >= rows) continue;            // no rows: this wavefront only fetches
-            const bool full = j0 + S::kKeys - 1 <= all_to && (j0 >= all_from || j0 + S::kKeys <= a.sinks);
-            if (full) compute(i, std::true_type{});
-            else compute(i, std::false_type{});
+        };
+        const bool idle = !NARROW && row - (lane & 31) >= rows;            // no rows: this wavefront only fetches
+        // two loops, so that what the tiles at the edges need takes no registers from the others
+        for (int i = 0; i < n_full; ++i) {
+            arrive(i);
+            if (!idle) compute(i, std::true_type{});
         }
-        l += xor_lane<32>(l);
+        for (int i = n_full; i < n; ++i) {
+            arrive(i);
+            if (!idle) compute(i, std::false_type{});
+        }
+        l += other_half(l);
 
         // what is left to do with the sums
         const bool last = a.mode == kConcat && a.n_split == 1;             // they are complete
