@@ -124,6 +124,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
     using S = Shape<D, NARROW>;
     using H = Half<T>;
     constexpr int kKeySteps = D / 16, kBlocks = D / 32, kKeyTiles = S::kKeys / 32;
+    constexpr int kBatch = D == 96 ? 3 : 4;
     const int lane = lane_id(), wave = wave_id(), half = lane >> 5;
     const int G = a.group;
     int at = blockIdx.x;
@@ -239,6 +240,9 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             const T* src = (const T*)a.q.data + tok * a.q.token_stride + head * a.q.head_stride + half * 8;
 #pragma unroll
             for (int s = 0; s < kKeySteps; ++s) q[s] = mine ? *(const s8_t*)(src + s * 16) : s8_t{};
+            // waited for here: the loops below count what is on its way themselves
+#pragma unroll
+            for (int s = 0; s < kKeySteps; ++s) asm volatile("" : "+v"(q[s]));
         }
 
         // fetching: lane l keeps the entry of row l of the wavefront's part of a tile
@@ -283,11 +287,25 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             f16v_t x[kKeyTiles];
 #pragma unroll
             for (int t = 0; t < kKeyTiles; ++t) x[t] = f16v_t{};
+            // reads of LDS run kBatch products ahead: one wavefront's products then hide their latency
+            constexpr int kScores = kKeySteps * kKeyTiles;
+            auto key = [&](int c) __attribute__((always_inline)) {
+                return *(const s8_t*)(tile_at + key_place[c / kKeyTiles] + c % kKeyTiles * 32 * S::kPitch);
+            };
+            s8_t k[2][kBatch];
 #pragma unroll
-            for (int s = 0; s < kKeySteps; ++s)
+            for (int u = 0; u < kBatch; ++u) k[0][u] = key(u);
 #pragma unroll
-                for (int t = 0; t < kKeyTiles; ++t)
-                    x[t] = H::mfma(*(const s8_t*)(tile_at + key_place[s] + t * 32 * S::kPitch), q[s], x[t]);
+            for (int c = 0; c < kScores; c += kBatch) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+                    if (c + kBatch + u < kScores) k[(c / kBatch + 1) & 1][u] = key(c + kBatch + u);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+                    x[(c + u) % kKeyTiles] = H::mfma(k[c / kBatch & 1][u], q[(c + u) / kKeyTiles], x[(c + u) % kKeyTiles]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
             auto sees = [&](int j) { return j <= lim && (j >= low || j < a.sinks); };
             if (!full) {
 #pragma unroll
@@ -385,10 +403,20 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
                 }
                 return;
             }
+            constexpr int kSums = kKeyTiles * 2 * kBlocks;
+            s8_t v[2][kBatch];
 #pragma unroll
-            for (int s = 0; s < kKeyTiles * 2; ++s)
+            for (int u = 0; u < kBatch; ++u) v[0][u] = value(u / kBlocks, u % kBlocks);
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) o[b] = H::mfma(value(s, b), p[s], o[b]);
+            for (int c = 0; c < kSums; c += kBatch) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+                    if (c + kBatch + u < kSums) v[(c / kBatch + 1) & 1][u] = value((c + kBatch + u) / kBlocks, (c + kBatch + u) % kBlocks);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) o[(c + u) % kBlocks] = H::mfma(v[c / kBatch & 1][u], p[(c + u) / kBlocks], o[(c + u) % kBlocks]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         };
 
         if (n > 0) {
