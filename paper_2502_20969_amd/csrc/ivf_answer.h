@@ -11,7 +11,7 @@ struct CacheView {
     void* k;
     void* v;
     int64_t page_stride, token_stride, head_stride, n_slots;
-    int page_shift;
+    int page_shift, page_bytes, token_bytes;
 };
 
 struct StepView {
@@ -20,6 +20,7 @@ struct StepView {
     int64_t own_cap, prefix_cap;         // keys that a row of the tables can name, at most INT32_MAX
     int64_t own_entries, prefix_entries; // entries that lie in the cache
     int n_seq, n_tokens, n_groups, shift, prefix_shift;
+    int own_last, prefix_last;           // the last of them
 };
 
 // Checks the caller's structures and fills the views; a status, with the error text set.

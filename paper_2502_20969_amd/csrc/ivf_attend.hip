@@ -86,6 +86,18 @@ template <> struct Half<__bf16> {
     }
 };
 
+// the value of lane (l & ~3) + u
+__device__ __forceinline__ int64_t quad_lane(int64_t x, int u) {
+    const int lo = (int)x, hi = (int)(x >> 32);
+    int a, b;
+    switch (u) {
+    case 0: a = __builtin_amdgcn_mov_dpp(lo, 0x00, 0xF, 0xF, true); b = __builtin_amdgcn_mov_dpp(hi, 0x00, 0xF, 0xF, true); break;
+    case 1: a = __builtin_amdgcn_mov_dpp(lo, 0x55, 0xF, 0xF, true); b = __builtin_amdgcn_mov_dpp(hi, 0x55, 0xF, 0xF, true); break;
+    case 2: a = __builtin_amdgcn_mov_dpp(lo, 0xAA, 0xF, 0xF, true); b = __builtin_amdgcn_mov_dpp(hi, 0xAA, 0xF, 0xF, true); break;
+    default: a = __builtin_amdgcn_mov_dpp(lo, 0xFF, 0xF, 0xF, true); b = __builtin_amdgcn_mov_dpp(hi, 0xFF, 0xF, 0xF, true); break;
+    }
+    return (int64_t)((uint64_t)(uint32_t)b << 32 | (uint32_t)a);
+}
 __device__ __forceinline__ float other_half(float x) { return __uint_as_float(xor_lane_u32<32>(__float_as_uint(x))); }
 
 // A maximum rises only when the new one is 2^kSlack above it: until then weights of up to 2^kSlack are summed, which
@@ -107,10 +119,11 @@ struct Shape {
     static constexpr int kWaveRows = NARROW ? kKeys : kKeys / kWaves;      // rows of a tile that a wavefront fetches
     static constexpr int kLoads = kWaveRows / kRowsPerLoad;                // loads for its keys, and as many for its values
     static constexpr int kRows = NARROW ? 32 : 32 * kWaves;                // rows of a workgroup
+    static constexpr int kSets = (kLoads + 3) / 4;
     static constexpr int kEntrySlots = kAhead > 1 ? 8 : 4;                 // tiles whose table entries are kept
     static constexpr int kStageBytes = (NARROW ? kWaves : 1) * kStages * kTileBytes;
-    static constexpr int kLds = kStageBytes + kWaves * kEntrySlots * 256;
-    static_assert(2 * kAhead < kEntrySlots, "an entry's place is not taken before its tile is fetched");
+    static constexpr int kLds = kStageBytes + kWaves * kEntrySlots * kSets * 256;
+    static_assert(2 * kAhead + 1 < kEntrySlots + kAhead && kAhead + 1 <= kEntrySlots, "an entry's place is not taken before its tile is fetched");
     static_assert(!NARROW || (size_t)kWaves * 32 * D * 4 + kWaves * 32 * 8 <= (size_t)kStageBytes, "room to join the wavefronts");
 };
 
@@ -168,7 +181,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
 
     unsigned char* stage = s_mem + (NARROW ? wave * S::kStages * S::kTileBytes : 0);
     const uint32_t stage_at = __builtin_amdgcn_readfirstlane(lds_address(stage));
-    const int32_t* entries = (const int32_t*)(s_mem + S::kStageBytes + wave * S::kEntrySlots * 256);
+    const int32_t* entries = (const int32_t*)(s_mem + S::kStageBytes + wave * S::kEntrySlots * S::kSets * 256);
     const uint32_t entries_at = __builtin_amdgcn_readfirstlane(lds_address(entries));
 
     // where a lane's pieces of a tile lie: of keys row l % 32, chunk 2 s + l / 32; of values see `value`.  Tiles of 32 keys, and
@@ -184,6 +197,17 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             const int r = 8 * u + 4 * half + (lane & 15) / 4, chunk = 4 * b + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
             value_place[u][b] = (S::kKeys + r) * S::kPitch + ((chunk ^ place_swap<S::kChunks>(r)) << 4) + (lane & 1) * 8;
         }
+
+    // the chunk of a row that a lane fetches, in bytes: sixteen rows repeat
+    constexpr int kChunkKinds = std::min(S::kLoads, 16 / S::kRowsPerLoad);
+    int chunk_bytes[kChunkKinds];
+#pragma unroll
+    for (int u = 0; u < kChunkKinds; ++u) {
+        const int r = (NARROW ? 0 : wave * S::kWaveRows) + u * S::kRowsPerLoad + lane / S::kChunks;
+        chunk_bytes[u] = ((lane % S::kChunks) ^ place_swap<S::kChunks>(r)) * 16;
+    }
+    const char* kbase = (const char*)a.cache.k + kvh * a.cache.head_stride * 2;
+    const char* vbase = (const char*)a.cache.v + kvh * a.cache.head_stride * 2;
 
     for (int tile = tile0; tile * S::kRows < rows; tile += a.n_tile) {
         // rows of the workgroup and of this lane
@@ -245,33 +269,42 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             for (int s = 0; s < kKeySteps; ++s) asm volatile("" : "+v"(q[s]));
         }
 
-        // fetching: lane l keeps the entry of row l of the wavefront's part of a tile
-        const int fetch_row = lane & (S::kWaveRows - 1);
-        auto key_of = [&](int i) { return min(first_key(i) + (NARROW ? 0 : wave * S::kWaveRows) + fetch_row, ke - 1); };
-        auto fetch_entries = [&](int i) {
-            const int key = key_of(i);
-            const int32_t* e = key < plen ? ptab + (key >> a.step.prefix_shift) : otab + ((key - plen) >> a.step.shift);
-            fetch4(e, entries_at + (i & (S::kEntrySlots - 1)) * 256);
+        // Fetching.  Load u of a wavefront brings rows u * kRowsPerLoad + lane / kChunks; four loads make a set, and lane l keeps
+        // the place of the row that load l % 4 of the set brings to its group, so that a load finds its lanes' places in the
+        // lanes' own quads
+        auto row_of = [&](int set) {
+            return (NARROW ? 0 : wave * S::kWaveRows) + (S::kLoads < 4 ? lane & (S::kLoads - 1) : set * 4 + (lane & 3)) * S::kRowsPerLoad + lane / S::kChunks;
         };
-        auto fetch_tile = [&](int i) {
-            const int key = key_of(i);
-            const bool pre = key < plen;
-            const int shift = pre ? a.step.prefix_shift : a.step.shift;
-            const int64_t limit = (pre ? a.step.prefix_entries : a.step.own_entries) - 1;
-            int64_t e = max(entries[(i & (S::kEntrySlots - 1)) * 64 + lane], 0);
-            if (e > limit) e = limit;
-            const int64_t slot = (e << shift) + ((pre ? key : key - plen) & ((1 << shift) - 1));
-            const int64_t off = (slot_offset(a.cache, slot) + kvh * a.cache.head_stride) * 2;
-            const int lo = (int)off, hi = (int)(off >> 32);
+        auto key_of = [&](int i, int set) { return min(first_key(i) + row_of(set), ke - 1); };
+        auto fetch_entries = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int set = 0; set < S::kSets; ++set) {
+                const int key = key_of(i, set);
+                const int32_t* e = key < plen ? ptab + (key >> a.step.prefix_shift) : otab + ((key - plen) >> a.step.shift);
+                fetch4(e, entries_at + ((i & (S::kEntrySlots - 1)) * S::kSets + set) * 256);
+            }
+        };
+        int64_t place[S::kSets];           // bytes from the cache's begin, of the next tile to be fetched
+        auto locate = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int set = 0; set < S::kSets; ++set) {
+                const int key = key_of(i, set);
+                const bool pre = key < plen;
+                const int shift = pre ? a.step.prefix_shift : a.step.shift, up = a.cache.page_shift - shift;
+                const int e = min(max(entries[((i & (S::kEntrySlots - 1)) * S::kSets + set) * 64 + lane], 0), pre ? a.step.prefix_last : a.step.own_last);
+                const int j = pre ? key : key - plen;
+                const int in_page = (e & ((1 << up) - 1)) << shift | (j & ((1 << shift) - 1));
+                place[set] = (int64_t)(e >> up) * a.cache.page_bytes + (int64_t)in_page * a.cache.token_bytes;
+            }
+        };
+        auto fetch_tile = [&](int i) __attribute__((always_inline)) {
             const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes + (NARROW ? 0 : wave * S::kWaveRows * S::kPitch);
 #pragma unroll
             for (int u = 0; u < S::kLoads; ++u) {
-                const int r = u * S::kRowsPerLoad + lane / S::kChunks;
-                const int chunk = (lane % S::kChunks) ^ place_swap<S::kChunks>((NARROW ? 0 : wave * S::kWaveRows) + r);
-                const int64_t o = (int64_t)((uint64_t)(uint32_t)__shfl(hi, r) << 32 | (uint32_t)__shfl(lo, r)) + chunk * 16;
-                if (D % 64 == 0 || chunk < D / 8) {
-                    fetch16((const char*)a.cache.k + o, to + u * 1024);
-                    fetch16((const char*)a.cache.v + o, to + S::kKeys * S::kPitch + u * 1024);
+                const int64_t at = quad_lane(place[u / 4], u & 3) + chunk_bytes[u % kChunkKinds];
+                if (D % 64 == 0 || chunk_bytes[u % kChunkKinds] < D * 2) {
+                    fetch16(kbase + at, to + u * 1024);
+                    fetch16(vbase + at, to + S::kKeys * S::kPitch + u * 1024);
                 }
             }
         };
@@ -336,10 +369,13 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
 #pragma unroll
             for (int t = 0; t < kKeyTiles; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], a.scale_log2, minus));
-                    sum[r & 1] += w;
-                    p[t * 2 + r / 8][r % 8] = __builtin_bit_cast(short, (T)w);
+                for (int r = 0; r < 16; r += 2) {
+                    const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], a.scale_log2, minus));
+                    const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r + 1], a.scale_log2, minus));
+                    sum[0] += w0;
+                    sum[1] += w1;
+                    p[t * 2 + r / 8][r % 8] = __builtin_bit_cast(short, (T)w0);
+                    p[t * 2 + r / 8][r % 8 + 1] = __builtin_bit_cast(short, (T)w1);
                 }
             l += sum[0] + sum[1];
             // V transposed, the keys in the order of p: lane l, element l % 32 of a block of 32, keys 16 s + 4 (l / 32) .. + 4 and
@@ -421,12 +457,13 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
 
         if (n > 0) {
 #pragma unroll
-            for (int i = 0; i < 2 * S::kAhead; ++i)
+            for (int i = 0; i <= 2 * S::kAhead; ++i)
                 if (i < n) fetch_entries(i);
             wait_loads<0>();
 #pragma unroll
             for (int i = 0; i < S::kAhead; ++i)
-                if (i < n) fetch_tile(i);
+                if (i < n) { locate(i); fetch_tile(i); }
+            if (S::kAhead < n) locate(S::kAhead);
         }
         auto arrive = [&](int i) __attribute__((always_inline)) {
             // tile i has arrived: kAhead - 1 younger ones may be on their way
@@ -434,17 +471,19 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             else wait_loads<0>();
             if (!NARROW) barrier();      // for every wavefront, and the tile before has been read
             if (i + S::kAhead < n) fetch_tile(i + S::kAhead);
-            if (i + 2 * S::kAhead < n) fetch_entries(i + 2 * S::kAhead);
+            if (i + 2 * S::kAhead + 1 < n) fetch_entries(i + 2 * S::kAhead + 1);
         };
         const bool idle = !NARROW && row - (lane & 31) >= rows;            // no rows: this wavefront only fetches
         // two loops, so that what the tiles at the edges need takes no registers from the others
         for (int i = 0; i < n_full; ++i) {
             arrive(i);
             if (!idle) compute(i, std::true_type{});
+            if (i + S::kAhead + 1 < n) locate(i + S::kAhead + 1);
         }
         for (int i = n_full; i < n; ++i) {
             arrive(i);
             if (!idle) compute(i, std::false_type{});
+            if (i + S::kAhead + 1 < n) locate(i + S::kAhead + 1);
         }
         l += other_half(l);
 

@@ -28,6 +28,8 @@ int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv
     if (cache->n_pages < 1 || cache->n_heads < 1 || cache->d < 1) return fail(IVF_EINVAL, "cache n_pages, n_heads and d must be at least 1");
     if (cache->page_stride % 8 != 0 || cache->token_stride % 8 != 0 || cache->head_stride % 8 != 0)
         return fail(IVF_EINVAL, "cache strides must be multiples of 8 elements");
+    for (int64_t stride : {cache->page_stride, cache->token_stride, cache->head_stride})
+        if (stride > (1 << 30) - 1 || stride < -(1 << 30)) return fail(IVF_ELIMIT, "cache stride of %lld elements", (long long)stride);
     const int cs = shift_of(cache->page);
     if (cs < 0) return fail(IVF_EINVAL, "cache page (%d) must be a power of two", cache->page);
     if (cache->n_pages > INT64_MAX >> 32) return fail(IVF_ELIMIT, "cache of %lld pages", (long long)cache->n_pages);
@@ -49,10 +51,12 @@ int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv
     const int64_t slots = cache->n_pages << cs;
     // a prefix and the own keys together stay below 2^31
     auto cap = [](int64_t stride, int shift) { return std::min<int64_t>(stride, (int64_t)1 << 30 >> shift) << shift; };
-    *cv = CacheView{cache->k, cache->v, cache->page_stride, cache->token_stride, cache->head_stride, slots, cs};
+    *cv = CacheView{cache->k, cache->v, cache->page_stride, cache->token_stride, cache->head_stride, slots, cs,
+                    (int)(cache->page_stride * 2), (int)(cache->token_stride * 2)};
     *sv = StepView{step->q_off, step->len, step->table, step->group_off, step->prefix_len, step->prefix_table,
                    step->table_stride, step->prefix_stride, cap(step->table_stride, ss), cap(step->prefix_stride, ps),
-                   slots >> ss, slots >> ps, step->n_seq, step->n_tokens, step->n_groups, ss, ps};
+                   slots >> ss, slots >> ps, step->n_seq, step->n_tokens, step->n_groups, ss, ps,
+                   (int)std::min<int64_t>((slots >> ss) - 1, INT32_MAX), (int)std::min<int64_t>((slots >> ps) - 1, INT32_MAX)};
     return IVF_OK;
 }
 
