@@ -37,10 +37,13 @@ struct AttendArgs {
     float* part_o;
     float2* part_ml;
     int parts;                       // 0: one pass over all keys, no partial sums
-    // this pass
-    int mode, part0, n_part;         // its range of partial sums
-    int n_split, n_tile;             // workgroups that share a row's keys; workgroups that share a unit's rows
-    int rows_lo, rows_hi;            // units with more than rows_lo and at most rows_hi rows
+    // one launch makes one pass or two, which read different keys
+    struct Pass {
+        int mode, part0, n_part;     // its range of partial sums
+        int n_split, n_tile;         // workgroups that share a row's keys; workgroups that share a unit's rows
+        int rows_lo, rows_hi;        // units with more than rows_lo and at most rows_hi rows
+    } pass[2];
+    int first_blocks;                // workgroups of the first pass
 };
 
 // ---- memory to LDS ------------------------------------------------------------------------------
@@ -111,8 +114,8 @@ struct Shape {
     static constexpr int kChunks = D <= 64 ? 8 : D <= 128 ? 16 : 32;       // 16-byte chunks of a staged row
     static constexpr int kPitch = kChunks * 16;
     static constexpr int kKeys = NARROW || D > 128 ? 32 : 64;              // keys of a tile
-    static constexpr int kWaves = NARROW && D > 128 ? 2 : 4;
-    static constexpr int kStages = NARROW && D <= 64 ? 4 : 2;
+    static constexpr int kWaves = NARROW ? 2 : 4;
+    static constexpr int kStages = 2;
     static constexpr int kAhead = kStages - 1;                             // tiles on their way while one is worked on
     static constexpr int kTileBytes = kKeys * kPitch * 2;                  // keys, then values
     static constexpr int kRowsPerLoad = 64 / kChunks;
@@ -141,42 +144,44 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
     const int lane = lane_id(), wave = wave_id(), half = lane >> 5;
     const int G = a.group;
     int at = blockIdx.x;
+    const bool second = at >= a.first_blocks;
+    const AttendArgs::Pass& pass = a.pass[second];
+    if (second) at -= a.first_blocks;
     const int kvh = at % a.hkv; at /= a.hkv;
-    const int tile0 = a.n_tile - 1 - at % a.n_tile; at /= a.n_tile;        // the rows that see most first
-    const int split = at % a.n_split, unit = at / a.n_split;
+    const int tile0 = pass.n_tile - 1 - at % pass.n_tile; at /= pass.n_tile;       // the rows that see most first
+    const int split = at % pass.n_split, unit = at / pass.n_split;
 
-    // the unit: its tokens and keys
-    const bool by_group = a.mode == kPrefix;
-    int s0 = unit, s1 = unit + 1, g;
+    // The unit: its tokens and keys.  Keys, positions, window and sinks are counted from the begin of what the pass reads: own
+    // keys alone do not wait for the prefix's length
+    const bool by_group = pass.mode == kPrefix;
+    int s0 = unit, s1 = unit + 1, g = -1;
     if (by_group) {
         g = unit;
         s0 = min(max(a.step.group_off[g], 0), a.step.n_seq);
         s1 = min(max(a.step.group_off[g + 1], s0), a.step.n_seq);
-    } else {
+    } else if (a.step.n_groups > 0) {
         g = group_of(a.step, unit);
     }
-    const int t0 = token_of(a.step, s0), t1 = token_of(a.step, s1);
+    const int t0 = token_of(a.step, s0), t1 = token_of(a.step, s1), own = by_group ? 0 : own_len(a.step, unit);
     const int rows = (t1 - t0) * G;
-    if (rows <= a.rows_lo || rows > a.rows_hi) return;
-    const int plen = prefix_of(a.step, g);
+    if (rows <= pass.rows_lo || rows > pass.rows_hi) return;
+    const int before = prefix_of(a.step, g);                               // keys of the prefix, which
+    const int plen = pass.mode == kOwn ? 0 : before;                          // this pass reads or not
     if (by_group && plen == 0) return;
-    const int own = by_group ? 0 : own_len(a.step, unit);
-    const int kb = a.mode == kOwn ? plen : 0, ke = plen + own;
+    const int sinks = pass.mode == kOwn ? (a.window > 0 ? a.sinks - before : 0) : a.sinks;
+    const int ke = plen + own;
     const int32_t* ptab = a.step.prefix_table + (int64_t)max(g, 0) * a.step.prefix_stride;
     const int32_t* otab = a.step.table + (int64_t)s0 * a.step.table_stride;
 
     // position of a token: where its sequence's keys end, less the tokens behind it
     auto position = [&](int t) {
-        int seq = unit;
-        if (by_group) {
-            int lo = s0, hi = s1;                   // the last sequence that begins at or before t
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (a.step.q_off[mid] <= t) lo = mid; else hi = mid;
-            }
-            seq = lo;
+        if (!by_group) return plen + own - (t1 - t);
+        int lo = s0, hi = s1;                       // the last sequence that begins at or before t
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (a.step.q_off[mid] <= t) lo = mid; else hi = mid;
         }
-        return plen + own_len(a.step, seq) - (token_of(a.step, seq + 1) - t);
+        return plen + own_len(a.step, lo) - (token_of(a.step, lo + 1) - t);
     };
 
     unsigned char* stage = s_mem + (NARROW ? wave * S::kStages * S::kTileBytes : 0);
@@ -209,14 +214,14 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
     const char* kbase = (const char*)a.cache.k + kvh * a.cache.head_stride * 2;
     const char* vbase = (const char*)a.cache.v + kvh * a.cache.head_stride * 2;
 
-    for (int tile = tile0; tile * S::kRows < rows; tile += a.n_tile) {
+    for (int tile = tile0; tile * S::kRows < rows; tile += pass.n_tile) {
         // rows of the workgroup and of this lane
         const int row_first = tile * S::kRows, row_last = min(rows, row_first + S::kRows) - 1;
         const int row = row_first + (NARROW ? 0 : wave * 32) + (lane & 31);
         const bool mine = row < rows;
         const int tok = t0 + (mine ? row : rows - 1) / G, head = kvh * G + (mine ? row : rows - 1) % G;
         const int pos = mine ? position(tok) : -1;
-        const int lim = min(pos, ke - 1);                                  // sees keys kb .. lim that are at or above low, or sinks
+        const int lim = min(pos, ke - 1);                                  // sees keys up to lim that are at or above low, or sinks
         const int low = a.window > 0 ? max(0, pos - a.window + 1) : 0;
         // over the workgroup's rows (positions rise inside a sequence; over a group, all rows are looked at)
         int most = -1, least = 0x7FFFFFFF;
@@ -233,20 +238,20 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         }
         most = __builtin_amdgcn_readfirstlane(most);
         least = __builtin_amdgcn_readfirstlane(least);
-        // the tiles of keys that some row sees: [0, n_sink) and [n_low, n_end) of the grid that begins at kb
+        // the tiles of keys that some row sees: [0, n_sink) and [n_low, n_end) of the grid
         const int end = min(ke, most + 1);
-        const int n_end = end > kb ? (end - kb + S::kKeys - 1) / S::kKeys : 0;
+        const int n_end = max(0, end + S::kKeys - 1) / S::kKeys;
         int n_low = 0, n_sink = 0;
         if (a.window > 0) {
-            n_low = min(n_end, max(0, max(0, least - a.window + 1) - kb) / S::kKeys);
-            n_sink = min(n_low, a.sinks > kb ? (min(a.sinks, end) - kb + S::kKeys - 1) / S::kKeys : 0);
+            n_low = min(n_end, max(0, least - a.window + 1) / S::kKeys);
+            n_sink = min(n_low, sinks > 0 ? (min(sinks, end) + S::kKeys - 1) / S::kKeys : 0);
         }
         const int seen = n_sink + n_end - n_low;
-        const int per = (seen + a.n_split - 1) / a.n_split;
+        const int per = (seen + pass.n_split - 1) / pass.n_split;
         const int v0 = min(seen, split * per), v1 = min(seen, v0 + per);
         // those whose keys all rows see come first: [inner0, inner1) of them
         const int all_low = a.window > 0 ? max(0, most - a.window + 1) : 0;
-        const int inner_to = (min(least, ke - 1) + 1 - kb) / S::kKeys, inner_from = all_low > kb ? (all_low - kb + S::kKeys - 1) / S::kKeys : 0;
+        const int inner_to = (min(least, ke - 1) + 1) / S::kKeys, inner_from = (all_low + S::kKeys - 1) / S::kKeys;
         const int inner0 = min(v1, max(v0, n_sink + max(inner_from - n_low, 0)));
         const int inner1 = min(v1, max(inner0, n_sink + inner_to - n_low)), inner = inner1 - inner0;
         // of these tiles the wavefront takes n, the first n_full of them inner ones
@@ -255,7 +260,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         auto first_key = [&](int i) {
             const int c = NARROW ? wave + i * S::kWaves : i;
             const int v = c < inner ? inner0 + c : v0 + c - inner < inner0 ? v0 + c - inner : v0 + c;
-            return kb + (v < n_sink ? v : v - n_sink + n_low) * S::kKeys;
+            return (v < n_sink ? v : v - n_sink + n_low) * S::kKeys;
         };
 
         // the rows of Q as the second operand: lane l, row l % 32, elements 16 s + 8 (l / 32) and on
@@ -339,7 +344,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
                     x[(c + u) % kKeyTiles] = H::mfma(k[c / kBatch & 1][u], q[(c + u) / kKeyTiles], x[(c + u) % kKeyTiles]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            auto sees = [&](int j) { return j <= lim && (j >= low || j < a.sinks); };
+            auto sees = [&](int j) { return j <= lim && (j >= low || j < sinks); };
             if (!full) {
 #pragma unroll
                 for (int t = 0; t < kKeyTiles; ++t)
@@ -488,16 +493,16 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         l += other_half(l);
 
         // what is left to do with the sums
-        const bool last = a.mode == kConcat && a.n_split == 1;             // they are complete
+        const bool last = pass.mode == kConcat && pass.n_split == 1;             // they are complete
         auto finish = [&](int t, int h, float mm, float ll) {              // by one lane per row
             if (a.lse && last) a.lse[(int64_t)t * a.hq + h] = ll > 0.f || ll != ll ? (mm + __builtin_amdgcn_logf(ll) - H::kLift) * 0.6931471805599453f : -INFINITY;
             if (a.parts == 0) return;
             float2* ml = a.part_ml + ((int64_t)t * a.hq + h) * a.parts;
-            ml[a.part0 + split] = make_float2(last ? NAN : mm, ll);
+            ml[pass.part0 + split] = make_float2(last ? NAN : mm, ll);
             if (split == 0) {
-                for (int i = a.n_split; i < a.n_part; ++i) ml[a.part0 + i] = make_float2(-INFINITY, 0.f);
-                if (a.mode == kOwn && plen == 0)                           // no prefix pass comes by here
-                    for (int i = 0; i < a.part0; ++i) ml[i] = make_float2(-INFINITY, 0.f);
+                for (int i = pass.n_split; i < pass.n_part; ++i) ml[pass.part0 + i] = make_float2(-INFINITY, 0.f);
+                if (pass.mode == kOwn && before == 0)                           // no prefix pass comes by here
+                    for (int i = 0; i < pass.part0; ++i) ml[i] = make_float2(-INFINITY, 0.f);
             }
         };
         if (!NARROW) {
@@ -505,7 +510,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
                 if (half == 0) finish(tok, head, m, l);
                 const float f = last ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f;
                 T* out = (T*)a.out.data + tok * a.out.token_stride + head * a.out.head_stride;
-                float* part = last ? nullptr : a.part_o + (((int64_t)tok * a.hq + head) * a.parts + a.part0 + split) * D;
+                float* part = last ? nullptr : a.part_o + (((int64_t)tok * a.hq + head) * a.parts + pass.part0 + split) * D;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -564,7 +569,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
                               __builtin_bit_cast(short, (T)(y.z * g1)), __builtin_bit_cast(short, (T)(y.w * g1))};
                     *(s4_t*)((T*)a.out.data + t * a.out.token_stride + h * a.out.head_stride + d) = z;
                 } else if (v1 > v0) {
-                    *(float4*)(a.part_o + (((int64_t)t * a.hq + h) * a.parts + a.part0 + split) * D + d) = y;
+                    *(float4*)(a.part_o + (((int64_t)t * a.hq + h) * a.parts + pass.part0 + split) * D + d) = y;
                 }
             }
             __syncthreads();
@@ -572,38 +577,64 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
     }
 }
 
-// Joins a row's partial sums: one wavefront per token and query head.
+// Joins a row's partial sums: one wavefront per token and query head.  Lane i weighs part i; then D / 4 lanes take a part's
+// elements, and several parts at a time are on their way.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-    constexpr int kPer = (D + 63) / 64;
+    constexpr int kLanes = D / 4, kAtOnce = kLanes <= 64 ? 64 / kLanes : 1;          // lanes of a part; parts of one load
+    constexpr int kUnroll = 4;
     const int64_t row = (int64_t)blockIdx.x * 4 + wave_id();
     const int lane = lane_id();
     if (row >= (int64_t)a.step.n_tokens * a.hq) return;
     const float2* ml = a.part_ml + row * a.parts;
-    float top = -INFINITY;
-    bool done = false;
-    for (int i = lane; i < a.parts; i += 64) { const float x = ml[i].x; done |= x != x; top = fmaxf(top, x); }
-    if (__ballot(done)) return;
-    for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-    float sum = 0.f, o[kPer] = {};
-    for (int i = 0; i < a.parts; ++i) {
-        const float2 p = ml[i];
-        if (p.x == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(p.x - top);
-        sum += p.y * f;
-        const float* src = a.part_o + (row * a.parts + i) * D;
+    const float* po = a.part_o + row * a.parts * D;
+    float m = -INFINITY, sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int group = min(lane / kLanes, kAtOnce - 1), d = lane % kLanes * 4;
+    for (int p0 = 0; p0 < a.parts; p0 += 64) {                                      // 64 parts at a time
+        const float2 p = p0 + lane < a.parts ? ml[p0 + lane] : make_float2(-INFINITY, 0.f);
+        if (__ballot(p.x != p.x)) return;                                          // complete already
+        float top = p.x;
+        for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+        const float m2 = fmaxf(m, top);
+        if (m2 == -INFINITY) continue;
+        const float keep = __builtin_amdgcn_exp2f(m - m2);
+        const float f = p.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(p.x - m2);
+        m = m2;
+        sum = sum * keep + group_sum<64>(p.y * f);
+        o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+        const int n = min(64, a.parts - p0);
+        for (int i0 = 0; i0 < n; i0 += kAtOnce * kUnroll) {
+            float4 y[kUnroll];
+            float w[kUnroll];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (e * 64 + lane < D) o[e] += src[e * 64 + lane] * f;
+            for (int u = 0; u < kUnroll; ++u) {
+                const int i = i0 + u * kAtOnce + group;
+                const float weight = __shfl(f, i & 63), at = __shfl(p.x, i & 63);      // by all lanes
+                const bool has = i < n && at > -INFINITY && lane < kLanes * kAtOnce;
+                y[u] = has ? *(const float4*)(po + (int64_t)(p0 + i) * D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                w[u] = has ? weight : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) { o.x += y[u].x * w[u]; o.y += y[u].y * w[u]; o.z += y[u].z * w[u]; o.w += y[u].w * w[u]; }
+        }
+    }
+    if (kAtOnce > 1) {
+        static_assert(kAtOnce <= 2 || kLanes == 16, "groups of lanes that swap");
+        if (kLanes == 32) { o.x += __shfl_xor(o.x, 32); o.y += __shfl_xor(o.y, 32); o.z += __shfl_xor(o.z, 32); o.w += __shfl_xor(o.w, 32); }
+        if (kLanes == 16)
+            for (int w = 32; w >= 16; w >>= 1) { o.x += __shfl_xor(o.x, w); o.y += __shfl_xor(o.y, w); o.z += __shfl_xor(o.z, w); o.w += __shfl_xor(o.w, w); }
+        if (kLanes == 24) { o.x += __shfl(o.x, (lane + 24) & 63); o.y += __shfl(o.y, (lane + 24) & 63); o.z += __shfl(o.z, (lane + 24) & 63); o.w += __shfl(o.w, (lane + 24) & 63); }
     }
     const int t = (int)(row / a.hq), h = (int)(row % a.hq);
-    T* out = (T*)a.out.data + t * a.out.token_stride + h * a.out.head_stride;
     const float f = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e)
-        if (e * 64 + lane < D) out[e * 64 + lane] = (T)(o[e] * f);
+    if (lane < kLanes) {
+        const s4_t y = {__builtin_bit_cast(short, (T)(o.x * f)), __builtin_bit_cast(short, (T)(o.y * f)), __builtin_bit_cast(short, (T)(o.z * f)),
+                        __builtin_bit_cast(short, (T)(o.w * f))};
+        *(s4_t*)((T*)a.out.data + t * a.out.token_stride + h * a.out.head_stride + d) = y;
+    }
     if (a.lse && lane == 0)
-        a.lse[row] = sum > 0.f || sum != sum ? (top + __builtin_amdgcn_logf(sum) - Half<T>::kLift) * 0.6931471805599453f : -INFINITY;
+        a.lse[row] = sum > 0.f || sum != sum ? (m + __builtin_amdgcn_logf(sum) - Half<T>::kLift) * 0.6931471805599453f : -INFINITY;
 }
 
 static int check_heads(const ivf_kv_cache* cache, int n_q_heads, int window, int sinks) {
@@ -644,11 +675,14 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
         const int64_t most = (keys + least - 1) / least;
         return (int)std::max<int64_t>(1, std::min<int64_t>({(want + units - 1) / units, most, 64}));
     };
+    // few rows: pieces of 512 keys and more for several workgroups a place on the chip (two fit a compute unit), smaller ones
+    // only while places are free
+    auto split_few = [&](int64_t units, int64_t keys) { return std::max(split(units, 4096, keys, 512), split(units, 512, keys, 128)); };
     p.tiles_narrow = 1;
     // (unknown: twice what sequences of equal lengths would need)
     const int64_t tile_rows = st->max_q > 0 || sv.n_seq == 1 ? most_q * group : std::min(rows, 2 * rows / sv.n_seq);
     p.tiles_wide = (int)std::max<int64_t>(1, (tile_rows + kWideRows - 1) / kWideRows);
-    if (p.narrow) p.split_narrow = split((int64_t)sv.n_seq * hkv, 4096, keys, 512);
+    if (p.narrow) p.split_narrow = split_few((int64_t)sv.n_seq * hkv, keys);
     if (p.wide) p.split_wide = split(hkv * ((rows + kWideRows - 1) / kWideRows + sv.n_seq - 1), 512, keys, 512);
     p.n_own = std::max(p.split_narrow, p.split_wide);
     if (p.shared) {
@@ -656,7 +690,8 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
         p.prefix_narrow = group_rows <= kNarrowRows;
         const int tile = p.prefix_narrow ? kNarrowRows : kWideRows;
         p.tiles_prefix = (int)std::max<int64_t>(1, (group_rows + tile - 1) / tile);
-        p.split_prefix = split((int64_t)sv.n_groups * hkv * p.tiles_prefix, p.prefix_narrow ? 2048 : 512, read_keys(pre), p.prefix_narrow ? 512 : 256);
+        const int64_t units = (int64_t)sv.n_groups * hkv * p.tiles_prefix;
+        p.split_prefix = p.prefix_narrow ? split_few(units, read_keys(pre)) : split(units, 512, read_keys(pre), 256);
         p.part_own = p.split_prefix;
     }
     p.parts = p.shared || p.n_own > 1 ? p.part_own + p.n_own : 0;
@@ -665,34 +700,39 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
 
 static size_t plan_bytes(const AttendPlan& p, int64_t rows, int d) { return (size_t)(rows * p.parts) * ((size_t)d * 4 + 8); }
 
+// One launch for one pass or two: units of the first and of the second.
 template <typename T, int D, bool NARROW>
-static hipError_t launch_pass(AttendArgs a, int64_t units, hipStream_t s) {
+static hipError_t launch_passes(AttendArgs a, int64_t units0, int64_t units1, hipStream_t s) {
     using S = Shape<D, NARROW>;
-    const int64_t grid = units * a.n_split * a.n_tile * a.hkv;
+    auto blocks = [&](int64_t units, const AttendArgs::Pass& p) { return units * p.n_split * p.n_tile * a.hkv; };
+    const int64_t first = blocks(units0, a.pass[0]), grid = first + blocks(units1, a.pass[1]);
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
     static const hipError_t allowed = hipFuncSetAttribute((const void*)attend_kernel<T, D, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
     if (allowed != hipSuccess) return allowed;
+    a.first_blocks = (int)first;
     hipLaunchKernelGGL((attend_kernel<T, D, NARROW>), dim3((unsigned)grid), dim3(S::kWaves * 64), S::kLds, s, a);
     return hipGetLastError();
 }
 
 template <typename T, int D>
 static hipError_t launch_attend(AttendArgs a, const AttendPlan& p, hipStream_t s) {
-    const int64_t rows = (int64_t)a.step.n_tokens * a.hq;
+    const int64_t rows = (int64_t)a.step.n_tokens * a.hq, units = a.step.n_seq, groups = p.shared ? a.step.n_groups : 0;
     hipError_t e;
     a.parts = p.parts;
-    if (p.shared) {
-        a.mode = kPrefix; a.part0 = 0; a.n_part = a.n_split = p.split_prefix; a.n_tile = p.tiles_prefix; a.rows_lo = 0; a.rows_hi = kAllRows;
-        if ((e = p.prefix_narrow ? launch_pass<T, D, true>(a, a.step.n_groups, s) : launch_pass<T, D, false>(a, a.step.n_groups, s))) return e;
+    const int mode = p.shared ? kOwn : kConcat;
+    // the prefix goes first, with those of the other keys' passes that the same kernel makes
+    const AttendArgs::Pass prefix = {kPrefix, 0, p.split_prefix, p.split_prefix, p.tiles_prefix, 0, kAllRows};
+    const AttendArgs::Pass wide = {mode, p.part_own, p.n_own, p.split_wide, p.tiles_wide, p.narrow ? kNarrowRows : 0, kAllRows};
+    const AttendArgs::Pass narrow = {mode, p.part_own, p.n_own, p.split_narrow, p.tiles_narrow, 0, p.wide ? kNarrowRows : kAllRows};
+    const int64_t groups_wide = p.prefix_narrow ? 0 : groups, groups_narrow = groups - groups_wide;
+    a.pass[0] = prefix;
+    if (groups_wide || p.wide) {
+        a.pass[1] = wide;
+        if ((e = launch_passes<T, D, false>(a, groups_wide, p.wide ? units : 0, s))) return e;
     }
-    a.mode = p.shared ? kOwn : kConcat; a.part0 = p.part_own; a.n_part = p.n_own;
-    if (p.wide) {
-        a.n_split = p.split_wide; a.n_tile = p.tiles_wide; a.rows_lo = p.narrow ? kNarrowRows : 0; a.rows_hi = kAllRows;
-        if ((e = launch_pass<T, D, false>(a, a.step.n_seq, s))) return e;
-    }
-    if (p.narrow) {
-        a.n_split = p.split_narrow; a.n_tile = p.tiles_narrow; a.rows_lo = 0; a.rows_hi = p.wide ? kNarrowRows : kAllRows;
-        if ((e = launch_pass<T, D, true>(a, a.step.n_seq, s))) return e;
+    if (groups_narrow || p.narrow) {
+        a.pass[1] = narrow;
+        if ((e = launch_passes<T, D, true>(a, groups_narrow, p.narrow ? units : 0, s))) return e;
     }
     if (p.parts > 0) {
         hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
