@@ -49,7 +49,7 @@ struct AttendArgs {
 // ---- memory to LDS ------------------------------------------------------------------------------
 // The loads are written as assembly so that the compiler, which cannot know which of them a read from LDS depends on,
 // does not wait for all of them; they have no register outputs, and are waited for by count.
-extern __shared__ __align__(16) unsigned char s_mem[];
+extern __shared__ __align__(1024) unsigned char s_mem[];
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
@@ -71,6 +71,7 @@ typedef float f16v_t __attribute__((ext_vector_type(16)));
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s4_t* lds_s4;
+typedef __attribute__((address_space(3))) const s8_t* lds_s8;
 
 template <typename T> struct Half;
 template <> struct Half<_Float16> {
@@ -189,19 +190,13 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
     const int32_t* entries = (const int32_t*)(s_mem + S::kStageBytes + wave * S::kEntrySlots * S::kSets * 256);
     const uint32_t entries_at = __builtin_amdgcn_readfirstlane(lds_address(entries));
 
-    // where a lane's pieces of a tile lie: of keys row l % 32, chunk 2 s + l / 32; of values see `value`.  Tiles of 32 keys, and
-    // steps of 16, follow at multiples of the pitch
-    int key_place[kKeySteps], value_place[2][kBlocks];
-#pragma unroll
-    for (int s = 0; s < kKeySteps; ++s)
-        key_place[s] = (lane & 31) * S::kPitch + (((2 * s + half) ^ place_swap<S::kChunks>(lane & 31)) << 4);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const int r = 8 * u + 4 * half + (lane & 15) / 4, chunk = 4 * b + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
-            value_place[u][b] = (S::kKeys + r) * S::kPitch + ((chunk ^ place_swap<S::kChunks>(r)) << 4) + (lane & 1) * 8;
-        }
+    // Where a lane's pieces of a tile lie: of keys row l % 32, chunk 2 s + l / 32; of values (see `value`) row 8 u + 4 (l / 32) +
+    // (l % 16) / 4, chunk 4 b + 2 (l / 16 % 2) + l % 4 / 2.  Rows begin at multiples of the pitch, so that s, b and u change single
+    // bits of the first place
+    const int key_place = (lane & 31) * S::kPitch + ((half ^ place_swap<S::kChunks>(lane & 31)) << 4);
+    const int value_row = 4 * half + (lane & 15) / 4;
+    const int value_place = (S::kKeys + value_row) * S::kPitch + (((2 * (lane >> 4 & 1) + (lane & 3) / 2) ^ place_swap<S::kChunks>(value_row)) << 4) + (lane & 1) * 8;
+    constexpr int kRowBit = S::kChunks == 8 ? 0 : 32;
 
     // the chunk of a row that a lane fetches, in bytes: sixteen rows repeat
     constexpr int kChunkKinds = std::min(S::kLoads, 16 / S::kRowsPerLoad);
@@ -211,6 +206,10 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         const int r = (NARROW ? 0 : wave * S::kWaveRows) + u * S::kRowsPerLoad + lane / S::kChunks;
         chunk_bytes[u] = ((lane % S::kChunks) ^ place_swap<S::kChunks>(r)) * 16;
     }
+    // in registers: a choice between two of the arguments would otherwise be a load, which waits for the tiles on their way
+    const int pre_shift = __builtin_amdgcn_readfirstlane(a.step.prefix_shift), own_shift = __builtin_amdgcn_readfirstlane(a.step.shift);
+    const int pre_last = __builtin_amdgcn_readfirstlane(a.step.prefix_last), own_last = __builtin_amdgcn_readfirstlane(a.step.own_last);
+    const int page_shift = a.cache.page_shift;
     const char* kbase = (const char*)a.cache.k + kvh * a.cache.head_stride * 2;
     const char* vbase = (const char*)a.cache.v + kvh * a.cache.head_stride * 2;
 
@@ -285,8 +284,8 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
 #pragma unroll
             for (int set = 0; set < S::kSets; ++set) {
                 const int key = key_of(i, set);
-                const int32_t* e = key < plen ? ptab + (key >> a.step.prefix_shift) : otab + ((key - plen) >> a.step.shift);
-                fetch4(e, entries_at + ((i & (S::kEntrySlots - 1)) * S::kSets + set) * 256);
+                const bool pre = key < plen;
+                fetch4((pre ? ptab : otab) + ((pre ? key : key - plen) >> (pre ? pre_shift : own_shift)), entries_at + ((i & (S::kEntrySlots - 1)) * S::kSets + set) * 256);
             }
         };
         int64_t place[S::kSets];           // bytes from the cache's begin, of the next tile to be fetched
@@ -295,8 +294,8 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             for (int set = 0; set < S::kSets; ++set) {
                 const int key = key_of(i, set);
                 const bool pre = key < plen;
-                const int shift = pre ? a.step.prefix_shift : a.step.shift, up = a.cache.page_shift - shift;
-                const int e = min(max(entries[((i & (S::kEntrySlots - 1)) * S::kSets + set) * 64 + lane], 0), pre ? a.step.prefix_last : a.step.own_last);
+                const int shift = pre ? pre_shift : own_shift, up = page_shift - shift;
+                const int e = min(max(entries[((i & (S::kEntrySlots - 1)) * S::kSets + set) * 64 + lane], 0), pre ? pre_last : own_last);
                 const int j = pre ? key : key - plen;
                 const int in_page = (e & ((1 << up) - 1)) << shift | (j & ((1 << shift) - 1));
                 place[set] = (int64_t)(e >> up) * a.cache.page_bytes + (int64_t)in_page * a.cache.token_bytes;
@@ -321,14 +320,15 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         auto compute = [&](int i, auto full_tag) __attribute__((always_inline)) {
             constexpr bool full = decltype(full_tag)::value;
             const int j0 = first_key(i);
-            const unsigned char* tile_at = stage + (i % S::kStages) * S::kTileBytes;
+            const uint32_t tile_at = stage_at + (i % S::kStages) * S::kTileBytes;
+            const uint32_t key_at = tile_at + key_place, value_at = tile_at + value_place;
             f16v_t x[kKeyTiles];
 #pragma unroll
             for (int t = 0; t < kKeyTiles; ++t) x[t] = f16v_t{};
             // reads of LDS run kBatch products ahead: one wavefront's products then hide their latency
             constexpr int kScores = kKeySteps * kKeyTiles;
             auto key = [&](int c) __attribute__((always_inline)) {
-                return *(const s8_t*)(tile_at + key_place[c / kKeyTiles] + c % kKeyTiles * 32 * S::kPitch);
+                return *(lds_s8)(uintptr_t)((key_at ^ (uint32_t)(c / kKeyTiles << 5)) + c % kKeyTiles * 32 * S::kPitch);
             };
             s8_t k[2][kBatch];
 #pragma unroll
@@ -389,7 +389,8 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
                 s8_t v;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const s4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(tile_at + value_place[u][b] + s * 16 * S::kPitch));
+                    const s4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s4)(uintptr_t)((value_at ^ (uint32_t)(b << 6 | u * kRowBit)) + (u * 8 + s * 16) * S::kPitch));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[u * 4 + e] = y[e];
                 }
@@ -478,7 +479,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             if (i + S::kAhead < n) fetch_tile(i + S::kAhead);
             if (i + 2 * S::kAhead + 1 < n) fetch_entries(i + 2 * S::kAhead + 1);
         };
-        const bool idle = !NARROW && row - (lane & 31) >= rows;            // no rows: this wavefront only fetches
+        const bool idle = !NARROW && row_first + wave * 32 >= rows;        // no rows: this wavefront only fetches
         // two loops, so that what the tiles at the edges need takes no registers from the others
         for (int i = 0; i < n_full; ++i) {
             arrive(i);
@@ -580,20 +581,17 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
 // Joins a row's partial sums: one wavefront per token and query head.  Lane i weighs part i; then D / 4 lanes take a part's
 // elements, and several parts at a time are on their way.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-    constexpr int kLanes = D / 4, kAtOnce = kLanes <= 64 ? 64 / kLanes : 1;          // lanes of a part; parts of one load
+__device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int lane) {
+    constexpr int kLanes = D / 4, kAtOnce = 64 / kLanes;             // lanes of a part; parts of one load
     constexpr int kUnroll = 4;
-    const int64_t row = (int64_t)blockIdx.x * 4 + wave_id();
-    const int lane = lane_id();
-    if (row >= (int64_t)a.step.n_tokens * a.hq) return;
     const float2* ml = a.part_ml + row * a.parts;
     const float* po = a.part_o + row * a.parts * D;
     float m = -INFINITY, sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     const int group = min(lane / kLanes, kAtOnce - 1), d = lane % kLanes * 4;
-    for (int p0 = 0; p0 < a.parts; p0 += 64) {                                      // 64 parts at a time
+    for (int p0 = 0; p0 < a.parts; p0 += 64) {                       // 64 parts at a time
         const float2 p = p0 + lane < a.parts ? ml[p0 + lane] : make_float2(-INFINITY, 0.f);
-        if (__ballot(p.x != p.x)) return;                                          // complete already
+        if (__ballot(p.x != p.x)) return;                            // complete already
         float top = p.x;
         for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
         const float m2 = fmaxf(m, top);
@@ -619,13 +617,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
             for (int u = 0; u < kUnroll; ++u) { o.x += y[u].x * w[u]; o.y += y[u].y * w[u]; o.z += y[u].z * w[u]; o.w += y[u].w * w[u]; }
         }
     }
-    if (kAtOnce > 1) {
-        static_assert(kAtOnce <= 2 || kLanes == 16, "groups of lanes that swap");
-        if (kLanes == 32) { o.x += __shfl_xor(o.x, 32); o.y += __shfl_xor(o.y, 32); o.z += __shfl_xor(o.z, 32); o.w += __shfl_xor(o.w, 32); }
-        if (kLanes == 16)
-            for (int w = 32; w >= 16; w >>= 1) { o.x += __shfl_xor(o.x, w); o.y += __shfl_xor(o.y, w); o.z += __shfl_xor(o.z, w); o.w += __shfl_xor(o.w, w); }
-        if (kLanes == 24) { o.x += __shfl(o.x, (lane + 24) & 63); o.y += __shfl(o.y, (lane + 24) & 63); o.z += __shfl(o.z, (lane + 24) & 63); o.w += __shfl(o.w, (lane + 24) & 63); }
-    }
+    // the groups of lanes
+    auto add = [&](int from) { o.x += __shfl(o.x, from); o.y += __shfl(o.y, from); o.z += __shfl(o.z, from); o.w += __shfl(o.w, from); };
+    if (kLanes == 16) { add(lane ^ 32); add(lane ^ 16); }
+    if (kLanes == 24) add((lane + 24) & 63);
+    if (kLanes == 32) add(lane ^ 32);
     const int t = (int)(row / a.hq), h = (int)(row % a.hq);
     const float f = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
     if (lane < kLanes) {
@@ -635,6 +631,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
     }
     if (a.lse && lane == 0)
         a.lse[row] = sum > 0.f || sum != sum ? (m + __builtin_amdgcn_logf(sum) - Half<T>::kLift) * 0.6931471805599453f : -INFINITY;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+    const int64_t rows = (int64_t)a.step.n_tokens * a.hq;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + wave_id(); row < rows; row += (int64_t)gridDim.x * 4) join_row<T, D>(a, row, lane_id());
 }
 
 static int check_heads(const ivf_kv_cache* cache, int n_q_heads, int window, int sinks) {
@@ -735,7 +737,7 @@ static hipError_t launch_attend(AttendArgs a, const AttendPlan& p, hipStream_t s
         if ((e = launch_passes<T, D, true>(a, groups_narrow, p.narrow ? units : 0, s))) return e;
     }
     if (p.parts > 0) {
-        hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 8192)), dim3(256), 0, s, a);
         return hipGetLastError();
     }
     return hipSuccess;
