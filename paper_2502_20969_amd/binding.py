@@ -515,14 +515,15 @@ def _i32(a, shape, what):
     return a.data_ptr()
 
 
-def _rows(a, n_tokens, n_heads, d, dtype, what):
-    """[n_tokens, heads, d] with the elements of a head side by side."""
-    if a.dtype is not dtype:
-        raise TypeError(f"{what} is {a.dtype}, the cache {dtype}")
-    shape, stride = a.shape, a.stride()
-    if not a.is_cuda or len(shape) != 3 or shape[0] != n_tokens or shape[2] != d or (n_heads is not None and shape[1] != n_heads):
-        raise ValueError(f"{what} has shape {tuple(shape)}, expected CUDA [{n_tokens}, {n_heads or 'heads'}, {d}]")
-    if stride[2] != 1 and d > 1:
+# The calls below run once per layer and step: their checks are kept short.
+def _rows(a, n_tokens, n_heads, cache, what):
+    """[n_tokens, n_heads, d] with the elements of a head side by side."""
+    if a.dtype is not cache.dtype:
+        raise TypeError(f"{what} is {a.dtype}, the cache {cache.dtype}")
+    stride = a.stride()
+    if a.shape != (n_tokens, n_heads, cache.d) or not a.is_cuda:
+        raise ValueError(f"{what} has shape {tuple(a.shape)}, expected CUDA [{n_tokens}, {n_heads}, {cache.d}]")
+    if stride[2] != 1:
         raise ValueError(f"the elements of a head of {what} must lie side by side")
     return RowsArg(a.data_ptr(), stride[0], stride[1])
 
@@ -537,8 +538,8 @@ class KvCache:
         if not (k.is_cuda and v.is_cuda) or k.dim() != 4 or k.stride(3) != 1:
             raise ValueError("expected CUDA tensors [n_pages, page, heads, d] with the elements of a head side by side")
         self.k, self.v, self.dtype = k, v, k.dtype
-        (pages, page, self.heads, self.d), st = k.shape, k.stride()
-        self.arg = KvCacheArg(k.data_ptr(), v.data_ptr(), pages, st[0], st[1], st[2], page, self.heads, self.d, _code(k.dtype))
+        (self.pages, self.page, self.heads, self.d), st = k.shape, k.stride()
+        self.arg = KvCacheArg(k.data_ptr(), v.data_ptr(), self.pages, st[0], st[1], st[2], self.page, self.heads, self.d, _code(k.dtype))
         self.ref = C.byref(self.arg)
 
 
@@ -563,6 +564,7 @@ class KvStep:
             a.n_groups, a.prefix_page, a.max_prefix = g, page if prefix_page is None else prefix_page, max_prefix
         self.arg, self.n_tokens = a, n_tokens
         self._keep = (q_off, lens, table, group_off, prefix_lens, prefix_table)
+        self._need = {}            # bytes of workspace by what they depend on
         self.ref = C.byref(a)
 
 
@@ -575,28 +577,38 @@ def _workspace(n, stream):
     return w
 
 
+_raw_stream = None
+
+
 def _on(stream):
-    return (_torch().cuda.current_stream() if stream is None else stream).cuda_stream
+    """The stream's handle; None: torch's current one."""
+    global _raw_stream
+    if stream is not None:
+        return stream.cuda_stream
+    t = _torch()
+    if _raw_stream is None:        # the handle alone, where this torch gives it, spares a Stream object per call
+        _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda device: t.cuda.current_stream(device).cuda_stream)
+    return _raw_stream(t.cuda.current_device())
 
 
 def ivf_kv_append(step, cache, k, v, rotary=None, positions=None, q=None, q_out=None, interleaved=False, stream=None):
     """Appends the new tokens' k and v [tokens, heads, d] to the cache; with rotary [positions, rot] float32 (cosines,
     then sines) keys and q [tokens, query heads, d] are rotated.  Returns q_out (default: a new tensor)."""
-    n, d, t = step.n_tokens, cache.d, _torch()
-    kr, vr = _rows(k, n, cache.heads, d, cache.dtype, "k"), _rows(v, n, cache.heads, d, cache.dtype, "v")
+    n = step.n_tokens
+    kr, vr = _rows(k, n, cache.heads, cache, "k"), _rows(v, n, cache.heads, cache, "v")
     qr = qo = rp = pp = None
     hq = n_pos = rot = 0
     if q is not None:
         if q_out is None:
-            q_out = t.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
             if stream is not None:
                 q_out.record_stream(stream)
         hq = q.shape[1]
-        qr, qo = _rows(q, n, hq, d, cache.dtype, "q"), _rows(q_out, n, hq, d, cache.dtype, "q_out")
+        qr, qo = _rows(q, n, hq, cache, "q"), _rows(q_out, n, hq, cache, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
     if rotary is not None:
-        if rotary.dtype is not t.float32 or not rotary.is_cuda or not rotary.is_contiguous() or rotary.dim() != 2:
+        if rotary.dtype is not _torch().float32 or not rotary.is_cuda or not rotary.is_contiguous() or rotary.dim() != 2:
             raise ValueError("rotary must be a contiguous float32 CUDA tensor [positions, rot]")
         n_pos, rot = rotary.shape
         rp = rotary.data_ptr()
@@ -612,24 +624,26 @@ def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0
     """Attention of the new tokens q [tokens, query heads, d] over the cache; returns out (default: a new tensor).
     lse: float32 [tokens, query heads] or None.  scale: default d ** -0.5.  workspace: a uint8 CUDA tensor of
     at least ivf_attend_workspace() bytes, default one for this call."""
-    n, d, t = step.n_tokens, cache.d, _torch()
+    n = step.n_tokens
     if out is None:
-        out = t.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
         if stream is not None:
             out.record_stream(stream)
     hq = q.shape[1]
-    qr, qo = _rows(q, n, hq, d, cache.dtype, "q"), _rows(out, n, hq, d, cache.dtype, "out")
-    lp = None
+    qr, qo = _rows(q, n, hq, cache, "q"), _rows(out, n, hq, cache, "out")
+    lp = wp = None
+    wn = 0
     if lse is not None:
-        if lse.dtype is not t.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape != (n, hq):
+        if lse.dtype is not _torch().float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape != (n, hq):
             raise ValueError("lse must be a contiguous float32 CUDA tensor [tokens, query heads]")
         lp = lse.data_ptr()
     if workspace is None:
-        need = ivf_attend_workspace(step, cache, hq, window, sinks)
-        if need:
-            workspace = _workspace(need, stream)
-    wp, wn = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    status = load().ivf_attend(step.ref, cache.ref, qr, hq, qo, lp, d ** -0.5 if scale is None else scale, window, sinks, wp, wn,
+        wn = ivf_attend_workspace(step, cache, hq, window, sinks)
+        if wn:
+            workspace = _workspace(wn, stream)
+    if workspace is not None:
+        wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    status = load().ivf_attend(step.ref, cache.ref, qr, hq, qo, lp, cache.d ** -0.5 if scale is None else scale, window, sinks, wp, wn,
                                _on(stream))
     if status != 0:
         _check(status)
@@ -638,20 +652,34 @@ def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0
 
 def ivf_attend_workspace(step, cache, n_q_heads, window=0, sinks=0):
     """Bytes of workspace of ivf_attend with these arguments."""
-    n = C.c_size_t(0)
-    status = load().ivf_attend_workspace(step.ref, cache.ref, n_q_heads, window, sinks, C.byref(n))
-    if status != 0:
-        _check(status)
-    return n.value
+    key = (cache.heads, cache.d, cache.page, cache.pages, n_q_heads, window, sinks)
+    need = step._need.get(key)
+    if need is None:
+        n = C.c_size_t(0)
+        _check(load().ivf_attend_workspace(step.ref, cache.ref, n_q_heads, window, sinks, C.byref(n)))
+        need = step._need[key] = n.value
+    return need
 
 
 def ivf_beam_workspace(n_prompts, beams_in, vocab, beams_out):
     """Bytes of workspace of ivf_beam_step with these sizes."""
     n = C.c_size_t(0)
-    status = load().ivf_beam_workspace(n_prompts, beams_in, vocab, beams_out, C.byref(n))
-    if status != 0:
-        _check(status)
+    _check(load().ivf_beam_workspace(n_prompts, beams_in, vocab, beams_out, C.byref(n)))
     return n.value
+
+
+def _state(src, dst, rows_in, rows_out):
+    """A state and its destination: rows of the same contiguous elements, evenly spaced."""
+    if src.dtype is not dst.dtype or not (src.is_cuda and dst.is_cuda):
+        raise ValueError("a state and its destination must be CUDA tensors of the same type")
+    if src.shape[0] != rows_in or dst.shape[0] != rows_out or src.shape[1:] != dst.shape[1:]:
+        raise ValueError("a state has a row per beam, before and after")
+    for x in (src, dst):
+        if not x.is_contiguous() and not x[0].is_contiguous():
+            raise ValueError("the rows of a state must be contiguous")
+    size = src.element_size()
+    row = src.numel() // rows_in * size
+    return BeamStateArg(src.data_ptr(), dst.data_ptr(), row, src.stride(0) * size if rows_in > 1 else row, dst.stride(0) * size if rows_out > 1 else row)
 
 
 def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), workspace=None, stream=None):
@@ -663,11 +691,11 @@ def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), 
     if logits.dim() != 3 or not logits.is_cuda or logits.stride(2) != 1:
         raise ValueError("logits must be a CUDA tensor [prompts, beams, vocab] with contiguous rows")
     p, b, vocab = logits.shape
-    stride = logits.stride(1) if b > 1 else logits.stride(0)
-    if p > 1 and logits.stride(0) != b * stride:
+    by_prompt, stride, _ = logits.stride()
+    if b == 1:
+        stride = by_prompt if p > 1 else vocab
+    elif p > 1 and by_prompt != b * stride:
         raise ValueError("the rows of logits must be evenly spaced")
-    if p * b == 1:
-        stride = vocab
     if scores.dtype is not t.float32 or not scores.is_cuda or not scores.is_contiguous() or scores.shape != (p, b):
         raise ValueError("scores must be a contiguous float32 CUDA tensor [prompts, beams]")
     dp = None
@@ -676,25 +704,22 @@ def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), 
             raise ValueError("done must be a contiguous bool or uint8 CUDA tensor [prompts, beams]")
         dp = done.data_ptr()
     n = b if beams_out is None else beams_out
-    args = (BeamStateArg * max(1, len(states)))()
-    for i, (src, dst) in enumerate(states):
-        if src.dtype is not dst.dtype or not (src.is_cuda and dst.is_cuda):
-            raise ValueError("a state and its destination must be CUDA tensors of the same type")
-        if src.shape[0] != p * b or dst.shape[0] != p * n or src.shape[1:] != dst.shape[1:] or not (src[0].is_contiguous() and dst[0].is_contiguous()):
-            raise ValueError("a state has a contiguous row per beam, before and after")
-        e, size = src[0].numel(), src.element_size()
-        args[i] = BeamStateArg(src.data_ptr(), dst.data_ptr(), e * size, src.stride(0) * size, (dst.stride(0) if p * n > 1 else e) * size)
+    args = (BeamStateArg * len(states))(*[_state(src, dst, p * b, p * n) for src, dst in states]) if states else None
     need = ivf_beam_workspace(p, b, vocab, n)
-    score, parent = t.empty(p, n, dtype=t.float32, device="cuda"), t.empty(p, n, dtype=t.int32, device="cuda")
-    token, out = t.empty(p, n, dtype=t.int32, device="cuda"), t.empty(p, n, dtype=t.bool, device="cuda")
+    # the scores, parents and tokens are one allocation
+    out = t.empty((3, p, n), dtype=t.int32, device="cuda")
+    score, parent, token = out.unbind(0)
+    score = score.view(t.float32)
+    fin = t.empty((p, n), dtype=t.bool, device="cuda")
     if workspace is None:
         workspace = _workspace(need, stream)
     if stream is not None:
-        for x in (score, parent, token, out):
-            x.record_stream(stream)
+        out.record_stream(stream)
+        fin.record_stream(stream)
+    at = out.data_ptr()
     status = load().ivf_beam_step(logits.data_ptr(), stride, _code(logits.dtype), p, b, vocab, scores.data_ptr(), dp, eos, n,
-                                  score.data_ptr(), parent.data_ptr(), token.data_ptr(), out.data_ptr(), args, len(states),
+                                  at, at + 4 * p * n, at + 8 * p * n, fin.data_ptr(), args, len(states),
                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _on(stream))
     if status != 0:
         _check(status)
-    return score, parent, token, out
+    return score, parent, token, fin
