@@ -22,16 +22,17 @@ struct BeamArgs {
     int32_t *parent, *token;
     uint8_t* done_out;
     unsigned long long* keys;     // [rows][parts][k] best logits, best first, packed with their tokens; 0 = none
-    float2* sums;                 // [rows][parts] maximum, and sum of exp(x - maximum)
+    float2* sums;                 // [rows][parts] R, and sum of exp(x - R); R +inf: number of infinite logits
     int prompts, beams, vocab, k, eos, parts, share;     // share: tokens of a part
     BeamMove moves[IVF_MAX_BEAM_STATES];
     int n_moves;
 };
 
 constexpr int kBeamThreads = 256;
-constexpr int kBeamElems = 32;                           // logits of a thread's part of a tile
-constexpr int kBeamTile = kBeamThreads * kBeamElems;
-constexpr int kBeamPool = 512;                           // candidates ranked at once
+constexpr int kBeamElems = 32;                           // logits of a lane's part of a tile
+constexpr int kBeamTile = 64 * kBeamElems;                // of a wavefront
+constexpr int kBeamPool = 256;                           // candidates ranked at once
+constexpr float kBeamSlack = 40.f;                       // terms of up to exp(40) are summed before the reference rises
 constexpr float kLog2e = 1.4426950408889634f;
 
 // A logit and its token as one word: larger is better, equal logits by lower token.  No continuation: 0.
@@ -46,29 +47,41 @@ __device__ __forceinline__ float logit_of(unsigned long long key) {
     return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
+// The largest value of a wavefront, in every lane, by moves between registers
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) {
+    x = max(x, xor_lane_u32<1>(x));
+    x = max(x, xor_lane_u32<2>(x));
+    x = max(x, xor_lane_u32<4>(x));
+    x = max(x, xor_lane_u32<8>(x));
+    x = max(x, xor_lane_u32<16>(x));
+    return max(x, xor_lane_u32<32>(x));
+}
 __device__ __forceinline__ float wave_max(float x) {
-    for (int w = 32; w >= 1; w >>= 1) x = fmaxf(x, __shfl_xor(x, w));
-    return x;
+    const uint32_t u = __float_as_uint(x), m = wave_max_u32(u & 0x80000000u ? ~u : u | 0x80000000u);
+    return __uint_as_float(m & 0x80000000u ? m ^ 0x80000000u : ~m);
 }
 __device__ __forceinline__ unsigned long long wave_max(unsigned long long x) {
-    for (int w = 32; w >= 1; w >>= 1) x = max(x, (unsigned long long)__shfl_xor((long long)x, w));
-    return x;
+    const uint32_t hi = (uint32_t)(x >> 32), top = wave_max_u32(hi);
+    return (unsigned long long)top << 32 | wave_max_u32(hi == top ? (uint32_t)x : 0u);
 }
 
 // 16 bytes of logits from any element
 template <typename T> struct Logits;
 template <> struct Logits<float> {
     static constexpr int kPer = 4;
+    static constexpr uint32_t kNone = 0xFF800000u;         // -inf
     static __device__ __forceinline__ float get(const uint4& v, int e) { return __uint_as_float((&v.x)[e]); }
 };
 template <> struct Logits<_Float16> {
     static constexpr int kPer = 8;
+    static constexpr uint32_t kNone = 0xFC00FC00u;
     static __device__ __forceinline__ float get(const uint4& v, int e) {
         return (float)__builtin_bit_cast(_Float16, (uint16_t)((&v.x)[e / 2] >> (16 * (e & 1))));
     }
 };
 template <> struct Logits<__bf16> {
     static constexpr int kPer = 8;
+    static constexpr uint32_t kNone = 0xFF80FF80u;
     static __device__ __forceinline__ float get(const uint4& v, int e) {
         const uint32_t w = (&v.x)[e / 2];
         return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
@@ -76,11 +89,11 @@ template <> struct Logits<__bf16> {
 };
 typedef u4_t u4_half_t __attribute__((aligned(2)));
 
-// The k best words of pool[0 .. n) to best[0 .. k), best first, by counting; best past n is 0.  All threads call it.
-__device__ __forceinline__ void rank_pool(const unsigned long long* pool, int n, unsigned long long* best, int k) {
-    for (int i = threadIdx.x; i < k; i += kBeamThreads)
-        if (i >= n) best[i] = 0;
-    for (int i = threadIdx.x; i < n; i += kBeamThreads) {
+// The k best words of pool[0 .. n) to best[0 .. k), best first, by counting, by the 64 lanes of a wavefront (threads =
+// 64) or all of a workgroup; best past n is 0.
+__device__ __forceinline__ void rank_pool(const unsigned long long* pool, int n, unsigned long long* best, int k, int first, int threads) {
+    for (int i = n + first; i < k; i += threads) best[i] = 0;
+    for (int i = first; i < n; i += threads) {
         const unsigned long long mine = pool[i];
         int rank = 0;
         for (int j = 0; j < n; ++j) rank += pool[j] > mine;
@@ -88,168 +101,158 @@ __device__ __forceinline__ void rank_pool(const unsigned long long* pool, int n,
     }
 }
 
-// Bound by reading the logits once: two tiles of 16-byte loads are on their way at a time (the one behind is requested
-// before one is worked on).  A thread keeps its own maximum and sum.  What may belong to the k best is rare: in the
-// first tile what reaches a value that k of the threads' maxima reach, later what is better than the k-th best so far;
-// it goes to a pool in LDS and is ranked by counting.
+// The same for the lists of a workgroup's wavefronts, in which 0 marks no entry: those go last.
+__device__ __forceinline__ void rank_parts(const unsigned long long* pool, int n, unsigned long long* best, int k) {
+    for (int i = threadIdx.x; i < n; i += kBeamThreads) {
+        const unsigned long long mine = pool[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += pool[j] > mine || (pool[j] == mine && j < i);
+        if (rank < k) best[rank] = mine;
+    }
+}
+
+// Sums of exp(x - R) of two sets, (R, sum), as one
+__device__ __forceinline__ float2 join_sums(float2 x, float2 y) {
+    const float2 hi = x.x >= y.x ? x : y, lo = x.x >= y.x ? y : x;
+    if (lo.x == hi.x) return make_float2(hi.x, hi.y + lo.y);
+    if (lo.x == -INFINITY || hi.x == INFINITY) return hi;
+    return make_float2(hi.x, hi.y + lo.y * __builtin_amdgcn_exp2f((lo.x - hi.x) * kLog2e));
+}
+
+// Bound by reading the logits once.  Wavefronts work for themselves: each takes every fourth tile of 32 logits a lane, the
+// next one requested before one is worked on, and sums exp(x - R) with an R that hardly ever has to rise.  What may belong to the k best is rare: in the first tile what
+// reaches a value that k of the lanes' maxima reach, later what is better than the k-th best so far; it goes to a pool
+// in LDS and is ranked by counting.
 template <typename T>
 __global__ __launch_bounds__(kBeamThreads) void beam_part_kernel(BeamArgs a) {
-    constexpr int kPer = Logits<T>::kPer, kLoads = kBeamElems / kPer;
-    __shared__ unsigned long long s_pool[kBeamPool + kBeamThreads];
-    __shared__ unsigned long long s_best[IVF_MAX_BEAMS];
-    __shared__ float s_edge[4];
-    __shared__ float2 s_sum[4];
-    __shared__ int s_count;
-    const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x, k = a.k;
+    constexpr int kPer = Logits<T>::kPer, kLoads = kBeamElems / kPer, kWaves = kBeamThreads / 64;
+    __shared__ unsigned long long s_pool[kWaves][kBeamPool];
+    __shared__ unsigned long long s_best[kWaves][IVF_MAX_BEAMS];
+    __shared__ float2 s_sum[kWaves];
+    const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts, lane = lane_id(), wave = wave_id(), k = a.k;
     if (a.done_in && a.done_in[row]) return;               // its only continuation needs no logits
     const int begin = part * a.share, end = min(a.vocab, begin + a.share);
     const T* x = (const T*)a.logits + row * a.row_stride;
     const int tiles = (end - begin + kBeamTile - 1) / kBeamTile;
+    unsigned long long *pool = s_pool[wave], *best = s_best[wave];
     auto request = [&](int tile, uint4 (&raw)[kLoads]) __attribute__((always_inline)) {
-        const int t0 = begin + tile * kBeamTile + tid * kPer;
+        const int t0 = begin + tile * kBeamTile + lane * kPer;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int t = t0 + i * kBeamThreads * kPer;
+            const int t = t0 + i * 64 * kPer;
             if (t + kPer <= end) {
                 const u4_t v = *(const u4_half_t*)(x + t);
                 raw[i] = make_uint4(v.x, v.y, v.z, v.w);
-            } else {                                       // the last few, one by one; none is taken for -inf below
-                uint32_t w[4] = {0, 0, 0, 0};
+            } else {                                       // the last few, one by one, with -inf behind them
+                uint32_t w[4];
+                for (int e = 0; e < 4; ++e) w[e] = Logits<T>::kNone;
                 for (int e = 0; e < kPer; ++e) {
                     if (t + e >= end) break;
                     if (kPer == 4) w[e] = __float_as_uint((float)x[t + e]);
-                    else w[e / 2] |= (uint32_t)((const uint16_t*)x)[t + e] << (16 * (e & 1));
+                    else if (e & 1) w[e / 2] = (w[e / 2] & 0xFFFFu) | (uint32_t)((const uint16_t*)x)[t + e] << 16;
+                    else w[e / 2] = (w[e / 2] & 0xFFFF0000u) | ((const uint16_t*)x)[t + e];
                 }
                 raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
     };
-    float m = -INFINITY, sum = 0.f;
+    float R = -INFINITY, sum = 0.f;                        // sum of exp(x - R); R +inf: number of infinite logits
     unsigned long long least = 0;                          // the k-th best so far; 0: fewer
     int have = 0;
     uint4 next[kLoads];
-    if (tiles > 0) request(0, next);
-    for (int tile = 0; tile < tiles; ++tile) {
+    if (wave < tiles) request(wave, next);
+    for (int tile = wave; tile < tiles; tile += kWaves) {
         uint4 raw[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) raw[i] = next[i];
-        if (tile + 1 < tiles) request(tile + 1, next);
-        const int t0 = begin + tile * kBeamTile + tid * kPer;
-        auto token = [&](int i, int e) { return t0 + i * kBeamThreads * kPer + e; };
-        auto value = [&](int i, int e) __attribute__((always_inline)) {      // -inf where there is none, and for NaN
-            const float v = fmaxf(Logits<T>::get(raw[i], e), -INFINITY);
-            return token(i, e) < end ? v : -INFINITY;
-        };
-        float top = -INFINITY;
+        if (tile + kWaves < tiles) request(tile + kWaves, next);
+        const int t0 = begin + tile * kBeamTile + lane * kPer;
+        auto token = [&](int i, int e) { return t0 + i * 64 * kPer + e; };
+        auto value = [&](int i, int e) __attribute__((always_inline)) { return Logits<T>::get(raw[i], e); };
+        float top = -INFINITY;                             // NaN counts for nothing
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
 #pragma unroll
             for (int e = 0; e < kPer; ++e) top = fmaxf(top, value(i, e));
-        if (top > -INFINITY) {
-            const float m2 = fmaxf(m, top);
-            if (m2 == INFINITY) {                          // infinite logits share the probability
-                if (m < INFINITY) sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-                    for (int e = 0; e < kPer; ++e) sum += value(i, e) == INFINITY ? 1.f : 0.f;
-            } else {
-                float add = 0.f;
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-                    for (int e = 0; e < kPer; ++e) add += __builtin_amdgcn_exp2f((value(i, e) - m2) * kLog2e);
-                sum = sum * __builtin_amdgcn_exp2f((m - m2) * kLog2e) + add;
-            }
-            m = m2;
+        // the sum, relative to a logit that no other is far above
+        if (__ballot(top > R + kBeamSlack)) {              // -inf at first
+            const float r2 = wave_max(fmaxf(top, R));
+            sum = R == -INFINITY || r2 == INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f((R - r2) * kLog2e);
+            R = r2;
         }
-        // what has to be reached: above `least`, or in the first tile at least `edge`, which k values reach if so many threads
-        // have any
-        float edge = -INFINITY;
-        if (tile == 0) {
-            float left = top;
-            // wavefronts whose threads all have a first load take part, in equal shares
-            const int waves = max(1, min(4, (end - begin) / (64 * kPer)));
-            const int need = (k + waves - 1) / waves;
-            for (int i = 0; i < need; ++i) {
-                edge = wave_max(left);
-                const uint64_t at = __ballot(left == edge);
-                if (lane_id() == __builtin_ctzll(at)) left = -INFINITY;
-            }
-            if (wave_id() >= waves) edge = INFINITY;
-            if (lane_id() == 0) s_edge[wave_id()] = edge;
-            __syncthreads();
-            edge = fminf(fminf(s_edge[0], s_edge[1]), fminf(s_edge[2], s_edge[3]));
-        }
-        auto passes = [&](float v, int t) { return v >= edge && pack_logit(v, t) > least; };
-        int mine = 0;
-        if (top >= edge && pack_logit(top, 0) > least) {
+        if (R > -INFINITY) {
+            float add[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) mine += passes(value(i, e), token(i, e));
-        }
-        if (tid == 0) s_count = have;
-        __syncthreads();
-        // room for them is taken one after the other; more than the pool holds (masses of equal values) go in by single
-        // elements, ranked in between
-        int at = mine ? atomicAdd(&s_count, mine) : 0;
-        __syncthreads();
-        const int total = s_count;
-        if (total == have) continue;
-        if (total <= kBeamPool) {
-            if (mine) {
+                for (int e = 0; e < kPer; ++e) add[e & 1] += __builtin_amdgcn_exp2f((value(i, e) - R) * kLog2e);
+            float more = add[0] + add[1];
+            if (__ballot(more != more)) {                  // NaN, or the largest is infinite: those share the probability
+                more = 0.f;
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i)
 #pragma unroll
                     for (int e = 0; e < kPer; ++e) {
-                        const float v = value(i, e);
-                        if (passes(v, token(i, e))) s_pool[at++] = pack_logit(v, token(i, e));
+                        const float v = fmaxf(value(i, e), -INFINITY);
+                        more += R == INFINITY ? (v == INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f((v - R) * kLog2e);
                     }
             }
-            __syncthreads();
-            rank_pool(s_pool, total, s_best, k);
-            have = min(total, k);
-            __syncthreads();
-            least = have == k ? s_best[k - 1] : 0;
-            for (int i = tid; i < have; i += kBeamThreads) s_pool[i] = s_best[i];
-            __syncthreads();
-        } else {
-            for (int i = 0; i < kLoads; ++i)
-                for (int e = 0; e < kPer; ++e) {
-                    float v = -INFINITY;                   // element (i, e), without indexing registers
-#pragma unroll
-                    for (int u = 0; u < kLoads; ++u)
-#pragma unroll
-                        for (int w = 0; w < kPer; ++w) if (u == i && w == e) v = value(u, w);
-                    if (tid == 0) s_count = have;
-                    __syncthreads();
-                    if (passes(v, token(i, e))) s_pool[atomicAdd(&s_count, 1)] = pack_logit(v, token(i, e));
-                    __syncthreads();
-                    const int n = s_count;
-                    if (n == have) continue;
-                    rank_pool(s_pool, n, s_best, k);
-                    have = min(n, k);
-                    __syncthreads();
-                    least = have == k ? s_best[k - 1] : 0;
-                    for (int j = tid; j < have; j += kBeamThreads) s_pool[j] = s_best[j];
-                    __syncthreads();
-                }
+            sum += more;
         }
+        // what has to be reached: above `least`, or in the first tile at least `edge`, which k of the lanes' maxima reach if so
+        // many lanes have any
+        float edge = -INFINITY;
+        if (tile == wave) {
+            float left = top;
+            for (int i = 0; i < k; ++i) {
+                edge = wave_max(left);
+                const uint64_t at = __ballot(left == edge);
+                if (lane == __builtin_ctzll(at)) left = -INFINITY;
+            }
+        }
+        // they go in by ballots; when the pool is full (masses of equal values) it is ranked in between
+        float reach = fmaxf(edge, least ? logit_of(least) : -INFINITY);
+        if (!__ballot(top >= reach && top > -INFINITY)) continue;
+        int n = have;
+        auto settle = [&]() {
+            __builtin_amdgcn_wave_barrier();
+            rank_pool(pool, n, best, k, lane, 64);
+            __builtin_amdgcn_wave_barrier();
+            have = n = min(n, k);
+            least = have == k ? best[k - 1] : 0;
+            if (least) reach = fmaxf(edge, logit_of(least));
+            if (lane < have) pool[lane] = best[lane];
+            __builtin_amdgcn_wave_barrier();
+        };
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const float v = value(i, e);
+                if (!__ballot(v >= reach)) continue;
+                const unsigned long long word = pack_logit(v, token(i, e));
+                const bool in = v >= reach && word > least;
+                const uint64_t who = __ballot(in);
+                if (in) pool[n + __popcll(who & ((1ull << lane) - 1ull))] = word;
+                n += __popcll(who);
+                if (n > kBeamPool - 64) settle();
+            }
+        if (n > have) settle();
     }
-    unsigned long long* out = a.keys + (int64_t)blockIdx.x * k;
-    for (int i = tid; i < k; i += kBeamThreads) out[i] = i < have ? s_pool[i] : 0;
-    const float wm = wave_max(m);
-    float ws = m == -INFINITY ? 0.f : m == wm ? sum : wm == INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f((m - wm) * kLog2e);
-    ws = group_sum<64>(ws);
-    if (lane_id() == 0) s_sum[wave_id()] = make_float2(wm, ws);
+    // join the lanes, then the wavefronts
+    const float ws = group_sum<64>(sum);
+    if (lane == 0) s_sum[wave] = make_float2(R, ws);
+    if (lane < k) pool[lane] = lane < have ? pool[lane] : 0;
     __syncthreads();
-    if (tid == 0) {
-        const float bm = fmaxf(fmaxf(s_sum[0].x, s_sum[1].x), fmaxf(s_sum[2].x, s_sum[3].x));
-        float bs = 0.f;
-        for (int w = 0; w < 4; ++w)
-            bs += s_sum[w].x == bm ? s_sum[w].y : s_sum[w].x == -INFINITY || bm == INFINITY ? 0.f : s_sum[w].y * __builtin_amdgcn_exp2f((s_sum[w].x - bm) * kLog2e);
-        a.sums[blockIdx.x] = make_float2(bm, bs);
+    // the lists of the four wavefronts, one behind the other
+    unsigned long long* both = s_pool[0];
+    if (wave > 0 && lane < k) both[wave * k + lane] = pool[lane];
+    __syncthreads();
+    rank_parts(both, kWaves * k, a.keys + (int64_t)blockIdx.x * k, k);
+    if (threadIdx.x == 0) {
+        float2 all = s_sum[0];
+        for (int w = 1; w < kWaves; ++w) all = join_sums(all, s_sum[w]);
+        a.sums[blockIdx.x] = all;
     }
 }
 
@@ -293,9 +296,8 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
         }
         for (int i = lane; i < a.parts * k; i += 64) lists[i] = a.keys[row * a.parts * k + i];
         const float2 ps = lane < a.parts ? a.sums[row * a.parts + lane] : make_float2(-INFINITY, 0.f);
-        const float top = wave_max(ps.x);
-        const float sum = group_sum<64>(ps.x == top ? ps.y : ps.x == -INFINITY || top == INFINITY ? 0.f : ps.y * __builtin_amdgcn_exp2f((ps.x - top) * kLog2e));
-        const float lse = logf(sum);
+        const float R = wave_max(ps.x);
+        const float sum = group_sum<64>(ps.x == R ? ps.y : ps.x == -INFINITY || R == INFINITY ? 0.f : ps.y * __builtin_amdgcn_exp2f((ps.x - R) * kLog2e));
         __builtin_amdgcn_wave_barrier();
         int at = 0;
         unsigned long long mine = 0;                       // the lane's result: the best of rank `lane`
@@ -306,6 +308,9 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
             if (best == 0) break;
             if (head == best) { ++at; head = at < k ? lists[lane * k + at] : 0; }
         }
+        // the logarithm of the sum of exp(x - top), top the largest logit: the factor between R and it in 64 bits
+        const float top = logit_of(__shfl((long long)mine, 0));
+        const float lse = logf(R == top ? sum : (float)((double)sum * exp((double)R - (double)top)));
         if (lane < k) {
             const float v = logit_of(mine);
             score[lane] = mine ? run + ((v == top ? 0.f : v - top) - lse) : -INFINITY;
@@ -349,11 +354,12 @@ struct BeamPlan { int parts, share; };
 // Parts of a row: enough workgroups for the chip (four of them fit a compute unit), tiles of their own, few enough for a wavefront
 // to join, whose lists (448 entries) fit LDS.
 static BeamPlan plan_beams(int64_t rows, int vocab, int k) {
-    const int tiles = (vocab + kBeamTile - 1) / kBeamTile;
+    constexpr int kShare = 4 * kBeamTile;                  // a tile for each of the wavefronts
+    const int tiles = (vocab + kShare - 1) / kShare;
     const int64_t want = std::max<int64_t>(1, 2048 / rows);
     const int parts = (int)std::min<int64_t>({want, tiles, 64, std::max(1, 448 / k)});
     const int per = (tiles + parts - 1) / parts;
-    return BeamPlan{(tiles + per - 1) / per, per * kBeamTile};
+    return BeamPlan{(tiles + per - 1) / per, per * kShare};
 }
 
 static int check_beams(int n_prompts, int beams_in, int vocab, int beams_out) {
