@@ -61,6 +61,10 @@ __device__ __forceinline__ void fetch16(const void* g, uint32_t to) {
 __device__ __forceinline__ void fetch4(const void* g, uint32_t to) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(g), "s"(to) : "memory");
 }
+// the same from `off` bytes behind a place that all lanes share
+__device__ __forceinline__ void fetch16(const void* base, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(off), "s"(base), "s"(to) : "memory");
+}
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory"); }
 __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -198,20 +202,26 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
     const int value_place = (S::kKeys + value_row) * S::kPitch + (((2 * (lane >> 4 & 1) + (lane & 3) / 2) ^ place_swap<S::kChunks>(value_row)) << 4) + (lane & 1) * 8;
     constexpr int kRowBit = S::kChunks == 8 ? 0 : 32;
 
-    // the chunk of a row that a lane fetches, in bytes: sixteen rows repeat
-    constexpr int kChunkKinds = std::min(S::kLoads, 16 / S::kRowsPerLoad);
-    int chunk_bytes[kChunkKinds];
-#pragma unroll
-    for (int u = 0; u < kChunkKinds; ++u) {
-        const int r = (NARROW ? 0 : wave * S::kWaveRows) + u * S::kRowsPerLoad + lane / S::kChunks;
-        chunk_bytes[u] = ((lane % S::kChunks) ^ place_swap<S::kChunks>(r)) * 16;
-    }
+    // the chunk of a row that a lane fetches by load 0, in bytes; another load's rows change single bits of it
+    const int chunk_place = ((lane % S::kChunks) ^ place_swap<S::kChunks>((NARROW ? 0 : wave * S::kWaveRows) + lane / S::kChunks)) * 16;
+    auto chunk_bytes = [&](int u) {
+        return (uint32_t)(chunk_place ^ (S::kChunks == 8 ? 0 : S::kChunks == 16 ? (u & 3) << 4 : (u & 1) << 7 | (u >> 1 & 3) << 4));
+    };
     // in registers: a choice between two of the arguments would otherwise be a load, which waits for the tiles on their way
     const int pre_shift = __builtin_amdgcn_readfirstlane(a.step.prefix_shift), own_shift = __builtin_amdgcn_readfirstlane(a.step.shift);
     const int pre_last = __builtin_amdgcn_readfirstlane(a.step.prefix_last), own_last = __builtin_amdgcn_readfirstlane(a.step.own_last);
     const int page_shift = a.cache.page_shift;
     const char* kbase = (const char*)a.cache.k + kvh * a.cache.head_stride * 2;
     const char* vbase = (const char*)a.cache.v + kvh * a.cache.head_stride * 2;
+    // Where a wavefront's rows of every tile lie in one page each, which then is found by scalar instructions alone: pages of at
+    // least so many tokens, and a prefix of whole groups of them.  (Without this the vector units, which bound long prompts, spend
+    // a third of their time on places.)
+    const bool paged = !NARROW && (plen == 0 || (1 << pre_shift >= S::kWaveRows && plen % S::kWaveRows == 0)) &&
+                       1 << own_shift >= S::kWaveRows && a.cache.token_bytes >= 0 && a.cache.token_bytes < 1 << 26;
+    uint32_t page_place[NARROW ? 1 : S::kLoads];
+#pragma unroll
+    for (int u = 0; u < (NARROW ? 1 : S::kLoads); ++u)
+        page_place[u] = (uint32_t)((u * S::kRowsPerLoad + lane / S::kChunks) * a.cache.token_bytes) + chunk_bytes(u);
 
     for (int tile = tile0; tile * S::kRows < rows; tile += pass.n_tile) {
         // rows of the workgroup and of this lane
@@ -288,6 +298,29 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
                 fetch4((pre ? ptab : otab) + ((pre ? key : key - plen) >> (pre ? pre_shift : own_shift)), entries_at + ((i & (S::kEntrySlots - 1)) * S::kSets + set) * 256);
             }
         };
+        // the first key of the wavefront's rows of a tile, where they lie in one page; its entry is read by a scalar load
+        auto page_key = [&](int i) { return min(first_key(i) + wave * S::kWaveRows, (ke - 1) & -S::kWaveRows); };
+        auto page_entry = [&](int i) {
+            const int key = page_key(i);
+            typedef const __attribute__((address_space(4))) int32_t* scalar_t;
+            return key < plen ? *(scalar_t)(uintptr_t)(ptab + (key >> pre_shift)) : *(scalar_t)(uintptr_t)(otab + ((key - plen) >> own_shift));
+        };
+        int entry = 0;                     // of the next tile to be fetched
+        auto fetch_paged = [&](int i) __attribute__((always_inline)) {
+            const int key = page_key(i);
+            const bool pre = key < plen;
+            const int shift = pre ? pre_shift : own_shift, up = page_shift - shift, j = pre ? key : key - plen;
+            const int e = min(max(entry, 0), pre ? pre_last : own_last);
+            const int in_page = (e & ((1 << up) - 1)) << shift | (j & ((1 << shift) - 1));
+            const int64_t at = (int64_t)(e >> up) * a.cache.page_bytes + (int64_t)in_page * a.cache.token_bytes;
+            const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes + wave * S::kWaveRows * S::kPitch;
+#pragma unroll
+            for (int u = 0; u < S::kLoads; ++u)
+                if (D % 64 == 0 || chunk_bytes(u) < D * 2) {
+                    fetch16(kbase + at, page_place[u], to + u * 1024);
+                    fetch16(vbase + at, page_place[u], to + S::kKeys * S::kPitch + u * 1024);
+                }
+        };
         int64_t place[S::kSets];           // bytes from the cache's begin, of the next tile to be fetched
         auto locate = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
@@ -305,8 +338,8 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes + (NARROW ? 0 : wave * S::kWaveRows * S::kPitch);
 #pragma unroll
             for (int u = 0; u < S::kLoads; ++u) {
-                const int64_t at = quad_lane(place[u / 4], u & 3) + chunk_bytes[u % kChunkKinds];
-                if (D % 64 == 0 || chunk_bytes[u % kChunkKinds] < D * 2) {
+                const int64_t at = quad_lane(place[u / 4], u & 3) + chunk_bytes(u);
+                if (D % 64 == 0 || chunk_bytes(u) < D * 2) {
                     fetch16(kbase + at, to + u * 1024);
                     fetch16(vbase + at, to + S::kKeys * S::kPitch + u * 1024);
                 }
@@ -461,7 +494,10 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             __builtin_amdgcn_sched_barrier(0);
         };
 
-        if (n > 0) {
+        if (paged) {
+            if (n > 0) { entry = page_entry(0); fetch_paged(0); }
+            if (n > 1) entry = page_entry(1);
+        } else if (n > 0) {
 #pragma unroll
             for (int i = 0; i <= 2 * S::kAhead; ++i)
                 if (i < n) fetch_entries(i);
@@ -476,6 +512,11 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
             if (S::kAhead > 1 && i + S::kAhead <= n) wait_loads<(S::kAhead - 1) * 2 * S::kLoads>();
             else wait_loads<0>();
             if (!NARROW) barrier();      // for every wavefront, and the tile before has been read
+            if (paged) {
+                if (i + 1 < n) fetch_paged(i + 1);
+                if (i + 2 < n) entry = page_entry(i + 2);
+                return;
+            }
             if (i + S::kAhead < n) fetch_tile(i + S::kAhead);
             if (i + 2 * S::kAhead + 1 < n) fetch_entries(i + 2 * S::kAhead + 1);
         };
@@ -484,12 +525,12 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         for (int i = 0; i < n_full; ++i) {
             arrive(i);
             if (!idle) compute(i, std::true_type{});
-            if (i + S::kAhead + 1 < n) locate(i + S::kAhead + 1);
+            if (!paged && i + S::kAhead + 1 < n) locate(i + S::kAhead + 1);
         }
         for (int i = n_full; i < n; ++i) {
             arrive(i);
             if (!idle) compute(i, std::false_type{});
-            if (i + S::kAhead + 1 < n) locate(i + S::kAhead + 1);
+            if (!paged && i + S::kAhead + 1 < n) locate(i + S::kAhead + 1);
         }
         l += other_half(l);
 
