@@ -718,9 +718,9 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
         const int64_t most = (keys + least - 1) / least;
         return (int)std::max<int64_t>(1, std::min<int64_t>({(want + units - 1) / units, most, 64}));
     };
-    // few rows: pieces of 512 keys and more for several workgroups a place on the chip (two fit a compute unit), smaller ones
+    // few rows: pieces of 1024 keys and more for several workgroups a place on the chip (two fit a compute unit), smaller ones
     // only while places are free
-    auto split_few = [&](int64_t units, int64_t keys) { return std::max(split(units, 4096, keys, 512), split(units, 512, keys, 128)); };
+    auto split_few = [&](int64_t units, int64_t keys) { return std::max(split(units, 4096, keys, 1024), split(units, 512, keys, 128)); };
     p.tiles_narrow = 1;
     // (unknown: twice what sequences of equal lengths would need)
     const int64_t tile_rows = st->max_q > 0 || sv.n_seq == 1 ? most_q * group : std::min(rows, 2 * rows / sv.n_seq);
