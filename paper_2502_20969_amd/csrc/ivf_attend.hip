@@ -135,13 +135,20 @@ struct Shape {
     static_assert(!NARROW || (size_t)kWaves * 32 * D * 4 + kWaves * 32 * 8 <= (size_t)kStageBytes, "room to join the wavefronts");
 };
 
+// x as if it were new: what follows from it is computed where it is used, not kept from before a loop.  With heads of 256 such values
+// would be kept in scratch memory, and a reload waits for every tile on its way (narrow, 24 sequences of up to 20,000 keys: 809 us
+// against 452)
+__device__ __forceinline__ int again(int x) { asm volatile("" : "+v"(x)); return x; }
+
 // chunk c of row r of a tile lies at place c ^ place_swap(r)
 template <int CHUNKS> __device__ __forceinline__ int place_swap(int row) {
     return CHUNKS == 8 ? row & 7 : (row & 3) << 2 | (row >> 2 & 3);
 }
 
+// Registers: two workgroups a compute unit, but of heads of 256 one, whose sums and queries alone take 192 (eight wavefronts: a prompt
+// of 8000 tokens 890 us against 803)
 template <typename T, int D, bool NARROW>
-__global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128 ? 1 : 2)) void attend_kernel(AttendArgs a) {
     using S = Shape<D, NARROW>;
     using H = Half<T>;
     constexpr int kKeySteps = D / 16, kBlocks = D / 32, kKeyTiles = S::kKeys / 32;
@@ -287,6 +294,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         // the place of the row that load l % 4 of the set brings to its group, so that a load finds its lanes' places in the
         // lanes' own quads
         auto row_of = [&](int set) {
+            const int lane = D > 128 ? again(lane_id()) : lane_id();
             return (NARROW ? 0 : wave * S::kWaveRows) + (S::kLoads < 4 ? lane & (S::kLoads - 1) : set * 4 + (lane & 3)) * S::kRowsPerLoad + lane / S::kChunks;
         };
         auto key_of = [&](int i, int set) { return min(first_key(i) + row_of(set), ke - 1); };
@@ -336,6 +344,10 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         };
         auto fetch_tile = [&](int i) __attribute__((always_inline)) {
             const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes + (NARROW ? 0 : wave * S::kWaveRows * S::kPitch);
+            const int swap = D > 128 ? again(chunk_place) : chunk_place;
+            auto chunk_bytes = [&](int u) {
+                return (uint32_t)(swap ^ (S::kChunks == 8 ? 0 : S::kChunks == 16 ? (u & 3) << 4 : (u & 1) << 7 | (u >> 1 & 3) << 4));
+            };
 #pragma unroll
             for (int u = 0; u < S::kLoads; ++u) {
                 const int64_t at = quad_lane(place[u / 4], u & 3) + chunk_bytes(u);
@@ -349,11 +361,21 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
         f16v_t o[kBlocks] = {};
         float m = -INFINITY, l = 0.f;
 
+        // The sums of heads of 256 stay in accumulation registers but where they are scaled; else all 128 change sides twice a tile (a
+        // prompt of 8000 tokens: 803 us against 659)
+        auto keep_sums = [&]() __attribute__((always_inline)) {
+            if constexpr (!NARROW && D > 128) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) asm volatile("" : "+a"(o[b]));
+            }
+        };
+
         // one tile: scores, weights, products; `full`: every row sees all its keys
         auto compute = [&](int i, auto full_tag) __attribute__((always_inline)) {
             constexpr bool full = decltype(full_tag)::value;
             const int j0 = first_key(i);
             const uint32_t tile_at = stage_at + (i % S::kStages) * S::kTileBytes;
+            keep_sums();
             const uint32_t key_at = tile_at + key_place, value_at = tile_at + value_place;
             f16v_t x[kKeyTiles];
 #pragma unroll
@@ -401,6 +423,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW ? 1 : 2)) 
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) o[b] *= f;
             }
+            keep_sums();
             const float minus = (m == -INFINITY ? 0.f : -m) + H::kLift;
             s8_t p[kKeyTiles * 2];
             float sum[2] = {0.f, 0.f};
