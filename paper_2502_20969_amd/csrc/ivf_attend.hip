@@ -180,7 +180,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
     const int before = prefix_of(a.step, g);                               // keys of the prefix, which
     const int plen = pass.mode == kOwn ? 0 : before;                          // this pass reads or not
     if (by_group && plen == 0) return;
-    const int sinks = pass.mode == kOwn ? (a.window > 0 ? a.sinks - before : 0) : a.sinks;
+    const int sinks = pass.mode == kOwn ? (a.window > 0 ? max(0, a.sinks - before) : 0) : a.sinks;
     const int ke = plen + own;
     const int32_t* ptab = a.step.prefix_table + (int64_t)max(g, 0) * a.step.prefix_stride;
     const int32_t* otab = a.step.table + (int64_t)s0 * a.step.table_stride;
@@ -401,13 +401,20 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
             __builtin_amdgcn_sched_barrier(0);
             auto sees = [&](int j) { return j <= lim && (j >= low || j < sinks); };
             if (!full) {
+                const int to = lim - j0 - 4 * half, from = low - j0 - 4 * half, sunk = sinks - j0 - 4 * half;
 #pragma unroll
                 for (int t = 0; t < kKeyTiles; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = j0 + t * 32 + (r & 3) + 8 * (r >> 2) + 4 * half;
-                        x[t][r] = sees(j) ? x[t][r] : -INFINITY;
-                    }
+                    for (int r = 0; r < 16; ++r) x[t][r] = t * 32 + (r & 3) + 8 * (r >> 2) <= to ? x[t][r] : -INFINITY;
+                if (a.window > 0) {
+#pragma unroll
+                    for (int t = 0; t < kKeyTiles; ++t)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int j = t * 32 + (r & 3) + 8 * (r >> 2);
+                            x[t][r] = j >= from || j < sunk ? x[t][r] : -INFINITY;
+                        }
+                }
             }
             float top = x[0][0];
 #pragma unroll
@@ -452,52 +459,45 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
                 }
                 return v;
             };
-            bool odd = false;
             if (!full) {
-                uint32_t any = 0;
-#pragma unroll 1
-                for (int s = 0; s < kKeyTiles * 2; ++s)
-#pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) {
-                        const s8_t v = value(s, b);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) any |= ((uint16_t)v[e] & H::kExponent) == H::kExponent;
-                    }
-                odd = __ballot(any != 0) != 0;
-            }
-            if (__builtin_expect(odd, 0)) {
-                // A value that is not finite, times the weight zero of a row that does not see it, would be NaN: such values are left
-                // out of the product, and counted instead for the rows that see them, the three kinds in one number
-#pragma unroll
-                for (int s = 0; s < kKeyTiles * 2; ++s)
-#pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) {
-                        s8_t v = value(s, b);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = ((uint16_t)v[e] & H::kExponent) == H::kExponent ? (short)0 : v[e];
-                        o[b] = H::mfma(v, p[s], o[b]);
-                    }
-                auto of = [](float x) { return __builtin_bit_cast(short, (T)x); };
+                // A value that is not finite, times the weight zero of a row that does not see it, is NaN.  So a block of the tile's
+                // sums is formed by itself, and added if it is finite (the check that costs least: reading all values for it
+                // beforehand took longer than the products).  If not, such values are left out of the product, and counted
+                // instead for the rows that see them, the three kinds in one number
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
                     f16v_t y{};
-#pragma unroll 1
-                    for (int s = 0; s < kKeyTiles * 2; ++s) {
-                        s8_t v = value(s, b), w;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const uint32_t bits = (uint16_t)v[e];
-                            v[e] = (bits & H::kExponent) != H::kExponent ? (short)0
-                                   : (bits & 0x7FFFu) != H::kExponent ? of(16384.f) : bits >> 15 ? of(128.f) : of(1.f);
-                            w[e] = sees(j0 + 16 * s + (e & 3) + 8 * (e >> 2) + 4 * half) ? of(1.f) : (short)0;
+                    for (int s = 0; s < kKeyTiles * 2; ++s) y = H::mfma(value(s, b), p[s], y);
+                    float odd = 0.f;                                   // NaN where one is not finite
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) odd = __builtin_fmaf(y[r], 0.f, odd);
+                    if (__builtin_expect(__ballot(odd != odd) != 0, 0)) {
+                        auto of = [](float x) { return __builtin_bit_cast(short, (T)x); };
+                        f16v_t n{};
+                        y = f16v_t{};
+#pragma unroll
+                        for (int s = 0; s < kKeyTiles * 2; ++s) {
+                            s8_t v = value(s, b), kind, seen;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int j = j0 + 16 * s + (e & 3) + 8 * (e >> 2) + 4 * half;
+                                const uint32_t bits = (uint16_t)v[e];
+                                const bool finite = (bits & H::kExponent) != H::kExponent;
+                                kind[e] = finite ? (short)0 : (bits & 0x7FFFu) != H::kExponent ? of(16384.f) : bits >> 15 ? of(128.f) : of(1.f);
+                                v[e] = finite ? v[e] : (short)0;
+                                seen[e] = sees(j) ? of(1.f) : (short)0;
+                            }
+                            y = H::mfma(v, p[s], y);
+                            n = H::mfma(kind, seen, n);
                         }
-                        y = H::mfma(v, w, y);
-                    }
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int n = (int)y[r];           // NaN, -inf and +inf by digits of 128
-                        if (n != 0) o[b][r] += n >= 16384 || ((n & 127) && n >= 128) ? NAN : n >= 128 ? -INFINITY : INFINITY;
+                        for (int r = 0; r < 16; ++r) {
+                            const int c = (int)n[r];           // NaN, -inf and +inf by digits of 128
+                            if (c != 0) y[r] += c >= 16384 || ((c & 127) && c >= 128) ? NAN : c >= 128 ? -INFINITY : INFINITY;
+                        }
                     }
+                    o[b] += y;
                 }
                 return;
             }
