@@ -544,6 +544,15 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
             if (i + 2 * S::kAhead + 1 < n) fetch_entries(i + 2 * S::kAhead + 1);
         };
         const bool idle = !NARROW && row_first + wave * 32 >= rows;        // no rows: this wavefront only fetches
+        // the keys that some row of the wavefront sees: [0, wave_sinks) and [wave_low, wave_lim]
+        int wave_lim = lim, wave_low = mine ? low : 0x7FFFFFFF;
+        for (int w = 16; w >= 1; w >>= 1) { wave_lim = max(wave_lim, __shfl_xor(wave_lim, w)); wave_low = min(wave_low, __shfl_xor(wave_low, w)); }
+        wave_lim = __builtin_amdgcn_readfirstlane(wave_lim);
+        wave_low = __builtin_amdgcn_readfirstlane(wave_low);
+        auto unseen = [&](int i) {
+            const int j = first_key(i);
+            return j > wave_lim || (j + S::kKeys <= wave_low && j >= sinks);
+        };
         // two loops, so that what the tiles at the edges need takes no registers from the others
         for (int i = 0; i < n_full; ++i) {
             arrive(i);
@@ -552,7 +561,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
         }
         for (int i = n_full; i < n; ++i) {
             arrive(i);
-            if (!idle) compute(i, std::false_type{});
+            if (!idle && !unseen(i)) compute(i, std::false_type{});
             if (!paged && i + S::kAhead + 1 < n) locate(i + S::kAhead + 1);
         }
         l += other_half(l);
@@ -730,13 +739,18 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
     auto known = [](int hint, int64_t cap) { return hint > 0 ? std::min<int64_t>(hint, cap) : cap; };
     const int64_t len = known(st->max_len, sv.own_cap), pre = sv.n_groups > 0 ? known(st->max_prefix, sv.prefix_cap) : 0;
     const int64_t most_q = known(st->max_q, sv.n_tokens);
-    p.shared = pre > 0 && sv.n_seq > sv.n_groups && rows < (int64_t)sv.n_seq * kWideRows;
+    // a pass of its own for the prefix costs a launch and partial sums, and saves the prefix's keys of all sequences but one: worth it
+    // from some hundred keys on (16 groups of 4, 8 key heads of 128: prefixes of 128 keys 39.7 us with it, 31.6 without; of 500 44.8 and
+    // 43.5; of 2000 55 and 73)
+    p.shared = pre >= 512 && sv.n_seq > sv.n_groups && rows < (int64_t)sv.n_seq * kWideRows;
     const int64_t keys_all = p.shared ? len : len + pre;
     // keys that a row reads: of a window a tile more
     auto read_keys = [&](int64_t keys) { return window > 0 ? std::min<int64_t>(keys, (int64_t)window + std::min<int64_t>(sinks, keys) + most_q + 64) : keys; };
     const int64_t keys = read_keys(keys_all);
     p.wide = sv.n_seq == 1 ? rows > kNarrowRows : most_q * group > kNarrowRows;
-    p.narrow = sv.n_seq == 1 ? !p.wide : true;
+    // where the sequences have about as many tokens each, none or few have few rows: not worth a launch of their own and the joining
+    // that its split brings (34 prompts of 361 to 1085 tokens: 103 us with it, 69 without)
+    p.narrow = !p.wide || rows < (int64_t)sv.n_seq * most_q * group / 2;
     auto split = [](int64_t units, int64_t want, int64_t keys, int64_t least) {
         const int64_t most = (keys + least - 1) / least;
         return (int)std::max<int64_t>(1, std::min<int64_t>({(want + units - 1) / units, most, 64}));
@@ -744,12 +758,14 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
     // few rows: pieces of 1024 keys and more for several workgroups a place on the chip (two fit a compute unit), smaller ones
     // only while places are free
     auto split_few = [&](int64_t units, int64_t keys) { return std::max(split(units, 4096, keys, 1024), split(units, 512, keys, 128)); };
+    // many rows: only as far as places are free, since every piece more is 2 x 4 d bytes a row written and read
+    auto split_many = [](int64_t units, int64_t keys) { return (int)std::max<int64_t>(1, std::min<int64_t>({512 / units, keys / 1024, 64})); };
     p.tiles_narrow = 1;
     // (unknown: twice what sequences of equal lengths would need)
     const int64_t tile_rows = st->max_q > 0 || sv.n_seq == 1 ? most_q * group : std::min(rows, 2 * rows / sv.n_seq);
     p.tiles_wide = (int)std::max<int64_t>(1, (tile_rows + kWideRows - 1) / kWideRows);
     if (p.narrow) p.split_narrow = split_few((int64_t)sv.n_seq * hkv, keys);
-    if (p.wide) p.split_wide = split(hkv * ((rows + kWideRows - 1) / kWideRows + sv.n_seq - 1), 512, keys, 512);
+    if (p.wide) p.split_wide = split_many(hkv * ((rows + kWideRows - 1) / kWideRows + sv.n_seq / 2), keys);
     p.n_own = std::max(p.split_narrow, p.split_wide);
     if (p.shared) {
         const int64_t group_rows = rows / sv.n_groups;
