@@ -6,6 +6,7 @@ module raises at import of the library if it has not been built.
 """
 import collections
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -661,6 +662,7 @@ def ivf_attend_workspace(step, cache, n_q_heads, window=0, sinks=0):
     return need
 
 
+@functools.lru_cache(maxsize=64)             # a function of the sizes alone
 def ivf_beam_workspace(n_prompts, beams_in, vocab, beams_out):
     """Bytes of workspace of ivf_beam_step with these sizes."""
     n = C.c_size_t(0)
@@ -672,12 +674,12 @@ def _state(src, dst, rows_in, rows_out):
     """A state and its destination: rows of the same contiguous elements, evenly spaced."""
     if src.dtype is not dst.dtype or not (src.is_cuda and dst.is_cuda):
         raise ValueError("a state and its destination must be CUDA tensors of the same type")
-    if src.shape[0] != rows_in or dst.shape[0] != rows_out or src.shape[1:] != dst.shape[1:]:
+    before, after = src.shape, dst.shape
+    if before[0] != rows_in or after[0] != rows_out or before[1:] != after[1:]:
         raise ValueError("a state has a row per beam, before and after")
-    for x in (src, dst):
-        if not x.is_contiguous() and not x[0].is_contiguous():
-            raise ValueError("the rows of a state must be contiguous")
-    size = src.element_size()
+    if not (src.is_contiguous() or src[0].is_contiguous()) or not (dst.is_contiguous() or dst[0].is_contiguous()):
+        raise ValueError("the rows of a state must be contiguous")
+    size = src.itemsize
     row = src.numel() // rows_in * size
     return BeamStateArg(src.data_ptr(), dst.data_ptr(), row, src.stride(0) * size if rows_in > 1 else row, dst.stride(0) * size if rows_out > 1 else row)
 
@@ -719,7 +721,7 @@ def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), 
     at = out.data_ptr()
     status = load().ivf_beam_step(logits.data_ptr(), stride, _code(logits.dtype), p, b, vocab, scores.data_ptr(), dp, eos, n,
                                   at, at + 4 * p * n, at + 8 * p * n, fin.data_ptr(), args, len(states),
-                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(), _on(stream))
+                                  workspace.data_ptr(), workspace.nbytes, _on(stream))
     if status != 0:
         _check(status)
     return score, parent, token, fin

@@ -273,9 +273,10 @@ __device__ __forceinline__ void move_row(const BeamMove& m, int64_t from_row, in
     for (int64_t i = done + i0; i < m.row_bytes; i += step) to[i] = from[i];
 }
 
-// One workgroup per prompt.  A wavefront joins the parts of a row, a lane per part: k times the best of the lists' heads.
-// Then one wavefront picks from the rows, a lane per row, in the same way; at last all move the states' rows, where they
-// are small.  Latency bounds it.
+// One workgroup per prompt.  A wavefront joins the parts of a row, then the rows' continuations are joined, and at last
+// all move the states' rows, where they are small.  Latency bounds it (7.3 us for 64 prompts of 8 beams): few candidates
+// are ranked by counting, which has no chain of dependent steps, more by taking k times the best of the sorted lists' heads, a
+// lane per list (9.4 us for those 64 prompts).
 constexpr int kPickThreads = 512;
 __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
     __shared__ float s_score[IVF_MAX_BEAMS * IVF_MAX_BEAMS];
@@ -291,50 +292,80 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamArgs a) {
         float* score = s_score + b * k;
         int32_t* token = s_token + b * k;
         if (done || !(run > -INFINITY)) {
-            if (lane < k) { score[lane] = done && lane == 0 ? run : -INFINITY; token[lane] = a.eos; }
+            if (lane < k) { score[lane] = done && lane == 0 && run > -INFINITY ? run : -INFINITY; token[lane] = a.eos; }
             continue;
         }
-        for (int i = lane; i < a.parts * k; i += 64) lists[i] = a.keys[row * a.parts * k + i];
+        const int n = a.parts * k;
+        const unsigned long long* keys = a.keys + row * n;
         const float2 ps = lane < a.parts ? a.sums[row * a.parts + lane] : make_float2(-INFINITY, 0.f);
+        unsigned long long mine = 0;                       // the lane's result: the best of rank `lane`
+        if (n <= 64) {                                     // by counting
+            const unsigned long long word = lane < n ? keys[lane] : 0;
+            const int lo = (int)word, hi = (int)(word >> 32);
+            int rank = 0;
+            for (int j = 0; j < n; ++j) {
+                const unsigned long long other = (unsigned long long)(uint32_t)__builtin_amdgcn_readlane(hi, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, j);
+                rank += other > word;
+            }
+            if (lane < k) lists[lane] = 0;
+            __builtin_amdgcn_wave_barrier();
+            if (word && rank < k) lists[rank] = word;
+            __builtin_amdgcn_wave_barrier();
+            if (lane < k) mine = lists[lane];
+            __builtin_amdgcn_wave_barrier();
+        } else {                                           // k times the best of the lists' heads
+            for (int i = lane; i < n; i += 64) lists[i] = keys[i];
+            __builtin_amdgcn_wave_barrier();
+            int at = 0;
+            unsigned long long head = lane < a.parts ? lists[lane * k] : 0;
+            for (int i = 0; i < k; ++i) {
+                const unsigned long long best = wave_max(head);
+                if (lane == i) mine = best;
+                if (best == 0) break;
+                if (head == best) { ++at; head = at < k ? lists[lane * k + at] : 0; }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
         const float R = wave_max(ps.x);
         const float sum = group_sum<64>(ps.x == R ? ps.y : ps.x == -INFINITY || R == INFINITY ? 0.f : ps.y * __builtin_amdgcn_exp2f((ps.x - R) * kLog2e));
-        __builtin_amdgcn_wave_barrier();
-        int at = 0;
-        unsigned long long mine = 0;                       // the lane's result: the best of rank `lane`
-        unsigned long long head = lane < a.parts ? lists[lane * k] : 0;
-        for (int i = 0; i < k; ++i) {
-            const unsigned long long best = wave_max(head);
-            if (lane == i) mine = best;
-            if (best == 0) break;
-            if (head == best) { ++at; head = at < k ? lists[lane * k + at] : 0; }
-        }
         // the logarithm of the sum of exp(x - top), top the largest logit: the factor between R and it in 64 bits
         const float top = logit_of(__shfl((long long)mine, 0));
         const float lse = logf(R == top ? sum : (float)((double)sum * exp((double)R - (double)top)));
         if (lane < k) {
             const float v = logit_of(mine);
-            score[lane] = mine ? run + ((v == top ? 0.f : v - top) - lse) : -INFINITY;
+            const float y = run + ((v == top ? 0.f : v - top) - lse);
+            score[lane] = mine && y > -INFINITY ? y : -INFINITY;
             token[lane] = (int32_t)~(uint32_t)mine;
         }
     }
     __syncthreads();
-    if (wave == 0) {
-        const bool mine = lane < a.beams;
+    const int n = a.beams * k;
+    auto put = [&](int i, float top, int from, int token) {      // continuation i: of row `from`, none if top is -inf
+        const bool reach = top > -INFINITY;
+        const int64_t o = (int64_t)prompt * k + i, row = row0 + (reach ? from : 0);
+        a.scores_out[o] = top;
+        a.parent[o] = (int32_t)row;
+        a.token[o] = reach ? token : -1;
+        a.done_out[o] = !reach || (a.done_in && a.done_in[row]) || token == a.eos;
+        s_parent[i] = (int32_t)row;
+    };
+    if (n <= kPickThreads) {                               // by counting, a thread per continuation
+        if (wave * 64 < n) {
+            const int c = min((int)threadIdx.x, n - 1);
+            const float mine = s_score[c];
+            int rank = 0;
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) rank += s_score[j] > mine || (s_score[j] == mine && j < c);
+            if ((int)threadIdx.x < n && rank < k) put(rank, mine, c / k, s_token[c]);
+        }
+    } else if (wave == 0) {                                // k times the best of the rows' heads
         int at = 0;
-        float head = mine ? s_score[lane * k] : -INFINITY;
+        float head = lane < a.beams ? s_score[lane * k] : -INFINITY;
         for (int i = 0; i < k; ++i) {
             const float top = wave_max(head);
             const uint64_t reach = __ballot(head == top && top > -INFINITY);
-            const int from = reach ? __builtin_ctzll(reach) : 0;
-            if (lane == from) {
-                const int o = prompt * k + i;
-                const int token = reach ? s_token[lane * k + at] : -1;
-                const bool done = reach && a.done_in && a.done_in[row0 + from];
-                a.scores_out[o] = top;
-                a.parent[o] = row0 + from;
-                a.token[o] = token;
-                a.done_out[o] = !reach || done || token == a.eos;
-                s_parent[i] = row0 + from;
+            if (lane == (reach ? __builtin_ctzll(reach) : 0)) {
+                put(i, top, lane, s_token[lane * k + at]);
                 if (reach) { ++at; head = at < k ? s_score[lane * k + at] : -INFINITY; }
             }
         }
@@ -351,12 +382,13 @@ __global__ __launch_bounds__(256) void beam_move_kernel(BeamArgs a) {
 
 struct BeamPlan { int parts, share; };
 
-// Parts of a row: enough workgroups for the chip (four of them fit a compute unit), tiles of their own, few enough for a wavefront
-// to join, whose lists (448 entries) fit LDS.
+// Parts of a row: four workgroups a compute unit (a wavefront's first tile, in which it finds what has to be reached, costs several
+// others: 64 prompts of 8 beams over 131,072 logits 49 us with 2048 workgroups, 43 with 1024, 52 with 512), tiles of their own, few
+// enough for a wavefront to join, whose lists (448 entries) fit LDS.
 static BeamPlan plan_beams(int64_t rows, int vocab, int k) {
     constexpr int kShare = 4 * kBeamTile;                  // a tile for each of the wavefronts
     const int tiles = (vocab + kShare - 1) / kShare;
-    const int64_t want = std::max<int64_t>(1, 2048 / rows);
+    const int64_t want = std::max<int64_t>(1, 1024 / rows);
     const int parts = (int)std::min<int64_t>({want, tiles, 64, std::max(1, 448 / k)});
     const int per = (tiles + parts - 1) / parts;
     return BeamPlan{(tiles + per - 1) / per, per * kShare};
