@@ -421,8 +421,8 @@ int ivf_schedule(ivf_index* index, const float* q, int32_t nq, int32_t micro, in
  * ivf_kv_cache: the keys and values of one layer.  Token slot t is place t % page of page t / page:
  *   element e of head h is at  (t / page) * page_stride + (t % page) * token_stride + h * head_stride + e
  * of k and of v, so pages can hold tokens one after the other or heads one after the other.  Strides count
- * elements and are multiples of 8; k and v are 16-byte aligned; dtype is IVF_F16 or IVF_BF16; page is a
- * power of two.
+ * elements and are multiples of 8, those of pages and tokens below 2^30; k and v are 16-byte aligned; dtype is
+ * IVF_F16 or IVF_BF16; page is a power of two.
  *
  * ivf_kv_step: the sequences of one step, for all layers.
  *   q_off     [n_seq + 1] first new token of each sequence, ascending from 0 to n_tokens
@@ -488,7 +488,7 @@ int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_
 /*
  * Attention of the new tokens over the cache: out = softmax(scale * q . k) v over the keys that a token sees, in
  * 32 bits, rounded once.  A token at position p sees key j when j <= p and, with window > 0, p - j < window or j <
- * sinks.  A token that sees nothing gets zeros.  The keys of a prefix are read once for all tokens of its group.
+ * sinks.  A token that sees nothing gets zeros.  The keys of a long prefix are read once for all tokens of its group.
  *   q, out     n_tokens x n_q_heads x d, of the cache's type; query head h reads key head
  *              h / (n_q_heads / cache->n_heads)
  *   lse        [n_tokens][n_q_heads] float32: the logarithm of the sum of the exponentials (-INF: nothing

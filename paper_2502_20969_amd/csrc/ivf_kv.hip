@@ -28,7 +28,7 @@ int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv
     if (cache->n_pages < 1 || cache->n_heads < 1 || cache->d < 1) return fail(IVF_EINVAL, "cache n_pages, n_heads and d must be at least 1");
     if (cache->page_stride % 8 != 0 || cache->token_stride % 8 != 0 || cache->head_stride % 8 != 0)
         return fail(IVF_EINVAL, "cache strides must be multiples of 8 elements");
-    for (int64_t stride : {cache->page_stride, cache->token_stride, cache->head_stride})
+    for (int64_t stride : {cache->page_stride, cache->token_stride})
         if (stride > (1 << 30) - 1 || stride < -(1 << 30)) return fail(IVF_ELIMIT, "cache stride of %lld elements", (long long)stride);
     const int cs = shift_of(cache->page);
     if (cs < 0) return fail(IVF_EINVAL, "cache page (%d) must be a power of two", cache->page);

@@ -120,3 +120,9 @@ def test_beam_steps():
     assert call(states=states, n_states=9) == -5
     for bad in (BeamStateArg(None, OK, 8, 8, 8), BeamStateArg(OK, None, 8, 8, 8), BeamStateArg(OK, OK, 0, 8, 8), BeamStateArg(OK, OK, 8, -8, 8), BeamStateArg(OK, OK, 8, 8, 4)):
         assert call(states=(BeamStateArg * 1)(bad), n_states=1) == -1
+
+
+@pytest.mark.parametrize("kw", [dict(page_stride=1 << 30), dict(token_stride=1 << 31), dict(n_pages=1 << 40)])
+def test_caches_beyond_the_limits(kw):
+    cache = _cache(**kw)
+    assert _append(cache=cache) == -5 and _attend(cache=cache) == -5

@@ -252,3 +252,32 @@ def test_in_a_graph(new):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 64), ("bf16", 128), ("f16", 256)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 17), (900, 0)])
+@pytest.mark.parametrize("new", [[1] * 9, [3, 1, 0, 2, 1, 1, 5, 1, 1], [40, 1, 1, 1, 60, 1, 1, 1, 1]])
+def test_long_prefixes_of_several_sequences(dtype, d, window, sinks, new):
+    """Prefixes that are read for their whole group at once, beside one without keys and a sequence in no group."""
+    own = [n + 13 * i for i, n in enumerate(new)]
+    _run(Problem(new, own, groups=[(4, 601), (2, 0), (2, 1500)], hkv=2, d=d, dtype=dtype, seed=d + window), 8, window, sinks)
+
+
+@pytest.mark.parametrize("page,own_page,prefix_page", [(1, 1, 1), (16, 1, 16), (64, 64, 8)])
+def test_long_prefixes_in_pages(page, own_page, prefix_page):
+    _run(Problem([1] * 40, [5 + i for i in range(40)], groups=[(30, 1000), (10, 999)], hkv=1, d=128, page=page, own_page=own_page,
+                 prefix_page=prefix_page, seed=page), 8)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_values_that_are_not_finite_count_where_they_are_seen(value):
+    """A prompt long enough for several wavefronts: tokens before the value keep theirs, others take it."""
+    pr = Problem([200], [330], hkv=1, d=128, page=16, seed=21)
+    key = 230
+    pr.v[pr.own_slots(0)[key], 0, 5] = value
+    step, cache = pr.step(P), pr.cache(P)
+    q = pr.rows(2)
+    got = P.ivf_attend(step, cache, q.cuda(), scale=pr.d ** -0.5).double().cpu().numpy()
+    sees = np.arange(130, 330) >= key
+    assert np.isfinite(got[~sees]).all() and np.isfinite(np.delete(got, 5, axis=2)).all()
+    assert (np.isnan(got[sees][:, :, 5]) if value != value else got[sees][:, :, 5] == value).all()

@@ -169,3 +169,15 @@ def test_in_a_graph():
         torch.cuda.synchronize()
         assert np.array_equal(got[2].cpu().numpy(), want[2]) and np.array_equal(got[1].cpu().numpy(), want[1])
         assert torch.equal(dst, src[got[1].view(-1).long()])
+
+
+def test_large_states():
+    """More than a prompt's workgroup moves beside the selection, in one launch with small ones."""
+    p, b, k = 3, 4, 5
+    states = [torch.randn(p * b, 9000), torch.randint(0, 1000, (p * b, 33), dtype=torch.int32)]
+    _run(_logits(p, b, 900, "f32", 31), _spread(p, b), k, states=states)
+
+
+@pytest.mark.parametrize("prompts,beams,k,vocab", [(1, 40, 64, 9000), (2, 5, 13, 120000), (300, 2, 2, 5000)])
+def test_joins_of_few_and_of_many(prompts, beams, k, vocab):
+    _run(_logits(prompts, beams, vocab, "bf16" if vocab < 10000 else "f32", 32 + k), _spread(prompts, beams), k)
