@@ -112,14 +112,14 @@ __device__ __forceinline__ float other_half(float x) { return __uint_as_float(xo
 // costs no precision, and the sums need not be scaled for every small rise.
 constexpr float kSlack = 8.f;
 
-// NARROW: the workgroup has one tile of 32 rows, its wavefronts take the tiles of keys in turn, each with LDS of its own.
-// Otherwise every wavefront has 32 rows of its own and all share the tiles.
-template <int D, bool NARROW>
+// NARROW: the workgroup has one tile of 32 rows, its NARROW wavefronts take the tiles of keys in turn, each with LDS of its own.
+// 0: every one of four wavefronts has 32 rows of its own and all share the tiles.
+template <int D, int NARROW>
 struct Shape {
     static constexpr int kChunks = D <= 64 ? 8 : D <= 128 ? 16 : 32;       // 16-byte chunks of a staged row
     static constexpr int kPitch = kChunks * 16;
     static constexpr int kKeys = NARROW || D > 128 ? 32 : 64;              // keys of a tile
-    static constexpr int kWaves = NARROW ? 2 : 4;
+    static constexpr int kWaves = NARROW ? NARROW : 4;
     static constexpr int kStages = 2;
     static constexpr int kAhead = kStages - 1;                             // tiles on their way while one is worked on
     static constexpr int kTileBytes = kKeys * kPitch * 2;                  // keys, then values
@@ -147,7 +147,7 @@ template <int CHUNKS> __device__ __forceinline__ int place_swap(int row) {
 
 // Registers: two workgroups a compute unit, but of heads of 256 one, whose sums and queries alone take 192 (eight wavefronts: a prompt
 // of 8000 tokens 890 us against 803)
-template <typename T, int D, bool NARROW>
+template <typename T, int D, int NARROW>
 __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128 ? 1 : 2)) void attend_kernel(AttendArgs a) {
     using S = Shape<D, NARROW>;
     using H = Half<T>;
@@ -726,6 +726,7 @@ struct AttendPlan {
     bool shared;                     // the prefix in a pass of its own
     bool narrow, wide;               // kernels that the own (or all) keys need
     bool prefix_narrow;
+    bool one_wave;                   // narrow workgroups of one wavefront
     int split_narrow, split_wide, split_prefix;
     int tiles_narrow, tiles_wide, tiles_prefix;      // workgroups along a unit's rows
     int parts, part_own, n_own;
@@ -733,7 +734,7 @@ struct AttendPlan {
 
 constexpr int kNarrowRows = 32, kWideRows = 128, kAllRows = 0x7FFFFFFF;
 
-static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv, int group, int window, int sinks) {
+static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv, int group, int d, int window, int sinks) {
     AttendPlan p{};
     const int64_t rows = (int64_t)sv.n_tokens * group;
     auto known = [](int hint, int64_t cap) { return hint > 0 ? std::min<int64_t>(hint, cap) : cap; };
@@ -776,6 +777,12 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
         p.split_prefix = p.prefix_narrow ? split_few(units, read_keys(pre)) : split(units, 512, read_keys(pre), 256);
         p.part_own = p.split_prefix;
     }
+    // A workgroup of one wavefront where many have little to do, or where two wavefronts' tiles leave no room for another workgroup:
+    // the start of one then hides behind the work of others (204 sequences of 1 to 5 tokens, a window of 10, 16 heads of 128: 58 us by
+    // two wavefronts, 44 by one; 180 of up to 114 keys, heads of 256: 73 and 51).  Else two share the start and the end (24 sequences
+    // of up to 60,000: 543 and 574)
+    const int64_t piece = std::max(keys / std::max(1, p.split_narrow), p.shared && p.prefix_narrow ? read_keys(pre) / p.split_prefix : 0);
+    p.one_wave = d > 64 && p.narrow && (int64_t)sv.n_seq * hkv * p.split_narrow >= 512 && (d > 128 || piece <= 256);
     p.parts = p.shared || p.n_own > 1 ? p.part_own + p.n_own : 0;
     return p;
 }
@@ -783,7 +790,7 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
 static size_t plan_bytes(const AttendPlan& p, int64_t rows, int d) { return (size_t)(rows * p.parts) * ((size_t)d * 4 + 8); }
 
 // One launch for one pass or two: units of the first and of the second.
-template <typename T, int D, bool NARROW>
+template <typename T, int D, int NARROW>
 static hipError_t launch_passes(AttendArgs a, int64_t units0, int64_t units1, hipStream_t s) {
     using S = Shape<D, NARROW>;
     auto blocks = [&](int64_t units, const AttendArgs::Pass& p) { return units * p.n_split * p.n_tile * a.hkv; };
@@ -810,11 +817,14 @@ static hipError_t launch_attend(AttendArgs a, const AttendPlan& p, hipStream_t s
     a.pass[0] = prefix;
     if (groups_wide || p.wide) {
         a.pass[1] = wide;
-        if ((e = launch_passes<T, D, false>(a, groups_wide, p.wide ? units : 0, s))) return e;
+        if ((e = launch_passes<T, D, 0>(a, groups_wide, p.wide ? units : 0, s))) return e;
     }
     if (groups_narrow || p.narrow) {
         a.pass[1] = narrow;
-        if ((e = launch_passes<T, D, true>(a, groups_narrow, p.narrow ? units : 0, s))) return e;
+        const int64_t n = p.narrow ? units : 0;
+        if constexpr (D > 64) e = p.one_wave ? launch_passes<T, D, 1>(a, groups_narrow, n, s) : launch_passes<T, D, 2>(a, groups_narrow, n, s);
+        else e = launch_passes<T, D, 2>(a, groups_narrow, n, s);
+        if (e) return e;
     }
     if (p.parts > 0) {
         hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 8192)), dim3(256), 0, s, a);
@@ -844,7 +854,7 @@ extern "C" int ivf_attend_workspace(const ivf_kv_step* step, const ivf_kv_cache*
     if (rc) return rc;
     if ((rc = check_heads(cache, n_q_heads, window, sinks))) return rc;
     if (!bytes) return fail(IVF_EINVAL, "bytes is NULL");
-    const AttendPlan p = plan_attend(step, sv, cache->n_heads, n_q_heads / cache->n_heads, window, sinks);
+    const AttendPlan p = plan_attend(step, sv, cache->n_heads, n_q_heads / cache->n_heads, cache->d, window, sinks);
     *bytes = plan_bytes(p, (int64_t)sv.n_tokens * n_q_heads, cache->d);
     return IVF_OK;
 }
@@ -861,7 +871,7 @@ extern "C" int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, co
     if (((uintptr_t)workspace & 15u) != 0) return fail(IVF_EINVAL, "workspace must be 16-byte aligned");
     a.q = *q; a.out = *out; a.lse = lse; a.scale_log2 = scale * 1.4426950408889634f;
     a.hq = n_q_heads; a.hkv = cache->n_heads; a.group = n_q_heads / cache->n_heads; a.window = window; a.sinks = sinks;
-    const AttendPlan p = plan_attend(step, a.step, a.hkv, a.group, window, sinks);
+    const AttendPlan p = plan_attend(step, a.step, a.hkv, a.group, cache->d, window, sinks);
     const int64_t rows = (int64_t)a.step.n_tokens * n_q_heads;
     const size_t need = plan_bytes(p, rows, cache->d);
     if (workspace_bytes < need || (need > 0 && !workspace))

@@ -281,3 +281,14 @@ def test_values_that_are_not_finite_count_where_they_are_seen(value):
     sees = np.arange(130, 330) >= key
     assert np.isfinite(got[~sees]).all() and np.isfinite(np.delete(got, 5, axis=2)).all()
     assert (np.isnan(got[sees][:, :, 5]) if value != value else got[sees][:, :, 5] == value).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 96), ("bf16", 128), ("f16", 256)])
+@pytest.mark.parametrize("window,sinks,groups", [(0, 0, []), (9, 4, [(300, 40)]), (0, 0, [(40, 0), (4, 600)])])
+def test_many_short_sequences(dtype, d, window, sinks, groups):
+    n = 520
+    _run(Problem([1 + i % 3 // 2 for i in range(n)], [2 + (i * 37) % 70 for i in range(n)], groups=groups, hkv=1, d=d, dtype=dtype, seed=17), 2, window, sinks)
+
+
+def test_many_long_pieces_of_wide_heads():
+    _run(Problem([1] * 64, [900 + i for i in range(64)], groups=[(16, 700)] * 4, hkv=8, d=256, page=64, seed=18), 8)
