@@ -708,8 +708,17 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int l
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-    const int64_t rows = (int64_t)a.step.n_tokens * a.hq;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + wave_id(); row < rows; row += (int64_t)gridDim.x * 4) join_row<T, D>(a, row, lane_id());
+    const int64_t rows = (int64_t)a.step.n_tokens * a.hq, stride = (int64_t)gridDim.x * 4, first = (int64_t)blockIdx.x * 4 + wave_id();
+    if (rows <= stride) {
+        if (first < rows) join_row<T, D>(a, first, lane_id());
+        return;
+    }
+    // several rows a wavefront, most of them complete already where there are prompts: asked for 64 at a time
+    for (int64_t row0 = first; row0 < rows; row0 += 64 * stride) {
+        const int64_t mine = row0 + lane_id() * stride;
+        const float m = mine < rows ? a.part_ml[mine * a.parts].x : NAN;
+        for (uint64_t left = __ballot(m == m); left; left &= left - 1) join_row<T, D>(a, row0 + __builtin_ctzll(left) * stride, lane_id());
+    }
 }
 
 static int check_heads(const ivf_kv_cache* cache, int n_q_heads, int window, int sinks) {
