@@ -40,7 +40,7 @@ struct AttendArgs {
     // one launch makes one pass or two, which read different keys
     struct Pass {
         int mode, part0, n_part;     // its range of partial sums
-        int n_split, n_tile;         // workgroups that share a row's keys; workgroups that share a unit's rows
+        int n_split, n_tile;         // workgroups that share a row's keys; that share a unit's rows (0: one per tile of each sequence)
         int rows_lo, rows_hi;        // units with more than rows_lo and at most rows_hi rows
     } pass[2];
     int first_blocks;                // workgroups of the first pass
@@ -160,8 +160,30 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
     const AttendArgs::Pass& pass = a.pass[second];
     if (second) at -= a.first_blocks;
     const int kvh = at % a.hkv; at /= a.hkv;
-    const int tile0 = pass.n_tile - 1 - at % pass.n_tile; at /= pass.n_tile;       // the rows that see most first
-    const int split = at % pass.n_split, unit = at / pass.n_split;
+    int tile0 = 0, split, unit;
+    if (pass.n_tile > 0) {
+        tile0 = pass.n_tile - 1 - at % pass.n_tile; at /= pass.n_tile;     // the rows that see most first
+        split = at % pass.n_split; unit = at / pass.n_split;
+    } else {
+        // the sequences' tiles one behind the other: which one this is, by looking at 64 sequences at a time
+        split = at % pass.n_split; at /= pass.n_split;
+        unit = -1;
+        for (int s = 0; s < a.step.n_seq && unit < 0; s += 64) {
+            const int i = min(s + lane, a.step.n_seq - 1);
+            const int n = s + lane < a.step.n_seq ? (max(0, token_of(a.step, i + 1) - token_of(a.step, i)) * G + S::kRows - 1) / S::kRows : 0;
+            int upto = n;
+            for (int w = 1; w < 64; w <<= 1) { const int x = __shfl_up(upto, w); upto += lane >= w ? x : 0; }
+            const uint64_t behind = __ballot(upto > at);
+            if (behind) {
+                const int l = __builtin_ctzll(behind);
+                unit = s + l;
+                tile0 = __builtin_amdgcn_readlane(upto, l) - 1 - at;
+            } else {
+                at -= __builtin_amdgcn_readlane(upto, 63);
+            }
+        }
+        if (unit < 0) return;
+    }
 
     // The unit: its tokens and keys.  Keys, positions, window and sinks are counted from the begin of what the pass reads: own
     // keys alone do not wait for the prefix's length
@@ -230,7 +252,8 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
     for (int u = 0; u < (NARROW ? 1 : S::kLoads); ++u)
         page_place[u] = (uint32_t)((u * S::kRowsPerLoad + lane / S::kChunks) * a.cache.token_bytes) + chunk_bytes(u);
 
-    for (int tile = tile0; tile * S::kRows < rows; tile += pass.n_tile) {
+    const int tile_step = pass.n_tile > 0 ? pass.n_tile : rows / S::kRows + 1;
+    for (int tile = tile0; tile * S::kRows < rows; tile += tile_step) {
         // rows of the workgroup and of this lane
         const int row_first = tile * S::kRows, row_last = min(rows, row_first + S::kRows) - 1;
         const int row = row_first + (NARROW ? 0 : wave * 32) + (lane & 31);
@@ -774,6 +797,9 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
     // (unknown: twice what sequences of equal lengths would need)
     const int64_t tile_rows = st->max_q > 0 || sv.n_seq == 1 ? most_q * group : std::min(rows, 2 * rows / sv.n_seq);
     p.tiles_wide = (int)std::max<int64_t>(1, (tile_rows + kWideRows - 1) / kWideRows);
+    // where most of these would find no rows, the sequences' tiles are counted out one behind the other instead (a prompt of 8000 tokens
+    // among 63 single ones: 126,000 workgroups that only end, 897 us; counted out 738.  Prompts of 361 to 1085 tokens: 67.7 and 68.9)
+    if (sv.n_seq * (int64_t)p.tiles_wide > 2 * (rows / kWideRows + sv.n_seq)) p.tiles_wide = 0;
     if (p.narrow) p.split_narrow = split_few((int64_t)sv.n_seq * hkv, keys);
     if (p.wide) p.split_wide = split_many(hkv * ((rows + kWideRows - 1) / kWideRows + sv.n_seq / 2), keys);
     p.n_own = std::max(p.split_narrow, p.split_wide);
@@ -802,7 +828,8 @@ static size_t plan_bytes(const AttendPlan& p, int64_t rows, int d) { return (siz
 template <typename T, int D, int NARROW>
 static hipError_t launch_passes(AttendArgs a, int64_t units0, int64_t units1, hipStream_t s) {
     using S = Shape<D, NARROW>;
-    auto blocks = [&](int64_t units, const AttendArgs::Pass& p) { return units * p.n_split * p.n_tile * a.hkv; };
+    const int64_t packed = (int64_t)a.step.n_tokens * a.group / S::kRows + a.step.n_seq;         // at least the sequences' tiles
+    auto blocks = [&](int64_t units, const AttendArgs::Pass& p) { return (p.n_tile > 0 ? units * p.n_tile : units ? packed : 0) * p.n_split * a.hkv; };
     const int64_t first = blocks(units0, a.pass[0]), grid = first + blocks(units1, a.pass[1]);
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
     static const hipError_t allowed = hipFuncSetAttribute((const void*)attend_kernel<T, D, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);

@@ -292,3 +292,10 @@ def test_many_short_sequences(dtype, d, window, sinks, groups):
 
 def test_many_long_pieces_of_wide_heads():
     _run(Problem([1] * 64, [900 + i for i in range(64)], groups=[(16, 700)] * 4, hkv=8, d=256, page=64, seed=18), 8)
+
+
+@pytest.mark.parametrize("hints", [dict(), dict(max_q=260, max_len=400)])
+def test_prompts_among_single_tokens(hints):
+    """Sequences of very different numbers of tokens, some with none, more of them than a wavefront has lanes."""
+    new = [(260 if i % 50 == 3 else 129 if i % 70 == 66 else i % 3) for i in range(150)]
+    _run(Problem(new, [n + i for i, n in enumerate(new)], groups=[(60, 33)], hkv=1, d=64, dtype="f16", seed=19), 2, hints=hints)
