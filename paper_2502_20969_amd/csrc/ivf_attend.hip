@@ -791,8 +791,9 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
     // few rows: pieces of 1024 keys and more for several workgroups a place on the chip (two fit a compute unit), smaller ones
     // only while places are free
     auto split_few = [&](int64_t units, int64_t keys) { return std::max(split(units, 4096, keys, 1024), split(units, 512, keys, 128)); };
-    // many rows: only as far as places are free, since every piece more is 2 x 4 d bytes a row written and read
-    auto split_many = [](int64_t units, int64_t keys) { return (int)std::max<int64_t>(1, std::min<int64_t>({512 / units, keys / 1024, 64})); };
+    // many rows: only as far as places are free, since every piece more is 2 x 4 d bytes a row written and read, and in pieces that
+    // outweigh the joining (6 prompts, 1840 keys, 2 key heads: one piece 50 us, two 36; 18 prompts, 1061 keys: 36 and 42)
+    auto split_many = [](int64_t units, int64_t keys) { return (int)std::max<int64_t>(1, std::min<int64_t>({512 / units, keys / 768, 64})); };
     p.tiles_narrow = 1;
     // (unknown: twice what sequences of equal lengths would need)
     const int64_t tile_rows = st->max_q > 0 || sv.n_seq == 1 ? most_q * group : std::min(rows, 2 * rows / sv.n_seq);
