@@ -16,6 +16,12 @@
 // Keys and values go from memory to LDS directly, without passing registers, 16 bytes a lane; the chunks of a row are
 // permuted on the way so that both kinds of LDS reads are spread over the banks.  The tables' entries are fetched into
 // LDS in the same way ahead of the tiles they name.
+//
+// What bounds it.  Few rows: memory, if the keys are long (24 sequences of up to 60,000 keys, 8 key heads of 128, bf16: 531 us, 5.6
+// TB/s), else the chain of lengths, table, keys and joins (one token over 700 keys: 8.9 us and 3 for the joining).  Many rows: LDS.  Each
+// wavefront reads a tile's keys and values once for its 32 rows, two bytes per 32 multiplications: a prompt of 16,000 tokens, 32 query
+// and 8 key heads of 128, 2.05 ms, 1000 TFLOP/s, at about 64 bytes a clock and compute unit.  64 rows a wavefront would halve the
+// reads, but their sums and queries do not fit beside a second wavefront's.
 #include "ivf_answer.h"
 #include "ivf_device.h"
 #include <algorithm>
@@ -674,7 +680,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
     }
 }
 
-// Joins a row's partial sums: one wavefront per token and query head.  Lane i weighs part i; then D / 4 lanes take a part's
+// Joins a row's partial sums: one wavefront per token and query head, bound by latency (1536 rows of 34 parts of 128: 7 us).  Lane i weighs part i; then D / 4 lanes take a part's
 // elements, and several parts at a time are on their way.
 template <typename T, int D>
 __device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int lane) {
@@ -789,7 +795,7 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
         return (int)std::max<int64_t>(1, std::min<int64_t>({(want + units - 1) / units, most, 64}));
     };
     // few rows: pieces of 1024 keys and more for several workgroups a place on the chip (two fit a compute unit), smaller ones
-    // only while places are free
+    // only while places are free (64 windows of 4096: pieces of 512 keys 214 us, of 1024 204; one token over 700 keys needs the small ones)
     auto split_few = [&](int64_t units, int64_t keys) { return std::max(split(units, 4096, keys, 1024), split(units, 512, keys, 128)); };
     // many rows: only as far as places are free, since every piece more is 2 x 4 d bytes a row written and read, and in pieces that
     // outweigh the joining (6 prompts, 1840 keys, 2 key heads: one piece 50 us, two 36; 18 prompts, 1061 keys: 36 and 42)

@@ -100,7 +100,9 @@ __device__ __forceinline__ void rotate(uint4& a, uint4& b, const float (&c)[8], 
 
 // One workgroup per new token.  A unit is sixteen elements of a head: in the rotated part eight pairs (two chunks of
 // eight that lie rot / 2 apart, or sixteen in a row), behind it sixteen in a row.  A thread keeps its unit's cosines and
-// sines and takes that unit of one head after the other.
+// sines and takes that unit of one head after the other.  Rotated in 32 bits, rounded once.
+// Bound by memory: 17,000 tokens of 64 query and 8 key heads of 128 in 131 us, 5.4 TB/s read and written.  One token per
+// sequence is a chain of loads (sequence, place, table, cosines): 3.8 us for one, 6.6 for 200.
 template <typename T, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     const int t = blockIdx.x, tid = threadIdx.x;
