@@ -489,8 +489,8 @@ int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_
  * Attention of the new tokens over the cache: out = softmax(scale * q . k) v over the keys that a token sees, in
  * 32 bits, rounded once.  A token at position p sees key j when j <= p and, with window > 0, p - j < window or j <
  * sinks.  A token that sees nothing gets zeros.  The keys of a long prefix are read once for all tokens of its group.
- *   q, out     n_tokens x n_q_heads x d, of the cache's type; query head h reads key head
- *              h / (n_q_heads / cache->n_heads)
+ *   q, out     n_tokens x n_q_heads x d, of the cache's type, which do not overlap; query head h reads key
+ *              head h / (n_q_heads / cache->n_heads)
  *   lse        [n_tokens][n_q_heads] float32: the logarithm of the sum of the exponentials (-INF: nothing
  *              seen), or NULL
  *   scale      > 0

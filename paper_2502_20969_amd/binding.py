@@ -569,13 +569,23 @@ class KvStep:
         self.ref = C.byref(a)
 
 
+def _new(stream, shape, dtype, kept=True):
+    """A tensor that the call's kernels on `stream` may write at once (memory that torch last gave to the current stream may
+    still be used there); kept: it is for the caller, whose current stream may read it later."""
+    t = _torch()
+    if stream is None:
+        return t.empty(shape, dtype=dtype, device="cuda")
+    now = t.cuda.current_stream()
+    with t.cuda.stream(stream):
+        x = t.empty(shape, dtype=dtype, device="cuda")
+    if kept:
+        x.record_stream(now)
+    return x
+
+
 def _workspace(n, stream):
     """n bytes that are free again, in stream order, once the call's kernels have run."""
-    t = _torch()
-    w = t.empty(n, dtype=t.uint8, device="cuda")
-    if stream is not None:
-        w.record_stream(stream)
-    return w
+    return _new(stream, n, _torch().uint8, False)
 
 
 _raw_stream = None
@@ -601,9 +611,7 @@ def ivf_kv_append(step, cache, k, v, rotary=None, positions=None, q=None, q_out=
     hq = n_pos = rot = 0
     if q is not None:
         if q_out is None:
-            q_out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
-            if stream is not None:
-                q_out.record_stream(stream)
+            q_out = _new(stream, q.shape, q.dtype)
         hq = q.shape[1]
         qr, qo = _rows(q, n, hq, cache, "q"), _rows(q_out, n, hq, cache, "q_out")
     elif q_out is not None:
@@ -627,9 +635,7 @@ def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0
     at least ivf_attend_workspace() bytes, default one for this call."""
     n = step.n_tokens
     if out is None:
-        out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
-        if stream is not None:
-            out.record_stream(stream)
+        out = _new(stream, q.shape, q.dtype)
     hq = q.shape[1]
     qr, qo = _rows(q, n, hq, cache, "q"), _rows(out, n, hq, cache, "out")
     lp = wp = None
@@ -709,15 +715,12 @@ def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), 
     args = (BeamStateArg * len(states))(*[_state(src, dst, p * b, p * n) for src, dst in states]) if states else None
     need = ivf_beam_workspace(p, b, vocab, n)
     # the scores, parents and tokens are one allocation
-    out = t.empty((3, p, n), dtype=t.int32, device="cuda")
+    out = _new(stream, (3, p, n), t.int32)
     score, parent, token = out.unbind(0)
     score = score.view(t.float32)
-    fin = t.empty((p, n), dtype=t.bool, device="cuda")
+    fin = _new(stream, (p, n), t.bool)
     if workspace is None:
         workspace = _workspace(need, stream)
-    if stream is not None:
-        out.record_stream(stream)
-        fin.record_stream(stream)
     at = out.data_ptr()
     status = load().ivf_beam_step(logits.data_ptr(), stride, _code(logits.dtype), p, b, vocab, scores.data_ptr(), dp, eos, n,
                                   at, at + 4 * p * n, at + 8 * p * n, fin.data_ptr(), args, len(states),

@@ -25,6 +25,7 @@
 #include "ivf_answer.h"
 #include "ivf_device.h"
 #include <algorithm>
+#include <atomic>
 #include <math.h>
 
 namespace ivf {
@@ -839,8 +840,13 @@ static hipError_t launch_passes(AttendArgs a, int64_t units0, int64_t units1, hi
     auto blocks = [&](int64_t units, const AttendArgs::Pass& p) { return (p.n_tile > 0 ? units * p.n_tile : units ? packed : 0) * p.n_split * a.hkv; };
     const int64_t first = blocks(units0, a.pass[0]), grid = first + blocks(units1, a.pass[1]);
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-    static const hipError_t allowed = hipFuncSetAttribute((const void*)attend_kernel<T, D, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-    if (allowed != hipSuccess) return allowed;
+    static std::atomic<uint64_t> allowed{0};            // the devices that know of the kernel's LDS
+    int device;
+    if (hipError_t e = hipGetDevice(&device)) return e;
+    if (const uint64_t bit = 1ull << (device & 63); !(allowed.load() & bit)) {
+        if (hipError_t e = hipFuncSetAttribute((const void*)attend_kernel<T, D, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds)) return e;
+        allowed |= bit;
+    }
     a.first_blocks = (int)first;
     hipLaunchKernelGGL((attend_kernel<T, D, NARROW>), dim3((unsigned)grid), dim3(S::kWaves * 64), S::kLds, s, a);
     return hipGetLastError();

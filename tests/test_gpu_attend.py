@@ -299,3 +299,24 @@ def test_prompts_among_single_tokens(hints):
     """Sequences of very different numbers of tokens, some with none, more of them than a wavefront has lanes."""
     new = [(260 if i % 50 == 3 else 129 if i % 70 == 66 else i % 3) for i in range(150)]
     _run(Problem(new, [n + i for i, n in enumerate(new)], groups=[(60, 33)], hkv=1, d=64, dtype="f16", seed=19), 2, hints=hints)
+
+
+def test_new_tensors_do_not_meet_pending_work():
+    """The calls' own tensors on another stream are not memory that the current stream still writes."""
+    pr = Problem([1] * 8, [40] * 8, hkv=2, d=64, dtype="f16", seed=20)
+    q = pr.rows(8)
+    want, _, tol = pr.attend(q, 0.125)
+    step, cache, qd, other = pr.step(P), pr.cache(P), q.cuda(), torch.cuda.Stream()
+    logits, scores = torch.randn(4, 2, 500).cuda(), torch.zeros(4, 2).cuda()
+    plain = P.ivf_beam_step(logits, scores)
+    torch.cuda.synchronize()
+    blocks = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (qd.nbytes, 96, 8, 4096, 16384)]
+    torch.cuda._sleep(100_000_000)
+    for b in blocks:
+        b.fill_(123)
+    del blocks, b
+    out = P.ivf_attend(step, cache, qd, scale=0.125, stream=other)
+    beams = P.ivf_beam_step(logits, scores, stream=other)
+    torch.cuda.synchronize()
+    assert (abs(out.double().cpu().numpy() - want) <= tol).all()
+    assert all(torch.equal(x, y) for x, y in zip(beams, plain))
