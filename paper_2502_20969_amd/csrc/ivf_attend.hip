@@ -641,7 +641,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
             float mm = -INFINITY;
 #pragma unroll
             for (int w = 0; w < S::kWaves; ++w) mm = fmaxf(mm, sm[w * 32 + (lane & 31)].x);
-            const float f = m == -INFINITY ? (m != m ? m : 0.f) : __builtin_amdgcn_exp2f(m - mm);
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm);
             if (mine) {
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
@@ -698,7 +698,10 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int l
         float top = p.x;
         for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
         const float m2 = fmaxf(m, top);
-        if (m2 == -INFINITY) continue;
+        if (m2 == -INFINITY) {                                       // nothing seen, or no score is a number: then the sums are NaN
+            sum += group_sum<64>(p.y);
+            continue;
+        }
         const float keep = __builtin_amdgcn_exp2f(m - m2);
         const float f = p.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(p.x - m2);
         m = m2;

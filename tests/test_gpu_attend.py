@@ -320,3 +320,40 @@ def test_new_tensors_do_not_meet_pending_work():
     torch.cuda.synchronize()
     assert (abs(out.double().cpu().numpy() - want) <= tol).all()
     assert all(torch.equal(x, y) for x, y in zip(beams, plain))
+
+
+@pytest.mark.parametrize("new,own,groups", [([2], [30], []), ([1], [3000], []), ([1] * 3, [700, 5, 90], [(2, 40)]), ([150], [150], []), ([130], [5000], []),
+                                            ([1] * 4, [9, 300, 1, 40], [(4, 700)]), ([40] * 3, [40, 90, 41], [(2, 1500)]), ([200, 1, 1], [200, 3000, 900], [])])
+@pytest.mark.parametrize("dtype,d", [("f16", 64), ("bf16", 128), ("bf16", 256)])
+def test_queries_that_are_not_numbers(new, own, groups, dtype, d):
+    """Not a number for the rows whose query is none, in one piece or many; the other rows keep theirs."""
+    pr = Problem(new, own, groups=groups, hkv=2, d=d, dtype=dtype, seed=22)
+    q = pr.rows(4) * 2
+    want, wl, tol = pr.attend(q, pr.d ** -0.5)
+    bad = np.zeros((pr.tokens, 4), bool)
+    bad[0, 1] = bad[-1, 3] = bad[pr.tokens // 2, 0] = True
+    q[torch.from_numpy(bad)] = float("nan")
+    q[0, 1] = 1.0
+    q[0, 1, 7] = float("nan")                               # one element is enough
+    step, cache = pr.step(P), pr.cache(P)
+    lse = torch.empty(pr.tokens, 4).cuda()
+    got = P.ivf_attend(step, cache, q.cuda(), lse=lse).double().cpu().numpy()
+    lse = lse.cpu().numpy()
+    assert np.isnan(got[bad]).all() and np.isnan(lse[bad]).all()
+    assert (np.abs(got - want) <= tol)[~bad].all()
+    np.testing.assert_allclose(lse[~bad], wl[~bad], rtol=2e-6, atol=1e-4)
+
+
+@pytest.mark.parametrize("new,own,key", [(1, 40, 39), (1, 3000, 2100), (70, 200, 150), (130, 5000, 4700)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_nothing_is_finite_where_a_key_that_is_not_finite_is_seen(new, own, key, value):
+    """All elements of a key that is not finite: scores of both signs of infinity, or NaN, and so NaN in every element."""
+    pr = Problem([new], [own], hkv=1, d=64, dtype="f16", seed=23)
+    q = pr.rows(2) * 2
+    want, _, tol = pr.attend(q, pr.d ** -0.5)
+    cache = pr.cache(P)
+    cache.k.view(-1, 1, 64)[int(pr.own_slots(0)[key])] = value
+    got = P.ivf_attend(pr.step(P), cache, q.cuda()).double().cpu().numpy()
+    sees = np.arange(own - new, own) >= key
+    assert np.isnan(got[sees]).all()
+    assert (np.abs(got - want) <= tol)[~sees].all()
