@@ -224,6 +224,8 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
         }
         return plen + own_len(a.step, lo) - (token_of(a.step, lo + 1) - t);
     };
+    // the window's first key, of a position that may be below 0
+    auto first_of = [&](int p) { return max(0, max(p, 0) - (a.window - 1)); };
 
     unsigned char* stage = s_mem + (NARROW ? wave * S::kStages * S::kTileBytes : 0);
     const uint32_t stage_at = __builtin_amdgcn_readfirstlane(lds_address(stage));
@@ -268,7 +270,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
         const int tok = t0 + (mine ? row : rows - 1) / G, head = kvh * G + (mine ? row : rows - 1) % G;
         const int pos = mine ? position(tok) : -1;
         const int lim = min(pos, ke - 1);                                  // sees keys up to lim that are at or above low, or sinks
-        const int low = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+        const int low = a.window > 0 ? first_of(pos) : 0;
         // over the workgroup's rows (positions rise inside a sequence; over a group, all rows are looked at)
         int most = -1, least = 0x7FFFFFFF;
         if (by_group) {
@@ -289,14 +291,14 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
         const int n_end = max(0, end + S::kKeys - 1) / S::kKeys;
         int n_low = 0, n_sink = 0;
         if (a.window > 0) {
-            n_low = min(n_end, max(0, least - a.window + 1) / S::kKeys);
+            n_low = min(n_end, first_of(least) / S::kKeys);
             n_sink = min(n_low, sinks > 0 ? (min(sinks, end) + S::kKeys - 1) / S::kKeys : 0);
         }
         const int seen = n_sink + n_end - n_low;
         const int per = (seen + pass.n_split - 1) / pass.n_split;
         const int v0 = min(seen, split * per), v1 = min(seen, v0 + per);
         // those whose keys all rows see come first: [inner0, inner1) of them
-        const int all_low = a.window > 0 ? max(0, most - a.window + 1) : 0;
+        const int all_low = a.window > 0 ? first_of(most) : 0;
         const int inner_to = (min(least, ke - 1) + 1) / S::kKeys, inner_from = (all_low + S::kKeys - 1) / S::kKeys;
         const int inner0 = min(v1, max(v0, n_sink + max(inner_from - n_low, 0)));
         const int inner1 = min(v1, max(inner0, n_sink + inner_to - n_low)), inner = inner1 - inner0;

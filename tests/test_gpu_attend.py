@@ -357,3 +357,15 @@ def test_nothing_is_finite_where_a_key_that_is_not_finite_is_seen(new, own, key,
     sees = np.arange(own - new, own) >= key
     assert np.isnan(got[sees]).all()
     assert (np.abs(got - want) <= tol)[~sees].all()
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 40, 2 ** 30])
+@pytest.mark.parametrize("sinks", [0, 1, 2 ** 31 - 1])
+def test_windows_beyond_all_keys_where_rows_see_nothing(window, sinks):
+    """Tokens at positions below zero beside others that see keys, under windows that reach beyond every key."""
+    pr = Problem([3, 40, 2, 1, 70], [3, 40, 2, 5, 70], hkv=1, d=64, seed=6)
+    pr.own = [1, 10, 0, 5, 33]
+    _run(pr, 2, window, sinks)
+    pr = Problem([3, 4, 40], [3, 4, 40], groups=[(2, 600)], hkv=1, d=64, seed=7)
+    pr.own = [1, 2, 9]
+    _run(pr, 2, window, sinks)
