@@ -438,7 +438,8 @@ int ivf_schedule(ivf_index* index, const float* q, int32_t nq, int32_t micro, in
  *             caller knows (0: unknown).  They size the launch: lengths beyond them are still computed
  *             right, but slower
  * Key j of a sequence is key j of its prefix, or own key j - prefix_len; new token i has position
- * prefix_len + len - (new tokens) + i.  Entries outside the cache and lengths outside the tables are not
+ * prefix_len + len - (new tokens) + i.  Of a prefix, and of a sequence's own keys, at most the first 2^30 - 1024
+ * count.  Entries outside the cache and lengths outside the tables are not
  * followed out of bounds: such keys are never written, and when read hold what some other slot holds.
  */
 typedef struct ivf_kv_cache {

@@ -17,7 +17,7 @@ struct CacheView {
 struct StepView {
     const int32_t *q_off, *len, *table, *group_off, *prefix_len, *prefix_table;
     int64_t table_stride, prefix_stride;
-    int64_t own_cap, prefix_cap;         // keys that a row of the tables can name, at most INT32_MAX
+    int64_t own_cap, prefix_cap;         // keys that a row of the tables can name, at most 2^30 - 1024
     int64_t own_entries, prefix_entries; // entries that lie in the cache
     int n_seq, n_tokens, n_groups, shift, prefix_shift;
     int own_last, prefix_last;           // the last of them

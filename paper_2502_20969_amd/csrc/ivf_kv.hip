@@ -49,8 +49,8 @@ int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv
             return fail(IVF_EINVAL, "step prefix_page (%d) must be a power of two of at most the cache's (%d)", step->prefix_page, cache->page);
     }
     const int64_t slots = cache->n_pages << cs;
-    // a prefix and the own keys together stay below 2^31
-    auto cap = [](int64_t stride, int shift) { return std::min<int64_t>(stride, (int64_t)1 << 30 >> shift) << shift; };
+    // a prefix and the own keys together, and the tile behind them, stay below 2^31
+    auto cap = [](int64_t stride, int shift) { return std::min<int64_t>(std::min<int64_t>(stride, (int64_t)1 << 30 >> shift) << shift, ((int64_t)1 << 30) - 1024); };
     *cv = CacheView{cache->k, cache->v, cache->page_stride, cache->token_stride, cache->head_stride, slots, cs,
                     (int)(cache->page_stride * 2), (int)(cache->token_stride * 2)};
     *sv = StepView{step->q_off, step->len, step->table, step->group_off, step->prefix_len, step->prefix_table,

@@ -369,3 +369,17 @@ def test_windows_beyond_all_keys_where_rows_see_nothing(window, sinks):
     pr = Problem([3, 4, 40], [3, 4, 40], groups=[(2, 600)], hkv=1, d=64, seed=7)
     pr.own = [1, 2, 9]
     _run(pr, 2, window, sinks)
+
+
+def test_as_many_keys_as_positions_count():
+    """A prefix and own keys that together pass the largest position: of both the first keys count, and a window finds the last."""
+    page, d = 1 << 14, 64
+    k = torch.zeros(1, page, 1, d, dtype=torch.bfloat16, device="cuda")
+    v = torch.ones_like(k)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32).cuda()
+    table = torch.zeros(1, 1 << 16, dtype=torch.int32, device="cuda")
+    step = P.KvStep(i32([0, 2]), i32([2 ** 31 - 1]), table, page=page, n_tokens=2, group_off=i32([0, 1]), prefix_lens=i32([2 ** 31 - 1]), prefix_table=table)
+    lse = torch.empty(2, 1, device="cuda")
+    out = P.ivf_attend(step, P.KvCache(k, v), torch.zeros(2, 1, d, dtype=torch.bfloat16, device="cuda"), lse=lse, window=100, sinks=3)
+    assert bool((out == 1).all())
+    np.testing.assert_allclose(lse.cpu().numpy(), np.log(103.0), rtol=1e-6)
