@@ -32,6 +32,7 @@ namespace ivf {
 using namespace dev;
 
 enum { kConcat, kOwn, kPrefix };     // keys of a pass: prefix and own, own only, prefix only
+constexpr int kNarrowRows = 32, kWideRows = 128, kAllRows = 0x7FFFFFFF;
 
 struct AttendArgs {
     CacheView cache;
@@ -40,10 +41,16 @@ struct AttendArgs {
     float* lse;
     float scale_log2;                // scale * log2(e)
     int hq, hkv, group, window, sinks;       // group: query heads per key head
-    // partial sums [token][query head][parts]: O [d] unnormalised, and (m, l); m NaN: the row's result is complete
+    // partial sums [token][query head][parts]: O [d] unnormalised, and (m, l); m of the first own one NaN: the row's result is
+    // complete, or its own sums are among the few
     float* part_o;
     float2* part_ml;
-    int parts;                       // 0: one pass over all keys, no partial sums
+    int parts, part_own;             // 0: no partial sums; those of the prefix, which come first
+    // where sequences of few and of many rows meet, the own sums of the few's [sequence][few_tokens][query head][few_parts]: their keys
+    // may be cut into many pieces, and the many rows of the others need no room for as many
+    float* few_o;
+    float2* few_ml;
+    int few_tokens, few_parts;       // 0: all are among the others
     // one launch makes one pass or two, which read different keys
     struct Pass {
         int mode, part0, n_part;     // its range of partial sums
@@ -600,13 +607,19 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
 
         // what is left to do with the sums
         const bool last = pass.mode == kConcat && pass.n_split == 1;             // they are complete
+        const bool few = NARROW && !by_group && a.few_tokens > 0;
+        auto piece = [&](int t, int h) {                                   // its place among the partial sums
+            return few ? (((int64_t)unit * a.few_tokens + (t - t0)) * a.hq + h) * a.few_parts + split : ((int64_t)t * a.hq + h) * a.parts + pass.part0 + split;
+        };
         auto finish = [&](int t, int h, float mm, float ll) {              // by one lane per row
             if (a.lse && last) a.lse[(int64_t)t * a.hq + h] = ll > 0.f || ll != ll ? (mm + __builtin_amdgcn_logf(ll) - H::kLift) * 0.6931471805599453f : -INFINITY;
+            if (few) a.few_ml[piece(t, h)] = make_float2(mm, ll);
             if (a.parts == 0) return;
             float2* ml = a.part_ml + ((int64_t)t * a.hq + h) * a.parts;
-            ml[pass.part0 + split] = make_float2(last ? NAN : mm, ll);
+            if (!few) ml[pass.part0 + split] = make_float2(last ? NAN : mm, ll);
+            else if (split == 0) ml[pass.part0].x = NAN;
             if (split == 0) {
-                for (int i = pass.n_split; i < pass.n_part; ++i) ml[pass.part0 + i] = make_float2(-INFINITY, 0.f);
+                for (int i = pass.n_split; i < pass.n_part && !few; ++i) ml[pass.part0 + i] = make_float2(-INFINITY, 0.f);
                 if (pass.mode == kOwn && before == 0)                           // no prefix pass comes by here
                     for (int i = 0; i < pass.part0; ++i) ml[i] = make_float2(-INFINITY, 0.f);
             }
@@ -616,7 +629,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
                 if (half == 0) finish(tok, head, m, l);
                 const float f = last ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f;
                 T* out = (T*)a.out.data + tok * a.out.token_stride + head * a.out.head_stride;
-                float* part = last ? nullptr : a.part_o + (((int64_t)tok * a.hq + head) * a.parts + pass.part0 + split) * D;
+                float* part = last ? nullptr : a.part_o + piece(tok, head) * D;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -675,7 +688,7 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
                               __builtin_bit_cast(short, (T)(y.z * g1)), __builtin_bit_cast(short, (T)(y.w * g1))};
                     *(s4_t*)((T*)a.out.data + t * a.out.token_stride + h * a.out.head_stride + d) = z;
                 } else if (v1 > v0) {
-                    *(float4*)(a.part_o + (((int64_t)t * a.hq + h) * a.parts + pass.part0 + split) * D + d) = y;
+                    *(float4*)((few ? a.few_o : a.part_o) + piece(t, h) * D + d) = y;
                 }
             }
             __syncthreads();
@@ -684,18 +697,19 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
 }
 
 // Joins a row's partial sums: one wavefront per token and query head, bound by latency (1536 rows of 34 parts of 128: 7 us).  Lane i weighs part i; then D / 4 lanes take a part's
-// elements, and several parts at a time are on their way.
-template <typename T, int D>
-__device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int lane) {
+// elements, and several parts at a time are on their way.  FEW: the own ones are those of place `few`.
+template <typename T, int D, bool FEW>
+__device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int64_t few, int lane) {
     constexpr int kLanes = D / 4, kAtOnce = 64 / kLanes;             // lanes of a part; parts of one load
     constexpr int kUnroll = 4;
-    const float2* ml = a.part_ml + row * a.parts;
-    const float* po = a.part_o + row * a.parts * D;
+    const int parts = FEW ? a.part_own + a.few_parts : a.parts;
+    auto ml = [&](int i) { return FEW && i >= a.part_own ? a.few_ml[few * a.few_parts + i - a.part_own] : a.part_ml[row * a.parts + i]; };
+    auto po = [&](int i) { return FEW && i >= a.part_own ? a.few_o + (few * a.few_parts + i - a.part_own) * D : a.part_o + (row * a.parts + i) * D; };
     float m = -INFINITY, sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     const int group = min(lane / kLanes, kAtOnce - 1), d = lane % kLanes * 4;
-    for (int p0 = 0; p0 < a.parts; p0 += 64) {                       // 64 parts at a time
-        const float2 p = p0 + lane < a.parts ? ml[p0 + lane] : make_float2(-INFINITY, 0.f);
+    for (int p0 = 0; p0 < parts; p0 += 64) {                         // 64 parts at a time
+        const float2 p = p0 + lane < parts ? ml(p0 + lane) : make_float2(-INFINITY, 0.f);
         if (__ballot(p.x != p.x)) return;                            // complete already
         float top = p.x;
         for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
@@ -709,7 +723,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int l
         m = m2;
         sum = sum * keep + group_sum<64>(p.y * f);
         o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
-        const int n = min(64, a.parts - p0);
+        const int n = min(64, parts - p0);
         for (int i0 = 0; i0 < n; i0 += kAtOnce * kUnroll) {
             float4 y[kUnroll];
             float w[kUnroll];
@@ -718,7 +732,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int l
                 const int i = i0 + u * kAtOnce + group;
                 const float weight = __shfl(f, i & 63), at = __shfl(p.x, i & 63);      // by all lanes
                 const bool has = i < n && at > -INFINITY && lane < kLanes * kAtOnce;
-                y[u] = has ? *(const float4*)(po + (int64_t)(p0 + i) * D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                y[u] = has ? *(const float4*)(po(p0 + i) + d) : make_float4(0.f, 0.f, 0.f, 0.f);
                 w[u] = has ? weight : 0.f;
             }
 #pragma unroll
@@ -741,18 +755,35 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, int64_t row, int l
         a.lse[row] = sum > 0.f || sum != sum ? (m + __builtin_amdgcn_logf(sum) - Half<T>::kLift) * 0.6931471805599453f : -INFINITY;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-    const int64_t rows = (int64_t)a.step.n_tokens * a.hq, stride = (int64_t)gridDim.x * 4, first = (int64_t)blockIdx.x * 4 + wave_id();
+    const int lane = lane_id();
+    const int64_t rows = !FEW || a.parts > 0 ? (int64_t)a.step.n_tokens * a.hq : 0, stride = (int64_t)gridDim.x * 4, first = (int64_t)blockIdx.x * 4 + wave_id();
     if (rows <= stride) {
-        if (first < rows) join_row<T, D>(a, first, lane_id());
-        return;
+        if (first < rows) join_row<T, D, false>(a, first, 0, lane);
+    } else {
+        // several rows a wavefront, most of them complete already where there are prompts: asked for 64 at a time
+        for (int64_t row0 = first; row0 < rows; row0 += 64 * stride) {
+            const int64_t mine = row0 + lane * stride;
+            const float m = mine < rows ? a.part_ml[mine * a.parts + a.part_own].x : NAN;
+            for (uint64_t left = __ballot(m == m); left; left &= left - 1) join_row<T, D, false>(a, row0 + __builtin_ctzll(left) * stride, 0, lane);
+        }
     }
-    // several rows a wavefront, most of them complete already where there are prompts: asked for 64 at a time
-    for (int64_t row0 = first; row0 < rows; row0 += 64 * stride) {
-        const int64_t mine = row0 + lane_id() * stride;
-        const float m = mine < rows ? a.part_ml[mine * a.parts].x : NAN;
-        for (uint64_t left = __ballot(m == m); left; left &= left - 1) join_row<T, D>(a, row0 + __builtin_ctzll(left) * stride, lane_id());
+    if (!FEW) return;
+    // the sequences of few rows: of their places, those that hold a token
+    const int64_t few = (int64_t)a.step.n_seq * a.few_tokens * a.hq;
+    for (int64_t at0 = first; at0 < few; at0 += 64 * stride) {
+        const int64_t mine = at0 + lane * stride;
+        int64_t row = -1;
+        if (mine < few) {
+            const int64_t place = mine / a.hq;
+            const int s = (int)(place / a.few_tokens), i = (int)(place % a.few_tokens), t0 = token_of(a.step, s), n = token_of(a.step, s + 1) - t0;
+            if (i < n && n * a.group <= kNarrowRows) row = (int64_t)(t0 + i) * a.hq + mine % a.hq;
+        }
+        for (uint64_t left = __ballot(row >= 0); left; left &= left - 1) {
+            const int l = __builtin_ctzll(left);
+            join_row<T, D, true>(a, __shfl(row, l), at0 + l * stride, lane);
+        }
     }
 }
 
@@ -773,17 +804,16 @@ struct AttendPlan {
     bool one_wave;                   // narrow workgroups of one wavefront
     int split_narrow, split_wide, split_prefix;
     int tiles_narrow, tiles_wide, tiles_prefix;      // workgroups along a unit's rows
-    int parts, part_own, n_own;
+    int parts, part_own, n_own;      // partial sums of a row, of them the prefix's and its own
+    int few_tokens;                  // those of sequences of few rows apart: so many tokens each
 };
-
-constexpr int kNarrowRows = 32, kWideRows = 128, kAllRows = 0x7FFFFFFF;
 
 static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv, int group, int d, int window, int sinks) {
     AttendPlan p{};
     const int64_t rows = (int64_t)sv.n_tokens * group;
     auto known = [](int hint, int64_t cap) { return hint > 0 ? std::min<int64_t>(hint, cap) : cap; };
     const int64_t len = known(st->max_len, sv.own_cap), pre = sv.n_groups > 0 ? known(st->max_prefix, sv.prefix_cap) : 0;
-    const int64_t most_q = known(st->max_q, sv.n_tokens);
+    const int64_t most_q = std::max<int64_t>(known(st->max_q, sv.n_tokens), (sv.n_tokens + sv.n_seq - 1) / sv.n_seq);
     // a pass of its own for the prefix costs a launch and partial sums, and saves the prefix's keys of all sequences but one: worth it
     // from some hundred keys on (16 groups of 4, 8 key heads of 128: prefixes of 128 keys 39.7 us with it, 31.6 without; of 500 44.8 and
     // 43.5; of 2000 55 and 73)
@@ -815,7 +845,7 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
     if (sv.n_seq * (int64_t)p.tiles_wide > 2 * (rows / kWideRows + sv.n_seq)) p.tiles_wide = 0;
     if (p.narrow) p.split_narrow = split_few((int64_t)sv.n_seq * hkv, keys);
     if (p.wide) p.split_wide = split_many(hkv * ((rows + kWideRows - 1) / kWideRows + sv.n_seq / 2), keys);
-    p.n_own = std::max(p.split_narrow, p.split_wide);
+    p.n_own = p.wide ? p.split_wide : p.split_narrow;
     if (p.shared) {
         const int64_t group_rows = rows / sv.n_groups;
         p.prefix_narrow = group_rows <= kNarrowRows;
@@ -832,10 +862,18 @@ static AttendPlan plan_attend(const ivf_kv_step* st, const StepView& sv, int hkv
     const int64_t piece = std::max(keys / std::max(1, p.split_narrow), p.shared && p.prefix_narrow ? read_keys(pre) / p.split_prefix : 0);
     p.one_wave = d > 64 && p.narrow && (int64_t)sv.n_seq * hkv * p.split_narrow >= 512 && (d > 128 || piece <= 256);
     p.parts = p.shared || p.n_own > 1 ? p.part_own + p.n_own : 0;
+    // (with them among the others, a prompt of 16,000 tokens beside two single ones of 60,000 keys took 16 GB of workspace for the
+    // pieces of the two; apart 24 MB)
+    if (p.narrow && p.wide && (p.shared || p.split_narrow > 1)) p.few_tokens = std::max(1, kNarrowRows / group);
     return p;
 }
 
-static size_t plan_bytes(const AttendPlan& p, int64_t rows, int d) { return (size_t)(rows * p.parts) * ((size_t)d * 4 + 8); }
+// partial sums of the tokens, and of the few's places
+static int64_t plan_sums(const AttendPlan& p, int64_t n_tokens, int hq) { return n_tokens * hq * p.parts; }
+static int64_t plan_few_sums(const AttendPlan& p, int64_t n_seq, int hq) { return n_seq * p.few_tokens * hq * p.split_narrow; }
+static size_t plan_bytes(const AttendPlan& p, const StepView& sv, int hq, int d) {
+    return (size_t)(plan_sums(p, sv.n_tokens, hq) + plan_few_sums(p, sv.n_seq, hq)) * ((size_t)d * 4 + 8);
+}
 
 // One launch for one pass or two: units of the first and of the second.
 template <typename T, int D, int NARROW>
@@ -862,6 +900,9 @@ static hipError_t launch_attend(AttendArgs a, const AttendPlan& p, hipStream_t s
     const int64_t rows = (int64_t)a.step.n_tokens * a.hq, units = a.step.n_seq, groups = p.shared ? a.step.n_groups : 0;
     hipError_t e;
     a.parts = p.parts;
+    a.part_own = p.part_own;
+    a.few_tokens = p.few_tokens;
+    a.few_parts = p.split_narrow;
     const int mode = p.shared ? kOwn : kConcat;
     // the prefix goes first, with those of the other keys' passes that the same kernel makes
     const AttendArgs::Pass prefix = {kPrefix, 0, p.split_prefix, p.split_prefix, p.tiles_prefix, 0, kAllRows};
@@ -880,8 +921,11 @@ static hipError_t launch_attend(AttendArgs a, const AttendPlan& p, hipStream_t s
         else e = launch_passes<T, D, 2>(a, groups_narrow, n, s);
         if (e) return e;
     }
-    if (p.parts > 0) {
-        hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 8192)), dim3(256), 0, s, a);
+    const int64_t joins = std::max(p.parts > 0 ? rows : 0, units * p.few_tokens * a.hq);
+    if (joins > 0) {
+        const dim3 grid((unsigned)std::min<int64_t>((joins + 3) / 4, 8192)), block(256);
+        if (p.few_tokens > 0) hipLaunchKernelGGL((attend_join_kernel<T, D, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((attend_join_kernel<T, D, false>), grid, block, 0, s, a);
         return hipGetLastError();
     }
     return hipSuccess;
@@ -909,7 +953,7 @@ extern "C" int ivf_attend_workspace(const ivf_kv_step* step, const ivf_kv_cache*
     if ((rc = check_heads(cache, n_q_heads, window, sinks))) return rc;
     if (!bytes) return fail(IVF_EINVAL, "bytes is NULL");
     const AttendPlan p = plan_attend(step, sv, cache->n_heads, n_q_heads / cache->n_heads, cache->d, window, sinks);
-    *bytes = plan_bytes(p, (int64_t)sv.n_tokens * n_q_heads, cache->d);
+    *bytes = plan_bytes(p, sv, n_q_heads, cache->d);
     return IVF_OK;
 }
 
@@ -926,12 +970,14 @@ extern "C" int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, co
     a.q = *q; a.out = *out; a.lse = lse; a.scale_log2 = scale * 1.4426950408889634f;
     a.hq = n_q_heads; a.hkv = cache->n_heads; a.group = n_q_heads / cache->n_heads; a.window = window; a.sinks = sinks;
     const AttendPlan p = plan_attend(step, a.step, a.hkv, a.group, cache->d, window, sinks);
-    const int64_t rows = (int64_t)a.step.n_tokens * n_q_heads;
-    const size_t need = plan_bytes(p, rows, cache->d);
+    const size_t need = plan_bytes(p, a.step, n_q_heads, cache->d);
     if (workspace_bytes < need || (need > 0 && !workspace))
         return fail(IVF_EINVAL, "this call needs %zu bytes of workspace (got %zu)", need, workspace ? workspace_bytes : (size_t)0);
     a.part_o = (float*)workspace;
-    a.part_ml = (float2*)((float*)workspace + (size_t)(rows * p.parts) * cache->d);
+    const int64_t sums = plan_sums(p, a.step.n_tokens, n_q_heads), few = plan_few_sums(p, a.step.n_seq, n_q_heads);
+    a.few_o = a.part_o + sums * cache->d;
+    a.part_ml = (float2*)(a.few_o + few * cache->d);
+    a.few_ml = a.part_ml + sums;
     HIP_TRY(cache->dtype == IVF_F16 ? launch_attend<_Float16>(a, p, cache->d, (hipStream_t)stream)
                                     : launch_attend<__bf16>(a, p, cache->d, (hipStream_t)stream));
     return IVF_OK;

@@ -126,3 +126,40 @@ def test_beam_steps():
 def test_caches_beyond_the_limits(kw):
     cache = _cache(**kw)
     assert _append(cache=cache) == -5 and _attend(cache=cache) == -5
+
+
+def _need(n_seq, n_tokens, hq, hkv, d, keys, page=64, groups=0, prefix=0, hints=(0, 0, 0)):
+    """Workspace of steps whose tables have room for `keys` own and `prefix` shared keys."""
+    n = C.c_size_t()
+    step = _step(n_seq=n_seq, n_tokens=n_tokens, page=page, table_stride=-(-keys // page), max_q=hints[0], max_len=hints[1])
+    if groups:
+        step.n_groups, step.group_off, step.prefix_len, step.prefix_table = groups, OK, OK, OK
+        step.prefix_stride, step.prefix_page, step.max_prefix = -(-prefix // page), page, hints[2]
+    cache = _cache(page=page, n_heads=hkv, d=d, n_pages=1 << 20, page_stride=page * hkv * d, token_stride=hkv * d, head_stride=d)
+    assert P.load().ivf_attend_workspace(step, cache, hq, 0, 0, C.byref(n)) == 0
+    return n.value
+
+
+@pytest.mark.parametrize("sizes", [dict(n_seq=3, n_tokens=16002, hq=32, hkv=8, d=128, keys=60000, hints=(16000, 60000, 0)),
+                                   dict(n_seq=8, n_tokens=32007, hq=64, hkv=8, d=128, keys=100000, hints=(32000, 100000, 0)),
+                                   dict(n_seq=3, n_tokens=15000, hq=32, hkv=8, d=128, keys=131072),
+                                   dict(n_seq=1, n_tokens=16000, hq=32, hkv=8, d=128, keys=60000, hints=(1, 60000, 0))])
+def test_prompts_beside_single_tokens_need_little_workspace(sizes):
+    """Rows whose keys are not cut need no room for the pieces of those whose are.  64 MB are the pieces of 32 rows of 128 for
+    each of 4096 workgroups."""
+    assert _need(**sizes) <= 128 << 20
+
+
+def test_workspaces_are_bounded():
+    """A row's keys are cut only as far as places on the chip are free: 4096 pieces of 32 rows or 512 of 128, of the own and of the prefix's keys, beside one
+    piece a row or tile of each."""
+    import random
+    rng = random.Random(5)
+    for _ in range(4000):
+        n_seq, hkv, d = round(2 ** rng.uniform(0, 11)), rng.choice([1, 2, 8, 16]), rng.choice([64, 96, 128, 256])
+        hq, n_tokens = hkv * rng.choice([1, 2, 7, 8, 40]), max(1, round(2 ** rng.uniform(0, 16)))
+        keys, groups = round(2 ** rng.uniform(0, 20)), rng.choice([0, 1, max(1, n_seq // 4), n_seq])
+        prefix = round(2 ** rng.uniform(0, 17)) if groups else 0
+        hints = tuple(rng.choice([0, 1, round(2 ** rng.uniform(0, 17))]) for _ in range(3))
+        sums = 2 * 4096 * 33 + 2 * 512 * 129 + 2 * n_tokens * hq + 2 * 129 * hkv * (n_seq + groups)
+        assert _need(n_seq, n_tokens, hq, hkv, d, keys, groups=groups, prefix=prefix, hints=hints) <= sums * (4 * d + 8), (n_seq, n_tokens, hq, hkv, d, keys, groups, prefix, hints)

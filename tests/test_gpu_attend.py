@@ -383,3 +383,22 @@ def test_as_many_keys_as_positions_count():
     out = P.ivf_attend(step, P.KvCache(k, v), torch.zeros(2, 1, d, dtype=torch.bfloat16, device="cuda"), lse=lse, window=100, sinks=3)
     assert bool((out == 1).all())
     np.testing.assert_allclose(lse.cpu().numpy(), np.log(103.0), rtol=1e-6)
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 64), ("bf16", 96), ("bf16", 128), ("f16", 256)])
+@pytest.mark.parametrize("new,own,groups", [([300, 1, 0, 2, 1, 8], [300, 3000, 9, 5, 1400, 700], []), ([150, 1, 9, 8, 1], [2500, 3000, 2000, 2000, 40], []),
+                                            ([150, 1, 9, 8, 1, 1], [180, 3000, 2000, 2000, 40, 0], [(2, 1300), (2, 0), (1, 40)]),
+                                            ([60, 1, 1, 0, 2], [2500, 1, 2500, 0, 90], [(4, 2600)])])
+@pytest.mark.parametrize("hints", [False, True])
+def test_prompts_beside_long_single_tokens(dtype, d, new, own, groups, hints):
+    """Few rows whose keys are cut into pieces beside many whose keys are not, or are too; with and without a shared prefix."""
+    pr = Problem(new, own, groups=groups, hkv=2, d=d, dtype=dtype, seed=24)
+    _run(pr, 8, hints=dict(max_q=max(new), max_len=max(own), max_prefix=max([p for _, p in groups] + [0])) if hints else {})
+
+
+@pytest.mark.parametrize("groups", [[], [(300, 700), (200, 0)]])
+def test_many_single_tokens_beside_prompts(groups):
+    """More places of few rows than wavefronts that join."""
+    n = 1100
+    new = [40 if i % 100 == 7 else i % 4 for i in range(n)]
+    _run(Problem(new, [m + (1500 if i % 97 == 5 else i % 30) for i, m in enumerate(new)], groups=groups, hkv=1, d=64, dtype="f16", seed=25), 8, hints=dict(max_q=40, max_len=1503))
