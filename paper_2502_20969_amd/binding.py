@@ -504,13 +504,20 @@ def _code(dtype):
     return code
 
 
-def _i32(a, shape, what):
-    """A contiguous int32 CUDA tensor of this shape (None in it: any size)."""
+def _elsewhere(what, a, device):
+    where = f"device {device}" if device >= 0 else "a CUDA device"
+    return ValueError(f"{what} is on {a.device}, not on {where} like the rest of the call")
+
+
+def _i32(a, shape, device, what):
+    """A contiguous int32 tensor of this shape (None in it: any size) on this device."""
     t = _torch()
     if a.dtype is not t.int32:
         raise TypeError(f"{what} must be int32")
-    if not a.is_cuda or not a.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous CUDA tensor")
+    if a.get_device() != device or device < 0:
+        raise _elsewhere(what, a, device)
+    if not a.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
     if len(a.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, a.shape)):
         raise ValueError(f"{what} has shape {tuple(a.shape)}, expected {tuple(shape)}")
     return a.data_ptr()
@@ -522,8 +529,10 @@ def _rows(a, n_tokens, n_heads, cache, what):
     if a.dtype is not cache.dtype:
         raise TypeError(f"{what} is {a.dtype}, the cache {cache.dtype}")
     stride = a.stride()
-    if a.shape != (n_tokens, n_heads, cache.d) or not a.is_cuda:
-        raise ValueError(f"{what} has shape {tuple(a.shape)}, expected CUDA [{n_tokens}, {n_heads}, {cache.d}]")
+    if a.shape != (n_tokens, n_heads, cache.d):
+        raise ValueError(f"{what} has shape {tuple(a.shape)}, expected [{n_tokens}, {n_heads}, {cache.d}]")
+    if a.get_device() != cache.device:
+        raise _elsewhere(what, a, cache.device)
     if stride[2] != 1:
         raise ValueError(f"the elements of a head of {what} must lie side by side")
     return RowsArg(a.data_ptr(), stride[0], stride[1])
@@ -538,7 +547,9 @@ class KvCache:
             raise ValueError("k and v must have the same type, shape and strides")
         if not (k.is_cuda and v.is_cuda) or k.dim() != 4 or k.stride(3) != 1:
             raise ValueError("expected CUDA tensors [n_pages, page, heads, d] with the elements of a head side by side")
-        self.k, self.v, self.dtype = k, v, k.dtype
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.get_device()
+        if v.get_device() != self.device:
+            raise _elsewhere("v", v, self.device)
         (self.pages, self.page, self.heads, self.d), st = k.shape, k.stride()
         self.arg = KvCacheArg(k.data_ptr(), v.data_ptr(), self.pages, st[0], st[1], st[2], self.page, self.heads, self.d, _code(k.dtype))
         self.ref = C.byref(self.arg)
@@ -553,17 +564,17 @@ class KvStep:
 
     def __init__(self, q_off, lens, table, page, n_tokens, max_q=0, max_len=0, group_off=None, prefix_lens=None, prefix_table=None,
                  prefix_page=None, max_prefix=0):
-        n = lens.shape[0]
-        a = KvStepArg(_i32(q_off, (n + 1,), "q_off"), _i32(lens, (n,), "lens"), _i32(table, (n, None), "table"), table.shape[1])
+        n, dev = lens.shape[0], lens.get_device()
+        a = KvStepArg(_i32(q_off, (n + 1,), dev, "q_off"), _i32(lens, (n,), dev, "lens"), _i32(table, (n, None), dev, "table"), table.shape[1])
         a.n_seq, a.n_tokens, a.page, a.max_q, a.max_len = n, n_tokens, page, max_q, max_len
         if group_off is not None:
             if prefix_lens is None or prefix_table is None:
                 raise ValueError("group_off, prefix_lens and prefix_table go together")
             g = prefix_lens.shape[0]
-            a.group_off, a.prefix_len = _i32(group_off, (g + 1,), "group_off"), _i32(prefix_lens, (g,), "prefix_lens")
-            a.prefix_table, a.prefix_stride = _i32(prefix_table, (g, None), "prefix_table"), prefix_table.shape[1]
+            a.group_off, a.prefix_len = _i32(group_off, (g + 1,), dev, "group_off"), _i32(prefix_lens, (g,), dev, "prefix_lens")
+            a.prefix_table, a.prefix_stride = _i32(prefix_table, (g, None), dev, "prefix_table"), prefix_table.shape[1]
             a.n_groups, a.prefix_page, a.max_prefix = g, page if prefix_page is None else prefix_page, max_prefix
-        self.arg, self.n_tokens = a, n_tokens
+        self.arg, self.n_tokens, self.device = a, n_tokens, dev
         self._keep = (q_off, lens, table, group_off, prefix_lens, prefix_table)
         self._need = {}            # bytes of workspace by what they depend on
         self.ref = C.byref(a)
@@ -588,24 +599,39 @@ def _workspace(n, stream):
     return _new(stream, n, _torch().uint8, False)
 
 
+def _room(workspace, device):
+    """Place and bytes of the caller's workspace."""
+    if workspace.get_device() != device:
+        raise _elsewhere("workspace", workspace, device)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace.data_ptr(), workspace.nbytes
+
+
 _raw_stream = None
 
 
-def _on(stream):
-    """The stream's handle; None: torch's current one."""
+def _on(stream, device):
+    """The stream's handle; None: torch's current one.  Kernels are launched on the current device, which the call's tensors have to be on."""
     global _raw_stream
+    t = _torch()
+    now = t.cuda.current_device()
+    if now != device or (stream is not None and stream.device_index != now):
+        raise ValueError(f"the current device is {now}, the tensors are on device {device}" + ("" if stream is None else f", the stream on {stream.device_index}"))
     if stream is not None:
         return stream.cuda_stream
-    t = _torch()
     if _raw_stream is None:        # the handle alone, where this torch gives it, spares a Stream object per call
         _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda device: t.cuda.current_stream(device).cuda_stream)
-    return _raw_stream(t.cuda.current_device())
+    return _raw_stream(now)
 
 
 def ivf_kv_append(step, cache, k, v, rotary=None, positions=None, q=None, q_out=None, interleaved=False, stream=None):
     """Appends the new tokens' k and v [tokens, heads, d] to the cache; with rotary [positions, rot] float32 (cosines,
     then sines) keys and q [tokens, query heads, d] are rotated.  Returns q_out (default: a new tensor)."""
-    n = step.n_tokens
+    n, dev = step.n_tokens, cache.device
+    if step.device != dev:
+        raise ValueError(f"the step is on device {step.device}, the cache on {dev}")
+    on = _on(stream, dev)
     kr, vr = _rows(k, n, cache.heads, cache, "k"), _rows(v, n, cache.heads, cache, "v")
     qr = qo = rp = pp = None
     hq = n_pos = rot = 0
@@ -617,13 +643,13 @@ def ivf_kv_append(step, cache, k, v, rotary=None, positions=None, q=None, q_out=
     elif q_out is not None:
         raise ValueError("q_out without q")
     if rotary is not None:
-        if rotary.dtype is not _torch().float32 or not rotary.is_cuda or not rotary.is_contiguous() or rotary.dim() != 2:
-            raise ValueError("rotary must be a contiguous float32 CUDA tensor [positions, rot]")
+        if rotary.dtype is not _torch().float32 or rotary.get_device() != dev or not rotary.is_contiguous() or rotary.dim() != 2:
+            raise ValueError("rotary must be a contiguous float32 tensor [positions, rot] on the cache's device")
         n_pos, rot = rotary.shape
         rp = rotary.data_ptr()
     if positions is not None:
-        pp = _i32(positions, (n,), "positions")
-    status = load().ivf_kv_append(step.ref, cache.ref, kr, vr, rp, n_pos, rot, 1 if interleaved else 0, pp, qr, qo, hq, _on(stream))
+        pp = _i32(positions, (n,), dev, "positions")
+    status = load().ivf_kv_append(step.ref, cache.ref, kr, vr, rp, n_pos, rot, 1 if interleaved else 0, pp, qr, qo, hq, on)
     if status != 0:
         _check(status)
     return q_out
@@ -633,7 +659,10 @@ def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0
     """Attention of the new tokens q [tokens, query heads, d] over the cache; returns out (default: a new tensor).
     lse: float32 [tokens, query heads] or None.  scale: default d ** -0.5.  workspace: a uint8 CUDA tensor of
     at least ivf_attend_workspace() bytes, default one for this call."""
-    n = step.n_tokens
+    n, dev = step.n_tokens, cache.device
+    if step.device != dev:
+        raise ValueError(f"the step is on device {step.device}, the cache on {dev}")
+    on = _on(stream, dev)
     if out is None:
         out = _new(stream, q.shape, q.dtype)
     hq = q.shape[1]
@@ -641,17 +670,16 @@ def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0
     lp = wp = None
     wn = 0
     if lse is not None:
-        if lse.dtype is not _torch().float32 or not lse.is_cuda or not lse.is_contiguous() or lse.shape != (n, hq):
-            raise ValueError("lse must be a contiguous float32 CUDA tensor [tokens, query heads]")
+        if lse.dtype is not _torch().float32 or lse.get_device() != dev or not lse.is_contiguous() or lse.shape != (n, hq):
+            raise ValueError("lse must be a contiguous float32 tensor [tokens, query heads] on the cache's device")
         lp = lse.data_ptr()
     if workspace is None:
         wn = ivf_attend_workspace(step, cache, hq, window, sinks)
         if wn:
             workspace = _workspace(wn, stream)
     if workspace is not None:
-        wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    status = load().ivf_attend(step.ref, cache.ref, qr, hq, qo, lp, cache.d ** -0.5 if scale is None else scale, window, sinks, wp, wn,
-                               _on(stream))
+        wp, wn = _room(workspace, dev)
+    status = load().ivf_attend(step.ref, cache.ref, qr, hq, qo, lp, cache.d ** -0.5 if scale is None else scale, window, sinks, wp, wn, on)
     if status != 0:
         _check(status)
     return out
@@ -676,10 +704,10 @@ def ivf_beam_workspace(n_prompts, beams_in, vocab, beams_out):
     return n.value
 
 
-def _state(src, dst, rows_in, rows_out):
+def _state(src, dst, rows_in, rows_out, device):
     """A state and its destination: rows of the same contiguous elements, evenly spaced."""
-    if src.dtype is not dst.dtype or not (src.is_cuda and dst.is_cuda):
-        raise ValueError("a state and its destination must be CUDA tensors of the same type")
+    if src.dtype is not dst.dtype or src.get_device() != device or dst.get_device() != device:
+        raise ValueError("a state and its destination must be tensors of the same type on the logits' device")
     before, after = src.shape, dst.shape
     if before[0] != rows_in or after[0] != rows_out or before[1:] != after[1:]:
         raise ValueError("a state has a row per beam, before and after")
@@ -696,23 +724,25 @@ def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), 
     CUDA tensors with a row per beam, before and after (prompts * beams and prompts * beams_out rows, each row
     contiguous).  Returns scores, parents (row of logits), tokens and done, each [prompts, beams_out]."""
     t = _torch()
-    if logits.dim() != 3 or not logits.is_cuda or logits.stride(2) != 1:
+    dev = logits.get_device()
+    if logits.dim() != 3 or dev < 0 or logits.stride(2) != 1:
         raise ValueError("logits must be a CUDA tensor [prompts, beams, vocab] with contiguous rows")
+    on = _on(stream, dev)
     p, b, vocab = logits.shape
     by_prompt, stride, _ = logits.stride()
     if b == 1:
         stride = by_prompt if p > 1 else vocab
     elif p > 1 and by_prompt != b * stride:
         raise ValueError("the rows of logits must be evenly spaced")
-    if scores.dtype is not t.float32 or not scores.is_cuda or not scores.is_contiguous() or scores.shape != (p, b):
-        raise ValueError("scores must be a contiguous float32 CUDA tensor [prompts, beams]")
+    if scores.dtype is not t.float32 or scores.get_device() != dev or not scores.is_contiguous() or scores.shape != (p, b):
+        raise ValueError("scores must be a contiguous float32 tensor [prompts, beams] on the logits' device")
     dp = None
     if done is not None:
-        if done.dtype not in (t.bool, t.uint8) or not done.is_cuda or not done.is_contiguous() or done.shape != (p, b):
-            raise ValueError("done must be a contiguous bool or uint8 CUDA tensor [prompts, beams]")
+        if done.dtype not in (t.bool, t.uint8) or done.get_device() != dev or not done.is_contiguous() or done.shape != (p, b):
+            raise ValueError("done must be a contiguous bool or uint8 tensor [prompts, beams] on the logits' device")
         dp = done.data_ptr()
     n = b if beams_out is None else beams_out
-    args = (BeamStateArg * len(states))(*[_state(src, dst, p * b, p * n) for src, dst in states]) if states else None
+    args = (BeamStateArg * len(states))(*[_state(src, dst, p * b, p * n, dev) for src, dst in states]) if states else None
     need = ivf_beam_workspace(p, b, vocab, n)
     # the scores, parents and tokens are one allocation
     out = _new(stream, (3, p, n), t.int32)
@@ -721,10 +751,11 @@ def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), 
     fin = _new(stream, (p, n), t.bool)
     if workspace is None:
         workspace = _workspace(need, stream)
+    wp, wn = _room(workspace, dev)
     at = out.data_ptr()
     status = load().ivf_beam_step(logits.data_ptr(), stride, _code(logits.dtype), p, b, vocab, scores.data_ptr(), dp, eos, n,
                                   at, at + 4 * p * n, at + 8 * p * n, fin.data_ptr(), args, len(states),
-                                  workspace.data_ptr(), workspace.nbytes, _on(stream))
+                                  wp, wn, on)
     if status != 0:
         _check(status)
     return score, parent, token, fin
