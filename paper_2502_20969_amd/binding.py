@@ -567,9 +567,9 @@ class KvStep:
         n, dev = lens.shape[0], lens.get_device()
         a = KvStepArg(_i32(q_off, (n + 1,), dev, "q_off"), _i32(lens, (n,), dev, "lens"), _i32(table, (n, None), dev, "table"), table.shape[1])
         a.n_seq, a.n_tokens, a.page, a.max_q, a.max_len = n, n_tokens, page, max_q, max_len
+        if (group_off is None) != (prefix_lens is None) or (group_off is None) != (prefix_table is None):
+            raise ValueError("group_off, prefix_lens and prefix_table go together")
         if group_off is not None:
-            if prefix_lens is None or prefix_table is None:
-                raise ValueError("group_off, prefix_lens and prefix_table go together")
             g = prefix_lens.shape[0]
             a.group_off, a.prefix_len = _i32(group_off, (g + 1,), dev, "group_off"), _i32(prefix_lens, (g,), dev, "prefix_lens")
             a.prefix_table, a.prefix_stride = _i32(prefix_table, (g, None), dev, "prefix_table"), prefix_table.shape[1]

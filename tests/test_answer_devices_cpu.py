@@ -146,3 +146,10 @@ def test_workspaces_with_holes(reached):
         with pytest.raises(ValueError):
             call(workspace=On(torch.zeros(8192, dtype=torch.uint8)[::2]))
     assert reached == []
+
+
+@pytest.mark.parametrize("names", [("prefix_lens", "prefix_table"), ("prefix_lens",), ("prefix_table",), ("group_off",), ("group_off", "prefix_lens"), ("group_off", "prefix_table")])
+def test_parts_of_a_prefix_alone(names):
+    shapes = dict(group_off=(2,), prefix_lens=(1,), prefix_table=(1, 4))
+    with pytest.raises(ValueError):
+        _step(**{name: _i32(*shapes[name]) if name in names else None for name in shapes})
