@@ -522,8 +522,8 @@ int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_row
  *   states     host array of n_states: row prompt * beams_out + i of `to` becomes row parent of `from`
  *              (row_bytes, and strides in bytes); `to` must not overlap `from`
  *   workspace  as in ivf_attend; its size is ivf_beam_workspace()
- * beams_in and beams_out are at most IVF_MAX_BEAMS, n_states at most IVF_MAX_BEAM_STATES; logits are IVF_F32,
- * IVF_F16 or IVF_BF16.
+ * beams_in and beams_out are at most IVF_MAX_BEAMS, n_states at most IVF_MAX_BEAM_STATES, vocab at most 2^30;
+ * logits are IVF_F32, IVF_F16 or IVF_BF16.
  */
 #define IVF_MAX_BEAMS 64
 #define IVF_MAX_BEAM_STATES 8

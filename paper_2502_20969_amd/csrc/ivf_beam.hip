@@ -400,6 +400,7 @@ static int check_beams(int n_prompts, int beams_in, int vocab, int beams_out) {
         return fail(IVF_EINVAL, "n_prompts, beams_in, vocab and beams_out must be at least 1");
     if (beams_in > IVF_MAX_BEAMS || beams_out > IVF_MAX_BEAMS)
         return fail(IVF_ELIMIT, "%d beams in, %d out: at most %d", beams_in, beams_out, IVF_MAX_BEAMS);
+    if (vocab > 1 << 30) return fail(IVF_ELIMIT, "vocab = %d is above 2^30", vocab);      // tokens are counted in int, up to a tile past the last
     if ((int64_t)n_prompts * std::max(beams_in, beams_out) > (1 << 24)) return fail(IVF_ELIMIT, "%d prompts of %d beams", n_prompts, beams_in);
     return IVF_OK;
 }

@@ -163,3 +163,13 @@ def test_workspaces_are_bounded():
         hints = tuple(rng.choice([0, 1, round(2 ** rng.uniform(0, 17))]) for _ in range(3))
         sums = 2 * 4096 * 33 + 2 * 512 * 129 + 2 * n_tokens * hq + 2 * 129 * hkv * (n_seq + groups)
         assert _need(n_seq, n_tokens, hq, hkv, d, keys, groups=groups, prefix=prefix, hints=hints) <= sums * (4 * d + 8), (n_seq, n_tokens, hq, hkv, d, keys, groups, prefix, hints)
+
+
+def test_vocabularies_beyond_the_limit():
+    """Tokens are counted in 32 bits, up to a tile past the last."""
+    L = P.load()
+    n = C.c_size_t()
+    for vocab in (2 ** 30 + 1, 2 ** 31 - 8192, 2 ** 31 - 1):
+        assert L.ivf_beam_workspace(1, 1, vocab, 1, C.byref(n)) == -5
+        assert L.ivf_beam_step(OK, vocab, 0, 1, 1, vocab, OK, None, 2, 1, OK, OK, OK, OK, None, 0, OK, 1 << 40, None) == -5
+    assert L.ivf_beam_workspace(1, 1, 2 ** 30, 1, C.byref(n)) == 0 and 0 < n.value < 1 << 20
