@@ -518,7 +518,7 @@ int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_row
  * Order: larger score, then lower beam, then larger logit, then lower token.
  *   scores_out, parent, token, done_out   [n_prompts][beams_out], best first: the score, the row it continues, the
  *              token, and 1 where the parent was done or the token is eos.  Where a prompt has fewer
- *              continuations: score -INF, parent = its first row, token -1, done 1
+ *              continuations: score -INF, parent = its first row, token -1, done 1.  They do not overlap the inputs
  *   states     host array of n_states: row prompt * beams_out + i of `to` becomes row parent of `from`
  *              (row_bytes, and strides in bytes); `to` must not overlap `from`
  *   workspace  as in ivf_attend; its size is ivf_beam_workspace()

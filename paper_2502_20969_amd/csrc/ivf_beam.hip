@@ -437,10 +437,13 @@ extern "C" int ivf_beam_step(const void* logits, int64_t row_stride, int dtype, 
     for (int i = 0; i < n_states; ++i) {
         const ivf_beam_state& s = states[i];
         if (!s.from || !s.to) return fail(IVF_EINVAL, "state %d: NULL", i);
+        if (s.from == s.to) return fail(IVF_EINVAL, "state %d: to is from", i);
         if (s.row_bytes < 1 || s.from_stride < 0 || s.to_stride < s.row_bytes) return fail(IVF_EINVAL, "state %d: row_bytes or strides", i);
         a.moves[i] = BeamMove{(const uint8_t*)s.from, (uint8_t*)s.to, s.row_bytes, s.from_stride, s.to_stride};
         moved += s.row_bytes * beams_out;
     }
+    if (scores_out == scores_in) return fail(IVF_EINVAL, "scores_out is scores_in");
+    if (done_out == done_in) return fail(IVF_EINVAL, "done_out is done_in");
     if (!workspace || ((uintptr_t)workspace & 15u) != 0) return fail(IVF_EINVAL, "workspace must be given and 16-byte aligned");
     if (workspace_bytes < need) return fail(IVF_EINVAL, "this call needs %zu bytes of workspace (got %zu)", need, workspace_bytes);
     const int64_t rows = (int64_t)n_prompts * beams_in;

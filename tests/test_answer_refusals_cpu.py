@@ -173,3 +173,17 @@ def test_vocabularies_beyond_the_limit():
         assert L.ivf_beam_workspace(1, 1, vocab, 1, C.byref(n)) == -5
         assert L.ivf_beam_step(OK, vocab, 0, 1, 1, vocab, OK, None, 2, 1, OK, OK, OK, OK, None, 0, OK, 1 << 40, None) == -5
     assert L.ivf_beam_workspace(1, 1, 2 ** 30, 1, C.byref(n)) == 0 and 0 < n.value < 1 << 20
+
+
+def test_what_is_read_is_not_written():
+    """A state's destination that begins where the state does, and outputs in the place of inputs that other workgroups may still read."""
+    L = P.load()
+    n = C.c_size_t()
+    assert L.ivf_beam_workspace(3, 2, 10, 2, C.byref(n)) == 0
+
+    def call(out=OK, fin=2 * OK, state=None):
+        states = (BeamStateArg * 1)(state) if state else None
+        return L.ivf_beam_step(OK, 10, 0, 3, 2, 10, 3 * OK, 4 * OK, 2, 2, out, 5 * OK, 6 * OK, fin, states, 1 if state else 0, OK, n.value, None)
+    assert call(out=3 * OK) == -1 and b"scores" in L.ivf_last_error()
+    assert call(fin=4 * OK) == -1 and b"done" in L.ivf_last_error()
+    assert call(state=BeamStateArg(7 * OK, 7 * OK, 8, 8, 8)) == -1 and b"state 0" in L.ivf_last_error()
