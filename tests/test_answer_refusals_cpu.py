@@ -187,3 +187,13 @@ def test_what_is_read_is_not_written():
     assert call(out=3 * OK) == -1 and b"scores" in L.ivf_last_error()
     assert call(fin=4 * OK) == -1 and b"done" in L.ivf_last_error()
     assert call(state=BeamStateArg(7 * OK, 7 * OK, 8, 8, 8)) == -1 and b"state 0" in L.ivf_last_error()
+
+
+@pytest.mark.parametrize("n_tokens,hq", [(3, 4), (3, 2), (600, 64)])
+def test_workspaces_of_attention_are_checked(n_tokens, hq):
+    """Steps whose keys are cut into pieces: a workspace that is missing or a byte too small."""
+    n = C.c_size_t()
+    step, cache = _step(table_stride=1000, n_tokens=n_tokens), _cache(n_pages=4000)
+    assert P.load().ivf_attend_workspace(step, cache, hq, 0, 0, C.byref(n)) == 0 and n.value > 0
+    for kw in (dict(nbytes=n.value - 1), dict(nbytes=0), dict(ws=None)):
+        assert _attend(step=step, cache=cache, hq=hq, **kw) == -1 and b"workspace" in P.load().ivf_last_error()
