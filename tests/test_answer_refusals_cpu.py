@@ -189,7 +189,7 @@ def test_what_is_read_is_not_written():
     assert call(state=BeamStateArg(7 * OK, 7 * OK, 8, 8, 8)) == -1 and b"state 0" in L.ivf_last_error()
 
 
-@pytest.mark.parametrize("n_tokens,hq", [(3, 4), (3, 2), (600, 64)])
+@pytest.mark.parametrize("n_tokens,hq", [(3, 4), (3, 2), (600, 4)])
 def test_workspaces_of_attention_are_checked(n_tokens, hq):
     """Steps whose keys are cut into pieces: a workspace that is missing or a byte too small."""
     n = C.c_size_t()
