@@ -608,21 +608,20 @@ def _room(workspace, device):
     return workspace.data_ptr(), workspace.nbytes
 
 
-_raw_stream = None
+_raw_stream = _device_now = None
 
 
 def _on(stream, device):
     """The stream's handle; None: torch's current one.  Kernels are launched on the current device, which the call's tensors have to be on."""
-    global _raw_stream
-    t = _torch()
-    now = t.cuda.current_device()
+    global _raw_stream, _device_now
+    if _raw_stream is None:        # the handle and the number alone, where this torch gives them, spare a Stream object and a check per call
+        t = _torch()
+        _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda device: t.cuda.current_stream(device).cuda_stream)
+        _device_now = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
+    now = _device_now()
     if now != device or (stream is not None and stream.device_index != now):
         raise ValueError(f"the current device is {now}, the tensors are on device {device}" + ("" if stream is None else f", the stream on {stream.device_index}"))
-    if stream is not None:
-        return stream.cuda_stream
-    if _raw_stream is None:        # the handle alone, where this torch gives it, spares a Stream object per call
-        _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda device: t.cuda.current_stream(device).cuda_stream)
-    return _raw_stream(now)
+    return _raw_stream(now) if stream is None else stream.cuda_stream
 
 
 def ivf_kv_append(step, cache, k, v, rotary=None, positions=None, q=None, q_out=None, interleaved=False, stream=None):
@@ -677,7 +676,8 @@ def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0
         wn = ivf_attend_workspace(step, cache, hq, window, sinks)
         if wn:
             workspace = _workspace(wn, stream)
-    if workspace is not None:
+            wp = workspace.data_ptr()
+    else:
         wp, wn = _room(workspace, dev)
     status = load().ivf_attend(step.ref, cache.ref, qr, hq, qo, lp, cache.d ** -0.5 if scale is None else scale, window, sinks, wp, wn, on)
     if status != 0:
@@ -751,7 +751,9 @@ def ivf_beam_step(logits, scores, beams_out=None, done=None, eos=-1, states=(), 
     fin = _new(stream, (p, n), t.bool)
     if workspace is None:
         workspace = _workspace(need, stream)
-    wp, wn = _room(workspace, dev)
+        wp, wn = workspace.data_ptr(), need
+    else:
+        wp, wn = _room(workspace, dev)
     at = out.data_ptr()
     status = load().ivf_beam_step(logits.data_ptr(), stride, _code(logits.dtype), p, b, vocab, scores.data_ptr(), dp, eos, n,
                                   at, at + 4 * p * n, at + 8 * p * n, fin.data_ptr(), args, len(states),

@@ -56,7 +56,7 @@ def reached(monkeypatch):
     monkeypatch.setattr(B, "load", lambda: lib)
     monkeypatch.setattr(B, "_raw_stream", lambda device: 0)
     monkeypatch.setattr(B, "_new", lambda stream, shape, dtype, kept=True: On(torch.zeros(shape, dtype=dtype)))
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(B, "_device_now", lambda: 0)
     B.ivf_beam_workspace.cache_clear()
     yield calls
     B.ivf_beam_workspace.cache_clear()
