@@ -10,7 +10,7 @@ namespace ivf {
 struct CacheView {
     void* k;
     void* v;
-    int64_t page_stride, token_stride, head_stride, n_slots;
+    int64_t page_stride, token_stride, head_stride;
     int page_shift, page_bytes, token_bytes;
 };
 
@@ -18,9 +18,9 @@ struct StepView {
     const int32_t *q_off, *len, *table, *group_off, *prefix_len, *prefix_table;
     int64_t table_stride, prefix_stride;
     int64_t own_cap, prefix_cap;         // keys that a row of the tables can name, at most 2^30 - 1024
-    int64_t own_entries, prefix_entries; // entries that lie in the cache
+    int64_t own_entries;                 // entries that lie in the cache
     int n_seq, n_tokens, n_groups, shift, prefix_shift;
-    int own_last, prefix_last;           // the last of them
+    int own_last, prefix_last;           // the last own entry, and the last prefix entry, that lies in the cache
 };
 
 // Checks the caller's structures and fills the views; a status, with the error text set.
@@ -50,11 +50,6 @@ __device__ __forceinline__ int prefix_of(const StepView& st, int g) {
     return g < 0 ? 0 : clamp_len(st.prefix_len[g], st.prefix_cap);
 }
 
-__device__ __forceinline__ int64_t slot_in(const int32_t* row, int64_t entries, int shift, int j) {
-    int64_t e = row[j >> shift];
-    e = e < 0 ? 0 : e >= entries ? entries - 1 : e;
-    return (e << shift) + (j & ((1 << shift) - 1));
-}
 __device__ __forceinline__ int64_t slot_offset(const CacheView& c, int64_t slot) {
     return (slot >> c.page_shift) * c.page_stride + (slot & ((1ll << c.page_shift) - 1)) * c.token_stride;
 }

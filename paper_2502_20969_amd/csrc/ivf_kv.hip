@@ -51,11 +51,11 @@ int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv
     const int64_t slots = cache->n_pages << cs;
     // a prefix and the own keys together, and the tile behind them, stay below 2^31
     auto cap = [](int64_t stride, int shift) { return std::min<int64_t>(std::min<int64_t>(stride, (int64_t)1 << 30 >> shift) << shift, ((int64_t)1 << 30) - 1024); };
-    *cv = CacheView{cache->k, cache->v, cache->page_stride, cache->token_stride, cache->head_stride, slots, cs,
+    *cv = CacheView{cache->k, cache->v, cache->page_stride, cache->token_stride, cache->head_stride, cs,
                     (int)(cache->page_stride * 2), (int)(cache->token_stride * 2)};
     *sv = StepView{step->q_off, step->len, step->table, step->group_off, step->prefix_len, step->prefix_table,
                    step->table_stride, step->prefix_stride, cap(step->table_stride, ss), cap(step->prefix_stride, ps),
-                   slots >> ss, slots >> ps, step->n_seq, step->n_tokens, step->n_groups, ss, ps,
+                   slots >> ss, step->n_seq, step->n_tokens, step->n_groups, ss, ps,
                    (int)std::min<int64_t>((slots >> ss) - 1, INT32_MAX), (int)std::min<int64_t>((slots >> ps) - 1, INT32_MAX)};
     return IVF_OK;
 }
