@@ -511,7 +511,7 @@ int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_row
  * Row r = prompt * beams_in + beam:
  *   logits     row r at r * row_stride (elements of dtype), `vocab` entries; logarithm of the softmax in 32 bits:
  *              (x - max) - log(sum of exp(x - max)).  -INF and NaN entries are no continuations (and count
- *              for nothing in the sum)
+ *              for nothing in the sum).  Where entries are +INF, these alone are, and share the probability: -log(their number)
  *   scores_in  [rows] the beams' scores; a continuation's score is score + log-softmax.  A beam at -INF
  *              offers nothing
  *   done_in    [rows] or NULL: a beam whose byte is not zero offers only the token `eos`, at its own score

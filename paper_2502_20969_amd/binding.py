@@ -656,7 +656,7 @@ def ivf_kv_append(step, cache, k, v, rotary=None, positions=None, q=None, q_out=
 
 def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0, workspace=None, stream=None):
     """Attention of the new tokens q [tokens, query heads, d] over the cache; returns out (default: a new tensor).
-    lse: float32 [tokens, query heads] or None.  scale: default d ** -0.5.  workspace: a uint8 CUDA tensor of
+    lse: float32 [tokens, query heads] or None.  scale: default d ** -0.5.  workspace: a contiguous CUDA tensor of
     at least ivf_attend_workspace() bytes, default one for this call."""
     n, dev = step.n_tokens, cache.device
     if step.device != dev:

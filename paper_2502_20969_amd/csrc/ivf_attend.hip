@@ -17,11 +17,12 @@
 // permuted on the way so that both kinds of LDS reads are spread over the banks.  The tables' entries are fetched into
 // LDS in the same way ahead of the tiles they name.
 //
-// What bounds it.  Few rows: memory, if the keys are long (24 sequences of up to 60,000 keys, 8 key heads of 128, bf16: 531 us, 5.6
-// TB/s), else the chain of lengths, table, keys and joins (one token over 700 keys: 8.9 us and 3 for the joining).  Many rows: LDS.  Each
-// wavefront reads a tile's keys and values once for its 32 rows, two bytes per 32 multiplications: a prompt of 16,000 tokens, 32 query
-// and 8 key heads of 128, 2.05 ms, 1000 TFLOP/s, at about 64 bytes a clock and compute unit.  64 rows a wavefront would halve the
-// reads, but their sums and queries do not fit beside a second wavefront's.
+// What bounds it.  Few rows: memory, if the keys are long (24 sequences of up to 60,000 keys, 8 key heads of 128, bf16: 533 us, 5.6
+// TB/s of reads, no byte twice), else the chain of lengths, table, keys and joins (one token over 700 keys: 9 us and 3 for the joining).
+// Many rows: the matrix and the vector instructions of a SIMD's two wavefronts, which seldom run side by side: of a prompt of 16,000
+// tokens, 32 query and 8 key heads of 128, in 2.04 ms, 1030 TFLOP/s, the matrix units are busy for 52 % of the SIMDs' cycles, vector
+// instructions (those that start products among them) for 47 %; LDS for 26 % of a compute unit's, without bank conflicts.  Heads of 64: 35 % and 56 %, LDS
+// 35 %, half of that by bank conflicts (three prompts, 4250 tokens, behind 6000 keys: 375 us, 650 TFLOP/s).
 #include "ivf_answer.h"
 #include "ivf_device.h"
 #include <algorithm>
@@ -159,7 +160,9 @@ template <int CHUNKS> __device__ __forceinline__ int place_swap(int row) {
 }
 
 // Registers: two workgroups a compute unit, but of heads of 256 one, whose sums and queries alone take 192 (eight wavefronts: a prompt
-// of 8000 tokens 890 us against 803)
+// of 8000 tokens 890 us against 803).  What the edge tiles need where a value is not finite decides how many: without it the kernel of many
+// rows would take 189 of heads of 128 and 133 of heads of 64, with it 256 and some 200 in scratch memory, and 202.  The loop over inner tiles
+// uses no scratch memory, an edge tile stores and reloads about ten values and waits for the tile on its way each time.
 template <typename T, int D, int NARROW>
 __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128 ? 1 : 2)) void attend_kernel(AttendArgs a) {
     using S = Shape<D, NARROW>;
@@ -258,8 +261,8 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
     const char* kbase = (const char*)a.cache.k + kvh * a.cache.head_stride * 2;
     const char* vbase = (const char*)a.cache.v + kvh * a.cache.head_stride * 2;
     // Where a wavefront's rows of every tile lie in one page each, which then is found by scalar instructions alone: pages of at
-    // least so many tokens, and a prefix of whole groups of them.  (Without this the vector units, which bound long prompts, spend
-    // a third of their time on places.)
+    // least so many tokens, and a prefix of whole groups of them.  Without this the vector units spend part of their time on places
+    // (three prompts, 4250 tokens, heads of 64, behind 6001 keys or with slots for table entries 407 us, behind 6000 in pages 373).
     const bool paged = !NARROW && (plen == 0 || (1 << pre_shift >= S::kWaveRows && plen % S::kWaveRows == 0)) &&
                        1 << own_shift >= S::kWaveRows && a.cache.token_bytes >= 0 && a.cache.token_bytes < 1 << 26;
     uint32_t page_place[NARROW ? 1 : S::kLoads];
@@ -470,8 +473,8 @@ __global__ __launch_bounds__((Shape<D, NARROW>::kWaves * 64), (NARROW || D > 128
             }
             keep_sums();
             // The weights are summed as they are and rounded to the cache's type for the product, whose operands are 16 bits wide: a term is
-            // off by at most 2^-9 (bf16) or 2^-12 (f16) of itself, as the result's own rounding is.  Against 64 bits the results are
-            // then off by 1.2 to 1.4 times what 32-bit weights leave (bf16 0.0022 and 0.0016, f16 0.00028 and 0.00021)
+            // off by at most 2^-8 (bf16) or 2^-11 (f16) of itself, as the result's own rounding is.  Against 64 bits the results are
+            // then off by 1.2 to 1.4 times what 32-bit weights leave (bf16 0.0022 of their size and 0.0017, f16 0.00028 and 0.00021)
             const float minus = (m == -INFINITY ? 0.f : -m) + H::kLift;
             s8_t p[kKeyTiles * 2];
             float sum[2] = {0.f, 0.f};
