@@ -63,7 +63,8 @@ enum ivf_status {
 };
 
 enum ivf_metric { IVF_IP = 0, IVF_L2 = 1 };
-enum ivf_dtype { IVF_F32 = 0, IVF_F16 = 1, IVF_BF16 = 2 }; /* storage type of list rows */
+enum ivf_dtype { IVF_F32 = 0, IVF_F16 = 1, IVF_BF16 = 2, /* storage types of list rows */
+                 IVF_E4M3 = 3                            /* of a paged cache only */ };
 enum ivf_placement {
     IVF_PLACE_DEVICE = 0, /* every list resident in HBM */
     IVF_PLACE_HOST = 1    /* lists in pinned host memory + a device prefetch buffer
@@ -423,6 +424,14 @@ int ivf_schedule(ivf_index* index, const float* q, int32_t nq, int32_t micro, in
  * of k and of v, so pages can hold tokens one after the other or heads one after the other.  Strides count
  * elements and are multiples of 8, those of pages and tokens below 2^30; k and v are 16-byte aligned; dtype is
  * IVF_F16 or IVF_BF16; page is a power of two.
+ * A quantised cache has dtype IVF_E4M3 and holds 8 bits an element: an e4m3 number (four significant bits, up to 448, 0x7F and 0xFF
+ * are NaN, no infinities) that stands for itself times a power of two, one for each token and head, of keys and of values.  Its bytes
+ * lie as above, with strides that are multiples of 16.  The power 2^e of head h of slot t is the byte e + 127 at
+ *   (t / page) * scale_page_stride + (t % page) * scale_token_stride + h * scale_head_stride
+ * of k_scale and of v_scale (any strides; those of pages and tokens below 2^30).  row_dtype, IVF_F16 or IVF_BF16, is the type of all rows
+ * that go into such a cache or come out of it, and e is at least -15 and at most 8 (f16), or -117 and 120 (bf16): every number
+ * that ivf_kv_append writes is then one of row_dtype.  Bytes outside that range count as its nearest end.  For the other dtypes
+ * k_scale and what follows it is not looked at.
  *
  * ivf_kv_step: the sequences of one step, for all layers.
  *   q_off     [n_seq + 1] first new token of each sequence, ascending from 0 to n_tokens
@@ -447,6 +456,10 @@ typedef struct ivf_kv_cache {
     void* v;
     int64_t n_pages, page_stride, token_stride, head_stride;
     int32_t page, n_heads, d, dtype;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int64_t scale_page_stride, scale_token_stride, scale_head_stride;
+    int32_t row_dtype;
 } ivf_kv_cache;
 
 typedef struct ivf_kv_step {
@@ -470,7 +483,7 @@ typedef struct ivf_rows {
 } ivf_rows;
 
 /*
- * Appends the new tokens' keys and values (n_tokens x cache->n_heads x d each, of the cache's type) to the
+ * Appends the new tokens' keys and values (n_tokens x cache->n_heads x d each, of the cache's type, or its row_dtype) to the
  * cache, each in the slot of its place, and rotates keys and, with q given, queries by position on the way.
  *   rotary     [n_positions][rot] float32: cosines of the rot / 2 angles of a position, then their sines; or
  *              NULL with rot = 0: nothing is rotated.  rot is a multiple of 16 of at most d; the elements from
@@ -481,6 +494,9 @@ typedef struct ivf_rows {
  *   q, q_out   n_tokens x n_q_heads x d each, or both NULL with n_q_heads = 0; q_out may be q
  * d is a multiple of 16 of at most 1024.  Tokens whose place is not in the table or whose entry is not in the
  * cache are not written (their queries are rotated).  Two tokens must not share a slot.
+ * A quantised cache gets the rotated numbers as they are in 32 bits (the two products and their sum rounded one by one), taken
+ * into +-240 * 2^8 (f16) or +-240 * 2^120 (bf16): e is the least of its range with 448 * 2^e at or above the head's largest, and each
+ * number x 2^-e goes to the nearest e4m3 number, ties to even.  What is not finite becomes NaN and counts for nothing in e.
  */
 int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_rows* k, const ivf_rows* v,
                   const float* rotary, int32_t n_positions, int32_t rot, int32_t interleaved, const int32_t* positions,
@@ -490,20 +506,59 @@ int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_
  * Attention of the new tokens over the cache: out = softmax(scale * q . k) v over the keys that a token sees, in
  * 32 bits, rounded once.  A token at position p sees key j when j <= p and, with window > 0, p - j < window or j <
  * sinks.  A token that sees nothing gets zeros.  The keys of a long prefix are read once for all tokens of its group.
- *   q, out     n_tokens x n_q_heads x d, of the cache's type, which do not overlap; query head h reads key
- *              head h / (n_q_heads / cache->n_heads)
+ *   q, out     n_tokens x n_q_heads x d, of the cache's type (a quantised cache's row_dtype), which do not overlap; query
+ *              head h reads key head h / (n_q_heads / cache->n_heads)
  *   lse        [n_tokens][n_q_heads] float32: the logarithm of the sum of the exponentials (-INF: nothing
  *              seen), or NULL
  *   scale      > 0
  *   workspace  device, 16-byte aligned, at least what ivf_attend_workspace() says for the same arguments; its
  *              contents need not be kept, and calls that may overlap need one each
  * d is 64, 96, 128 or 256.  Keys and values in slots that a token does not see never reach its result, whatever
- * they hold; probabilities are rounded to the cache's type before the product with the values.
+ * they hold; probabilities are rounded to the rows' type before the product with the values.
  */
 int ivf_attend_workspace(const ivf_kv_step* step, const ivf_kv_cache* cache, int32_t n_q_heads, int32_t window, int32_t sinks,
                          size_t* bytes);
 int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_rows* q, int32_t n_q_heads, const ivf_rows* out,
                float* lse, float scale, int32_t window, int32_t sinks, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Reads keys and values out of the cache, rotated as they lie there, into rows of its type (a quantised cache's row_dtype, in which
+ * what the cache holds is exact): row r of out_off[s] .. out_off[s + 1] becomes key first[s] + r - out_off[s] of sequence s.
+ *   out_off    [n_seq + 1] ascending, device
+ *   first      [n_seq] device, or NULL: 0
+ *   k, v       n_rows x cache->n_heads x d, of which rows outside all sequences, and those of keys that a sequence does not
+ *              have, are left as they were
+ * d is a multiple of 16.  The step's new tokens are keys like the others.
+ */
+int ivf_kv_read(const ivf_kv_step* step, const ivf_kv_cache* cache, const int32_t* out_off, const int32_t* first, int64_t n_rows,
+                const ivf_rows* k, const ivf_rows* v, void* stream);
+
+/*
+ * Verifies drafted tokens against the target's probabilities.  A sequence's new tokens of this step are one that is settled and, behind
+ * it, drafts (copied from a passage, or drawn by a smaller model); row t of logits is what the target says behind token t, p_t =
+ * softmax(scale * row t) in 64 bits.  Token t, a draft, is accepted if all drafts before it are and uniform[t] * d < p_(t-1)(token),
+ * d = draft[t][token], or 1 without `draft`.  Behind the last accepted one, token a, a token follows that is drawn by uniform[q_off[s]]:
+ * from p_a if a is the sequence's last; else from max(p_a - draft[a + 1], 0), or without `draft` from p_a less the refused token (from
+ * p_a where that leaves nothing).  To draw by u from weights: the first token at which their running sum, in order, is above u times
+ * their sum.
+ *   step       q_off, len, n_seq and n_tokens are used
+ *   logits     row t at t * row_stride (elements of dtype: IVF_F32, IVF_F16 or IVF_BF16), `vocab` entries.  -INF and NaN have
+ *              probability zero; where entries are +INF, these alone have one, and share it
+ *   scale      >= 0, the inverse of a temperature.  0: a draft is accepted if it is the largest entry's token, and that of the largest
+ *              entry follows (of equal ones the first); uniform and draft are not looked at
+ *   tokens     [n_tokens] the tokens; a draft outside the vocabulary is refused (the first of a sequence is not looked at)
+ *   uniform    [n_tokens] numbers from 0 to below 1
+ *   draft      NULL, or row t at t * draft_stride: the float32 probabilities that draft t was drawn from (those of settled tokens
+ *              are not looked at); entries not above zero, and NaN, count as zero
+ *   accepted, follows, len_out   [n_seq] the accepted drafts; the token that follows, -1 where a row has no entry of a probability
+ *              and for sequences without new tokens; len less the drafts that were not accepted.  len_out may be step->len
+ *   workspace  as in ivf_attend; its size is ivf_verify_workspace()
+ * vocab is at most 2^30.
+ */
+int ivf_verify_workspace(int32_t n_seq, int32_t n_tokens, int32_t vocab, size_t* bytes);
+int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int64_t row_stride, int dtype, int32_t vocab, float scale,
+                     const int32_t* tokens, const float* uniform, const float* draft, int64_t draft_stride, int32_t* accepted,
+                     int32_t* follows, int32_t* len_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * One step of a beam search for n_prompts prompts of beams_in beams: of all continuations of a prompt's beams

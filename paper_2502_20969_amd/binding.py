@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libivf.so")
 
 IVF_IP, IVF_L2 = 0, 1
-IVF_F32, IVF_F16, IVF_BF16 = 0, 1, 2
+IVF_F32, IVF_F16, IVF_BF16, IVF_E4M3 = 0, 1, 2, 3
 IVF_PLACE_DEVICE, IVF_PLACE_HOST = 0, 1
 IVF_PREFETCH_RESET = 1
 IVF_MAX_K = 112
@@ -28,7 +28,7 @@ EXPORTS = [
     "ivf_prefetch_ways", "ivf_resident", "ivf_batched_scores", "ivf_get_layout", "ivf_profile_enable", "ivf_profile_read",
     "ivf_profile_reset", "ivf_set_host_threads", "ivf_set_pipeline_depth", "ivf_synchronize",
     "ivf_set_batch_mode", "ivf_limit_batch_memory", "ivf_cache_configure", "ivf_cache_end_round", "ivf_cache_hotness",
-    "ivf_schedule", "ivf_kv_append", "ivf_attend", "ivf_attend_workspace", "ivf_beam_step", "ivf_beam_workspace", "ivf_host_scan", "ivf_host_scan_capacity", "ivf_prefetch_amount", "ivf_prefetch_plan", "ivf_cache_plan", "ivf_strerror", "ivf_last_error",
+    "ivf_schedule", "ivf_kv_append", "ivf_attend", "ivf_attend_workspace", "ivf_kv_read", "ivf_verify_draft", "ivf_verify_workspace", "ivf_beam_step", "ivf_beam_workspace", "ivf_host_scan", "ivf_host_scan_capacity", "ivf_prefetch_amount", "ivf_prefetch_plan", "ivf_cache_plan", "ivf_strerror", "ivf_last_error",
 ]
 
 
@@ -59,7 +59,8 @@ class Profile(C.Structure):
 class KvCacheArg(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("page_stride", C.c_int64),
                 ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("page", C.c_int32), ("n_heads", C.c_int32),
-                ("d", C.c_int32), ("dtype", C.c_int32)]
+                ("d", C.c_int32), ("dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("scale_page_stride", C.c_int64), ("scale_token_stride", C.c_int64), ("scale_head_stride", C.c_int64), ("row_dtype", C.c_int32)]
 
 
 class KvStepArg(C.Structure):
@@ -128,6 +129,9 @@ def load():
     L.ivf_kv_append.argtypes = [step, cache, rows, rows, vp, i32, i32, i32, vp, rows, rows, i32, vp]
     L.ivf_attend_workspace.argtypes = [step, cache, i32, i32, i32, C.POINTER(sz)]
     L.ivf_attend.argtypes = [step, cache, rows, i32, rows, vp, C.c_float, i32, i32, vp, sz, vp]
+    L.ivf_kv_read.argtypes = [step, cache, vp, vp, i64, rows, rows, vp]
+    L.ivf_verify_workspace.argtypes = [i32, i32, i32, C.POINTER(sz)]
+    L.ivf_verify_draft.argtypes = [step, vp, i64, ci, i32, C.c_float, vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]
     L.ivf_beam_workspace.argtypes = [i32, i32, i32, i32, C.POINTER(sz)]
     L.ivf_beam_step.argtypes = [vp, i64, ci, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, C.POINTER(BeamStateArg), i32, vp, sz, vp]
     L.ivf_strerror.argtypes = [ci]
@@ -527,7 +531,7 @@ def _i32(a, shape, device, what):
 def _rows(a, n_tokens, n_heads, cache, what):
     """[n_tokens, n_heads, d] with the elements of a head side by side."""
     if a.dtype is not cache.dtype:
-        raise TypeError(f"{what} is {a.dtype}, the cache {cache.dtype}")
+        raise TypeError(f"{what} is {a.dtype}, the cache's rows are {cache.dtype}")
     stride = a.stride()
     if a.shape != (n_tokens, n_heads, cache.d):
         raise ValueError(f"{what} has shape {tuple(a.shape)}, expected [{n_tokens}, {n_heads}, {cache.d}]")
@@ -538,11 +542,25 @@ def _rows(a, n_tokens, n_heads, cache, what):
     return RowsArg(a.data_ptr(), stride[0], stride[1])
 
 
+_byte_types = None
+
+
+def _bytes(a, codes):
+    """Whether a holds e4m3 numbers (codes), or powers of two, in a type of their own or as bytes."""
+    global _byte_types
+    if _byte_types is None:
+        t = _torch()
+        _byte_types = (t.uint8, t.float8_e8m0fnu), (t.uint8, t.float8_e4m3fn)
+    return a.dtype in _byte_types[codes]
+
+
 class KvCache:
     """The paged cache of one layer: k and v [n_pages, page, heads, d], views of any page, token and head order
-    (a cache of head-major pages is passed as `pages.transpose(1, 2)`)."""
+    (a cache of head-major pages is passed as `pages.transpose(1, 2)`).  A quantised cache has e4m3 numbers (float8_e4m3fn or
+    uint8) in k and v, their powers of two (float8_e8m0fnu or uint8) in k_scale and v_scale [n_pages, page, heads], in any order,
+    and rows of type dtype (float16 or bfloat16)."""
 
-    def __init__(self, k, v):
+    def __init__(self, k, v, k_scale=None, v_scale=None, dtype=None):
         if k.dtype is not v.dtype or k.shape != v.shape or k.stride() != v.stride():
             raise ValueError("k and v must have the same type, shape and strides")
         if not (k.is_cuda and v.is_cuda) or k.dim() != 4 or k.stride(3) != 1:
@@ -551,7 +569,22 @@ class KvCache:
         if v.get_device() != self.device:
             raise _elsewhere("v", v, self.device)
         (self.pages, self.page, self.heads, self.d), st = k.shape, k.stride()
-        self.arg = KvCacheArg(k.data_ptr(), v.data_ptr(), self.pages, st[0], st[1], st[2], self.page, self.heads, self.d, _code(k.dtype))
+        self.k_scale, self.v_scale, self.quantised = k_scale, v_scale, k_scale is not None
+        if (k_scale is None) != (v_scale is None) or (k_scale is None) != (dtype is None):
+            raise ValueError("k_scale, v_scale and dtype go together")
+        if not self.quantised:
+            self.arg = KvCacheArg(k.data_ptr(), v.data_ptr(), self.pages, st[0], st[1], st[2], self.page, self.heads, self.d, _code(k.dtype))
+        else:
+            if not _bytes(k, True) or k_scale.dtype is not v_scale.dtype or not _bytes(k_scale, False):
+                raise TypeError("a quantised cache has float8_e4m3fn or uint8 numbers, and float8_e8m0fnu or uint8 scales")
+            for what, a in (("k_scale", k_scale), ("v_scale", v_scale)):
+                if a.get_device() != self.device:
+                    raise _elsewhere(what, a, self.device)
+            if k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3] or k_scale.stride() != v_scale.stride():
+                raise ValueError("expected k_scale and v_scale [n_pages, page, heads] with the same strides")
+            self.dtype, sc = dtype, k_scale.stride()
+            self.arg = KvCacheArg(k.data_ptr(), v.data_ptr(), self.pages, st[0], st[1], st[2], self.page, self.heads, self.d, IVF_E4M3,
+                                  k_scale.data_ptr(), v_scale.data_ptr(), sc[0], sc[1], sc[2], _code(dtype))
         self.ref = C.byref(self.arg)
 
 
@@ -687,13 +720,86 @@ def ivf_attend(step, cache, q, out=None, lse=None, scale=None, window=0, sinks=0
 
 def ivf_attend_workspace(step, cache, n_q_heads, window=0, sinks=0):
     """Bytes of workspace of ivf_attend with these arguments."""
-    key = (cache.heads, cache.d, cache.page, cache.pages, n_q_heads, window, sinks)
+    key = (cache.heads, cache.d, cache.page, cache.pages, cache.quantised, n_q_heads, window, sinks)
     need = step._need.get(key)
     if need is None:
         n = C.c_size_t(0)
         _check(load().ivf_attend_workspace(step.ref, cache.ref, n_q_heads, window, sinks, C.byref(n)))
         need = step._need[key] = n.value
     return need
+
+
+def ivf_kv_read(step, cache, out_off, k, v, first=None, stream=None):
+    """Reads keys and values out of the cache into k and v [rows, heads, d] of its rows' type: rows out_off[s] .. out_off[s + 1]
+    become the keys first[s] (default 0) and on of sequence s.  out_off [sequences + 1] and first [sequences] are int32 CUDA tensors.
+    Returns k and v."""
+    dev, n = cache.device, k.shape[0]
+    if step.device != dev:
+        raise ValueError(f"the step is on device {step.device}, the cache on {dev}")
+    on = _on(stream, dev)
+    kr, vr = _rows(k, n, cache.heads, cache, "k"), _rows(v, n, cache.heads, cache, "v")
+    op = _i32(out_off, (step.arg.n_seq + 1,), dev, "out_off")
+    fp = None if first is None else _i32(first, (step.arg.n_seq,), dev, "first")
+    if n:
+        _check(load().ivf_kv_read(step.ref, cache.ref, op, fp, n, kr, vr, on))
+    return k, v
+
+
+@functools.lru_cache(maxsize=64)             # a function of the sizes alone
+def ivf_verify_workspace(n_seq, n_tokens, vocab):
+    """Bytes of workspace of ivf_verify_draft with these sizes."""
+    n = C.c_size_t(0)
+    _check(load().ivf_verify_workspace(n_seq, n_tokens, vocab, C.byref(n)))
+    return n.value
+
+
+def _matrix(a, n_rows, what):
+    """[n_rows, vocab] with the entries of a row side by side; the distance of its rows."""
+    if a.dim() != 2 or a.shape[0] != n_rows or a.stride(1) != 1:
+        raise ValueError(f"{what} must be [{n_rows}, vocab] with contiguous rows")
+    return a.stride(0) if n_rows > 1 else a.shape[1]
+
+
+def ivf_verify_draft(step, logits, tokens, uniform=None, draft=None, scale=1.0, lens_out=None, workspace=None, stream=None):
+    """Verifies the drafted tokens of a step: of each sequence's new tokens (int32 [tokens]) the first is settled, the others are
+    drafts.  logits [tokens, vocab] (float32, float16 or bfloat16) is what the target says behind each token, uniform float32 [tokens]
+    in [0, 1) decides on the drafts and, by that of the settled token, on the token that follows.  draft: float32 [tokens, vocab], the
+    probabilities that the drafts were drawn from, None where they were not drawn (copied text).  scale: the inverse of the temperature,
+    0: the largest logit alone.  Returns per sequence the number of accepted drafts, the token that follows them, and the
+    lengths less the refused ones (in lens_out, which may be the step's lens)."""
+    t = _torch()
+    dev, n = step.device, step.n_tokens
+    on = _on(stream, dev)
+    if logits.get_device() != dev:
+        raise _elsewhere("logits", logits, dev)
+    stride, vocab, dtype = _matrix(logits, n, "logits"), logits.shape[1], _code(logits.dtype)
+    tp = _i32(tokens, (n,), dev, "tokens")
+    up = dp = None
+    by_draft = 0
+    if uniform is not None:
+        if uniform.dtype is not t.float32 or uniform.get_device() != dev or not uniform.is_contiguous() or uniform.shape != (n,):
+            raise ValueError("uniform must be a contiguous float32 tensor [tokens] on the step's device")
+        up = uniform.data_ptr()
+    if draft is not None:
+        if draft.dtype is not t.float32 or draft.get_device() != dev or draft.shape[-1] != vocab:
+            raise ValueError("draft must be a float32 tensor [tokens, vocab] on the step's device")
+        by_draft, dp = _matrix(draft, n, "draft"), draft.data_ptr()
+    s = step.arg.n_seq
+    out = _new(stream, (2 if lens_out is not None else 3, s), t.int32)
+    if lens_out is None:
+        lens_out = out[2]
+    lp = _i32(lens_out, (s,), dev, "lens_out")
+    need = ivf_verify_workspace(s, n, vocab)
+    if workspace is None:
+        workspace = _workspace(need, stream)
+        wp, wn = workspace.data_ptr(), need
+    else:
+        wp, wn = _room(workspace, dev)
+    at = out.data_ptr()
+    status = load().ivf_verify_draft(step.ref, logits.data_ptr(), stride, dtype, vocab, scale, tp, up, dp, by_draft, at, at + 4 * s, lp, wp, wn, on)
+    if status != 0:
+        _check(status)
+    return out[0], out[1], lens_out
 
 
 @functools.lru_cache(maxsize=64)             # a function of the sizes alone

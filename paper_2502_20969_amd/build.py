@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libivf.so")
 
-HIP_SOURCES = ["ivf_kernels.hip", "ivf_batched.hip", "ivf_sched.hip", "ivf_api.hip", "ivf_attend.hip", "ivf_kv.hip", "ivf_beam.hip"]
+HIP_SOURCES = ["ivf_kernels.hip", "ivf_batched.hip", "ivf_sched.hip", "ivf_api.hip", "ivf_attend.hip", "ivf_attend_quant.hip", "ivf_kv.hip", "ivf_verify.hip", "ivf_beam.hip"]
 HOST_SOURCES = ["host_scan.cpp", "host_plan.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

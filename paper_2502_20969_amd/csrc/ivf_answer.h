@@ -23,8 +23,18 @@ struct StepView {
     int own_last, prefix_last;           // the last own entry, and the last prefix entry, that lies in the cache
 };
 
-// Checks the caller's structures and fills the views; a status, with the error text set.
-int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv, StepView* sv);
+// The powers of two of a quantised cache.  Strides count bytes.
+struct QuantView {
+    uint8_t* k;
+    uint8_t* v;
+    int64_t page_stride, token_stride, head_stride;
+    int least, most;                     // bytes that stand for powers of the rows' type
+};
+
+// Checks the caller's structures and fills the views; a status, with the error text set.  `qv`: filled for a quantised cache.
+int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv, StepView* sv, QuantView* qv);
+// The type of the rows that go into a cache and come out of it
+inline int row_type(const ivf_kv_cache* cache) { return cache->dtype == IVF_E4M3 ? cache->row_dtype : cache->dtype; }
 // Checks the rows of `what`: pointer, alignment and strides.
 int check_rows(const ivf_rows* r, const char* what);
 
@@ -52,6 +62,25 @@ __device__ __forceinline__ int prefix_of(const StepView& st, int g) {
 
 __device__ __forceinline__ int64_t slot_offset(const CacheView& c, int64_t slot) {
     return (slot >> c.page_shift) * c.page_stride + (slot & ((1ll << c.page_shift) - 1)) * c.token_stride;
+}
+
+__device__ __forceinline__ int64_t scale_offset(const CacheView& c, const QuantView& q, int64_t slot) {
+    return (slot >> c.page_shift) * q.page_stride + (slot & ((1ll << c.page_shift) - 1)) * q.token_stride;
+}
+// 2^e of a byte e + 127
+__device__ __forceinline__ float power_of(const QuantView& q, int byte) {
+    return __uint_as_float((uint32_t)min(max(byte, q.least), q.most) << 23);
+}
+
+// Slot of key j of sequence s, group g, whose prefix has plen keys: taken into the cache
+__device__ __forceinline__ int64_t slot_of_key(const StepView& st, int s, int g, int plen, int j) {
+    if (j < plen) {
+        const int e = st.prefix_table[g * st.prefix_stride + (j >> st.prefix_shift)];
+        return ((int64_t)min(max(e, 0), st.prefix_last) << st.prefix_shift) + (j & ((1 << st.prefix_shift) - 1));
+    }
+    j -= plen;
+    const int e = st.table[s * st.table_stride + (j >> st.shift)];
+    return ((int64_t)min(max(e, 0), st.own_last) << st.shift) + (j & ((1 << st.shift) - 1));
 }
 
 }  // namespace dev

@@ -32,6 +32,9 @@
 namespace ivf {
 using namespace dev;
 
+hipError_t launch_attend_quant(const CacheView& cache, const QuantView& quant, const StepView& step, int row_dtype, const ivf_rows& q, const ivf_rows& out,
+                               float* lse, float scale_log2, int hq, int group, int d, int window, int sinks, hipStream_t s);
+
 enum { kConcat, kOwn, kPrefix };     // keys of a pass: prefix and own, own only, prefix only
 constexpr int kNarrowRows = 32, kWideRows = 128, kAllRows = 0x7FFFFFFF;
 
@@ -949,11 +952,12 @@ using namespace ivf;
 
 extern "C" int ivf_attend_workspace(const ivf_kv_step* step, const ivf_kv_cache* cache, int32_t n_q_heads, int32_t window,
                                     int32_t sinks, size_t* bytes) {
-    CacheView cv; StepView sv;
-    int rc = make_views(step, cache, &cv, &sv);
+    CacheView cv; StepView sv; QuantView qv;
+    int rc = make_views(step, cache, &cv, &sv, &qv);
     if (rc) return rc;
     if ((rc = check_heads(cache, n_q_heads, window, sinks))) return rc;
     if (!bytes) return fail(IVF_EINVAL, "bytes is NULL");
+    if (cache->dtype == IVF_E4M3) { *bytes = 0; return IVF_OK; }
     const AttendPlan p = plan_attend(step, sv, cache->n_heads, n_q_heads / cache->n_heads, cache->d, window, sinks);
     *bytes = plan_bytes(p, sv, n_q_heads, cache->d);
     return IVF_OK;
@@ -963,7 +967,8 @@ extern "C" int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, co
                           const ivf_rows* out, float* lse, float scale, int32_t window, int32_t sinks, void* workspace,
                           size_t workspace_bytes, void* stream) {
     AttendArgs a{};
-    int rc = make_views(step, cache, &a.cache, &a.step);
+    QuantView qv;
+    int rc = make_views(step, cache, &a.cache, &a.step, &qv);
     if (rc) return rc;
     if ((rc = check_heads(cache, n_q_heads, window, sinks))) return rc;
     if ((rc = check_rows(q, "q")) || (rc = check_rows(out, "out"))) return rc;
@@ -971,6 +976,10 @@ extern "C" int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, co
     if (((uintptr_t)workspace & 15u) != 0) return fail(IVF_EINVAL, "workspace must be 16-byte aligned");
     a.q = *q; a.out = *out; a.lse = lse; a.scale_log2 = scale * 1.4426950408889634f;
     a.hq = n_q_heads; a.hkv = cache->n_heads; a.group = n_q_heads / cache->n_heads; a.window = window; a.sinks = sinks;
+    if (cache->dtype == IVF_E4M3) {
+        HIP_TRY(launch_attend_quant(a.cache, qv, a.step, cache->row_dtype, a.q, a.out, lse, a.scale_log2, a.hq, a.group, cache->d, window, sinks, (hipStream_t)stream));
+        return IVF_OK;
+    }
     const AttendPlan p = plan_attend(step, a.step, a.hkv, a.group, cache->d, window, sinks);
     const size_t need = plan_bytes(p, a.step, n_q_heads, cache->d);
     if (workspace_bytes < need || (need > 0 && !workspace))

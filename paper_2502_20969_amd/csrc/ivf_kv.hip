@@ -3,6 +3,7 @@
 #include "ivf_answer.h"
 #include "ivf_device.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace ivf {
 using namespace dev;
@@ -20,16 +21,27 @@ static int shift_of(int32_t page) {
     return __builtin_ctz((unsigned)page);
 }
 
-int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv, StepView* sv) {
+int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv, StepView* sv, QuantView* qv) {
     if (!step || !cache) return fail(IVF_EINVAL, "step or cache is NULL");
     if (!cache->k || !cache->v) return fail(IVF_EINVAL, "cache k or v is NULL");
     if ((((uintptr_t)cache->k | (uintptr_t)cache->v) & 15u) != 0) return fail(IVF_EINVAL, "cache k and v must be 16-byte aligned");
-    if (cache->dtype != IVF_F16 && cache->dtype != IVF_BF16) return fail(IVF_EINVAL, "cache type %d: f16 or bf16 only", cache->dtype);
+    const bool quant = cache->dtype == IVF_E4M3;
+    if (!quant && cache->dtype != IVF_F16 && cache->dtype != IVF_BF16) return fail(IVF_EINVAL, "cache type %d: f16, bf16 or e4m3 only", cache->dtype);
     if (cache->n_pages < 1 || cache->n_heads < 1 || cache->d < 1) return fail(IVF_EINVAL, "cache n_pages, n_heads and d must be at least 1");
-    if (cache->page_stride % 8 != 0 || cache->token_stride % 8 != 0 || cache->head_stride % 8 != 0)
-        return fail(IVF_EINVAL, "cache strides must be multiples of 8 elements");
+    const int lot = quant ? 16 : 8;
+    if (cache->page_stride % lot != 0 || cache->token_stride % lot != 0 || cache->head_stride % lot != 0)
+        return fail(IVF_EINVAL, "cache strides must be multiples of %d elements", lot);
     for (int64_t stride : {cache->page_stride, cache->token_stride})
         if (stride > (1 << 30) - 1 || stride < -(1 << 30)) return fail(IVF_ELIMIT, "cache stride of %lld elements", (long long)stride);
+    if (quant) {
+        if (!cache->k_scale || !cache->v_scale) return fail(IVF_EINVAL, "cache k_scale or v_scale is NULL");
+        const bool half = cache->row_dtype == IVF_F16;
+        if (!half && cache->row_dtype != IVF_BF16) return fail(IVF_EINVAL, "row_dtype %d: f16 or bf16 only", cache->row_dtype);
+        for (int64_t stride : {cache->scale_page_stride, cache->scale_token_stride})
+            if (stride > (1 << 30) - 1 || stride < -(1 << 30)) return fail(IVF_ELIMIT, "scale stride of %lld bytes", (long long)stride);
+        *qv = QuantView{cache->k_scale, cache->v_scale, cache->scale_page_stride, cache->scale_token_stride, cache->scale_head_stride,
+                        127 + (half ? -15 : -117), 127 + (half ? 8 : 120)};
+    }
     const int cs = shift_of(cache->page);
     if (cs < 0) return fail(IVF_EINVAL, "cache page (%d) must be a power of two", cache->page);
     if (cache->n_pages > INT64_MAX >> 32) return fail(IVF_ELIMIT, "cache of %lld pages", (long long)cache->n_pages);
@@ -52,7 +64,7 @@ int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv
     // a prefix and the own keys together, and the tile behind them, stay below 2^31
     auto cap = [](int64_t stride, int shift) { return std::min<int64_t>(std::min<int64_t>(stride, (int64_t)1 << 30 >> shift) << shift, ((int64_t)1 << 30) - 1024); };
     *cv = CacheView{cache->k, cache->v, cache->page_stride, cache->token_stride, cache->head_stride, cs,
-                    (int)(cache->page_stride * 2), (int)(cache->token_stride * 2)};
+                    (int)(cache->page_stride * (quant ? 1 : 2)), (int)(cache->token_stride * (quant ? 1 : 2))};
     *sv = StepView{step->q_off, step->len, step->table, step->group_off, step->prefix_len, step->prefix_table,
                    step->table_stride, step->prefix_stride, cap(step->table_stride, ss), cap(step->prefix_stride, ps),
                    slots >> ss, step->n_seq, step->n_tokens, step->n_groups, ss, ps,
@@ -62,6 +74,7 @@ int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv
 
 struct AppendArgs {
     CacheView cache;
+    QuantView quant;
     StepView step;
     ivf_rows k, v, q, q_out;
     const float* rotary;
@@ -98,25 +111,19 @@ __device__ __forceinline__ void rotate(uint4& a, uint4& b, const float (&c)[8], 
     b = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// One workgroup per new token.  A unit is sixteen elements of a head: in the rotated part eight pairs (two chunks of
-// eight that lie rot / 2 apart, or sixteen in a row), behind it sixteen in a row.  A thread keeps its unit's cosines and
-// sines and takes that unit of one head after the other.  Rotated in 32 bits, rounded once.
-// Bound by memory: 17,000 tokens of 64 query and 8 key heads of 128 in 131 us, 5.4 TB/s read and written.  One token per
-// sequence is a chain of loads (sequence, place, table, cosines): 3.8 us for one, 6.6 for 200.
-template <typename T, bool INTERLEAVED>
-__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
-    const int t = blockIdx.x, tid = threadIdx.x;
+// Slot and position of a new token, by a workgroup of 256; -1: no slot.
+__device__ __forceinline__ int64_t place_token(const AppendArgs& a, int t, int& pos) {
     // the sequence: how many of them begin at or before t
     int below = 0;
-    for (int i = tid; i < a.step.n_seq; i += 256) below += a.step.q_off[i] <= t;
+    for (int i = threadIdx.x; i < a.step.n_seq; i += 256) below += a.step.q_off[i] <= t;
     __shared__ int s_count;
-    if (tid == 0) s_count = 0;
+    if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
     if (below) atomicAdd(&s_count, below);
     __syncthreads();
     const int seq = s_count - 1;
     int64_t slot = -1;
-    int pos = 0;
+    pos = 0;
     if (seq >= 0) {
         const int place = a.step.len[seq] - (a.step.q_off[seq + 1] - t);
         pos = place + prefix_of(a.step, group_of(a.step, seq));
@@ -126,6 +133,19 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
         }
     }
     if (a.positions) pos = a.positions[t];
+    return slot;
+}
+
+// One workgroup per new token.  A unit is sixteen elements of a head: in the rotated part eight pairs (two chunks of
+// eight that lie rot / 2 apart, or sixteen in a row), behind it sixteen in a row.  A thread keeps its unit's cosines and
+// sines and takes that unit of one head after the other.  Rotated in 32 bits, rounded once.
+// Bound by memory: 17,000 tokens of 64 query and 8 key heads of 128 in 131 us, 5.4 TB/s read and written.  One token per
+// sequence is a chain of loads (sequence, place, table, cosines): 3.8 us for one, 6.6 for 200.
+template <typename T, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
+    const int t = blockIdx.x, tid = threadIdx.x;
+    int pos;
+    const int64_t slot = place_token(a, t, pos);
     const int upr = a.d / 16;                               // units of a head
     const int heads = a.hq + 2 * a.hkv;
     const int64_t base = slot < 0 ? 0 : slot_offset(a.cache, slot);
@@ -155,6 +175,149 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     }
 }
 
+// Eight pairs of numbers rotated as 32-bit numbers, products and sum rounded one by one: what is quantised does not depend
+// on which of them a compiler joins.  INTERLEAVED: x are sixteen in a row, pairs side by side; else x[i] and x[8 + i] are a pair.
+template <bool INTERLEAVED>
+__device__ __forceinline__ void rotate_exact(float (&x)[16], const float (&c)[8], const float (&s)[8]) {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float& xa = x[INTERLEAVED ? 2 * i : i];
+        float& xb = x[INTERLEAVED ? 2 * i + 1 : 8 + i];
+        const float a = xa, b = xb;
+        xa = a * c[i] - b * s[i];
+        xb = b * c[i] + a * s[i];
+    }
+}
+
+// Four numbers of at most 448 as e4m3, ties to even
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// The same into a quantised cache.  The units of a head go to the lanes of a group of `width`, a power of two, which find the head's
+// largest number by exchanging it.
+template <typename T, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void kv_append_quant_kernel(AppendArgs a) {
+    const int t = blockIdx.x, tid = threadIdx.x;
+    int pos;
+    const int64_t slot = place_token(a, t, pos);
+    const int upr = a.d / 16, width = upr <= 1 ? 1 : 1 << (32 - __builtin_clz(upr - 1));
+    const int heads = a.hq + 2 * a.hkv, per = 256 / width, u = tid & (width - 1);
+    const bool unit = u < upr, turns = u * 16 < a.rot;
+    const int64_t base = slot < 0 ? 0 : slot_offset(a.cache, slot), scales = slot < 0 ? 0 : scale_offset(a.cache, a.quant, slot);
+    int lo = u * 16, hi = lo + 8;                           // where the unit's two chunks begin
+    float c[8], s[8];
+    if (turns) {
+        if (!INTERLEAVED) { lo = u * 8; hi = lo + a.rot / 2; }
+        const float* row = a.rotary + (int64_t)min(max(pos, 0), a.n_positions - 1) * a.rot + u * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { c[i] = row[i]; s[i] = row[i + a.rot / 2]; }
+    }
+    const float most = __uint_as_float((uint32_t)a.quant.most << 23) * 240.f;
+    for (int h = tid / width; h < heads; h += per) {
+        const bool is_q = h < a.hq, is_v = h >= a.hq + a.hkv;
+        const int hh = is_q ? h : is_v ? h - a.hq - a.hkv : h - a.hq;
+        const ivf_rows& r = is_q ? a.q : is_v ? a.v : a.k;
+        if (!is_q && slot < 0) continue;
+        const T* src = (const T*)r.data + t * r.token_stride + hh * r.head_stride;
+        uint4 x = make_uint4(0, 0, 0, 0), y = x;
+        if (unit) { x = *(const uint4*)(src + lo); y = *(const uint4*)(src + hi); }
+        if (is_q) {
+            if (turns) rotate<T, INTERLEAVED>(x, y, c, s);
+            T* dst = (T*)a.q_out.data + t * a.q_out.token_stride + hh * a.q_out.head_stride;
+            if (unit) { *(uint4*)(dst + lo) = x; *(uint4*)(dst + hi) = y; }
+            continue;
+        }
+        float f[16];
+        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { f[2 * i] = to_float<T>(w[i] & 0xFFFFu); f[2 * i + 1] = to_float<T>(w[i] >> 16); }
+        if (turns && !is_v) rotate_exact<INTERLEAVED>(f, c, s);
+        uint32_t top = 0;                                   // the largest, as bits
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool finite = (__float_as_uint(f[i]) & 0x7F800000u) != 0x7F800000u;
+            f[i] = finite ? fminf(fmaxf(f[i], -most), most) : NAN;
+            top = max(top, finite ? __float_as_uint(f[i]) & 0x7FFFFFFFu : 0u);
+        }
+        for (int step = 1; step < width; step <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, step));
+        // 448 = 1.75 * 2^8
+        const int byte = max((int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u), a.quant.least);
+        const float by = __uint_as_float((uint32_t)(254 - byte) << 23);
+        uint32_t code[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) code[i] = to_e4m3(f[4 * i] * by, f[4 * i + 1] * by, f[4 * i + 2] * by, f[4 * i + 3] * by);
+        if (!unit) continue;
+        uint8_t* dst = (uint8_t*)(is_v ? a.cache.v : a.cache.k) + base + hh * a.cache.head_stride;
+        *(uint2*)(dst + lo) = make_uint2(code[0], code[1]);
+        *(uint2*)(dst + hi) = make_uint2(code[2], code[3]);
+        if (u == 0) (is_v ? a.quant.v : a.quant.k)[scales + hh * a.quant.head_stride] = (uint8_t)byte;
+    }
+}
+
+struct ReadArgs {
+    CacheView cache;
+    QuantView quant;
+    StepView step;
+    ivf_rows k, v;
+    const int32_t *out_off, *first;
+    int64_t n_rows;
+    int hkv, d;
+};
+
+// Two e4m3 numbers times a power of two, in T
+template <typename T, bool HIGH> __device__ __forceinline__ uint32_t from_e4m3(uint32_t code, float power) {
+    if constexpr (std::is_same<T, _Float16>::value) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(code, power, HIGH));
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, power, HIGH));
+}
+
+// A workgroup reads kReadRows rows: its first lanes find their slots, then all take pieces of 16 elements.
+constexpr int kReadRows = 8;
+template <typename T, bool QUANT>
+__global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
+    __shared__ int64_t s_slot[kReadRows];
+    const int64_t row0 = (int64_t)blockIdx.x * kReadRows;
+    if (threadIdx.x < kReadRows) {
+        const int64_t r = row0 + threadIdx.x;
+        int64_t slot = -1;
+        if (r < a.n_rows && r >= a.out_off[0] && r < a.out_off[a.step.n_seq]) {
+            int lo = 0, hi = a.step.n_seq;                  // out_off[lo] <= r < out_off[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.out_off[mid] <= r) lo = mid; else hi = mid;
+            }
+            const int g = group_of(a.step, lo), plen = prefix_of(a.step, g);
+            const int64_t j = r - a.out_off[lo] + (a.first ? a.first[lo] : 0);
+            if (j >= 0 && j < plen + own_len(a.step, lo)) slot = slot_of_key(a.step, lo, g, plen, (int)j);
+        }
+        s_slot[threadIdx.x] = slot;
+    }
+    __syncthreads();
+    const int upr = a.d / 16, per = 2 * a.hkv * upr;
+    for (int i = threadIdx.x; i < kReadRows * per; i += 256) {
+        const int64_t slot = s_slot[i / per], r = row0 + i / per;
+        if (slot < 0) continue;
+        const int unit = i % per % upr, h = i % per / upr % a.hkv;
+        const bool is_v = i % per >= a.hkv * upr;
+        const ivf_rows& to = is_v ? a.v : a.k;
+        T* dst = (T*)to.data + r * to.token_stride + h * to.head_stride + unit * 16;
+        const int64_t at = slot_offset(a.cache, slot) + h * a.cache.head_stride + unit * 16;
+        const void* pool = is_v ? a.cache.v : a.cache.k;
+        if (QUANT) {
+            const uint4 c = *(const uint4*)((const uint8_t*)pool + at);
+            const float p = power_of(a.quant, (is_v ? a.quant.v : a.quant.k)[scale_offset(a.cache, a.quant, slot) + h * a.quant.head_stride]);
+            *(uint4*)dst = make_uint4(from_e4m3<T, false>(c.x, p), from_e4m3<T, true>(c.x, p), from_e4m3<T, false>(c.y, p), from_e4m3<T, true>(c.y, p));
+            *(uint4*)(dst + 8) = make_uint4(from_e4m3<T, false>(c.z, p), from_e4m3<T, true>(c.z, p), from_e4m3<T, false>(c.w, p), from_e4m3<T, true>(c.w, p));
+        } else {
+            const uint4 x = *(const uint4*)((const T*)pool + at), y = *(const uint4*)((const T*)pool + at + 8);
+            *(uint4*)dst = x;
+            *(uint4*)(dst + 8) = y;
+        }
+    }
+}
+
 }  // namespace ivf
 
 using namespace ivf;
@@ -163,7 +326,7 @@ extern "C" int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache,
                              const float* rotary, int32_t n_positions, int32_t rot, int32_t interleaved, const int32_t* positions,
                              const ivf_rows* q, const ivf_rows* q_out, int32_t n_q_heads, void* stream) {
     AppendArgs a{};
-    int rc = make_views(step, cache, &a.cache, &a.step);
+    int rc = make_views(step, cache, &a.cache, &a.step, &a.quant);
     if (rc) return rc;
     if ((rc = check_rows(k, "k")) || (rc = check_rows(v, "v"))) return rc;
     if (n_q_heads < 0 || (n_q_heads == 0) != (q == nullptr) || (q == nullptr) != (q_out == nullptr))
@@ -180,12 +343,42 @@ extern "C" int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache,
     a.hq = n_q_heads; a.hkv = cache->n_heads; a.d = cache->d;
     const dim3 grid(step->n_tokens), block(256);
     hipStream_t s = (hipStream_t)stream;
-    if (cache->dtype == IVF_F16) {
+    if (cache->dtype == IVF_E4M3) {
+        const bool half = cache->row_dtype == IVF_F16;
+        if (half && interleaved) hipLaunchKernelGGL((kv_append_quant_kernel<_Float16, true>), grid, block, 0, s, a);
+        else if (half) hipLaunchKernelGGL((kv_append_quant_kernel<_Float16, false>), grid, block, 0, s, a);
+        else if (interleaved) hipLaunchKernelGGL((kv_append_quant_kernel<__bf16, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((kv_append_quant_kernel<__bf16, false>), grid, block, 0, s, a);
+    } else if (cache->dtype == IVF_F16) {
         if (interleaved) hipLaunchKernelGGL((kv_append_kernel<_Float16, true>), grid, block, 0, s, a);
         else hipLaunchKernelGGL((kv_append_kernel<_Float16, false>), grid, block, 0, s, a);
     } else {
         if (interleaved) hipLaunchKernelGGL((kv_append_kernel<__bf16, true>), grid, block, 0, s, a);
         else hipLaunchKernelGGL((kv_append_kernel<__bf16, false>), grid, block, 0, s, a);
+    }
+    HIP_TRY(hipGetLastError());
+    return IVF_OK;
+}
+
+extern "C" int ivf_kv_read(const ivf_kv_step* step, const ivf_kv_cache* cache, const int32_t* out_off, const int32_t* first, int64_t n_rows,
+                           const ivf_rows* k, const ivf_rows* v, void* stream) {
+    ReadArgs a{};
+    int rc = make_views(step, cache, &a.cache, &a.step, &a.quant);
+    if (rc) return rc;
+    if (!out_off) return fail(IVF_EINVAL, "out_off is NULL");
+    if ((rc = check_rows(k, "k")) || (rc = check_rows(v, "v"))) return rc;
+    if (cache->d % 16 != 0) return fail(IVF_EINVAL, "d must be a multiple of 16 (got %d)", cache->d);
+    if (n_rows < 1) return fail(IVF_EINVAL, "n_rows must be at least 1");
+    if (n_rows > INT32_MAX) return fail(IVF_ELIMIT, "%lld rows", (long long)n_rows);
+    if ((int64_t)kReadRows * 2 * cache->n_heads * (cache->d / 16) > 1 << 30) return fail(IVF_ELIMIT, "%d heads of %d", cache->n_heads, cache->d);
+    a.k = *k; a.v = *v; a.out_off = out_off; a.first = first; a.n_rows = n_rows; a.hkv = cache->n_heads; a.d = cache->d;
+    const dim3 grid((unsigned)((n_rows + kReadRows - 1) / kReadRows)), block(256);
+    hipStream_t s = (hipStream_t)stream;
+    if (cache->dtype == IVF_E4M3) {
+        if (cache->row_dtype == IVF_F16) hipLaunchKernelGGL((kv_read_kernel<_Float16, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((kv_read_kernel<__bf16, true>), grid, block, 0, s, a);
+    } else {
+        hipLaunchKernelGGL((kv_read_kernel<_Float16, false>), grid, block, 0, s, a);
     }
     HIP_TRY(hipGetLastError());
     return IVF_OK;
