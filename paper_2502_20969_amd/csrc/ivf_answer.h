@@ -3,6 +3,7 @@
 #pragma once
 #include "../../include/ivf.h"
 #include "ivf_internal.h"
+#include <type_traits>
 
 namespace ivf {
 
@@ -70,6 +71,12 @@ __device__ __forceinline__ int64_t scale_offset(const CacheView& c, const QuantV
 // 2^e of a byte e + 127
 __device__ __forceinline__ float power_of(const QuantView& q, int byte) {
     return __uint_as_float((uint32_t)min(max(byte, q.least), q.most) << 23);
+}
+
+// Two e4m3 numbers times a power of two, in T
+template <typename T, bool HIGH> __device__ __forceinline__ uint32_t from_e4m3(uint32_t code, float power) {
+    if constexpr (std::is_same<T, _Float16>::value) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(code, power, HIGH));
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, power, HIGH));
 }
 
 // Slot of key j of sequence s, group g, whose prefix has plen keys: taken into the cache

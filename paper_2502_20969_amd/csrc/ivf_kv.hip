@@ -3,7 +3,6 @@
 #include "ivf_answer.h"
 #include "ivf_device.h"
 #include <algorithm>
-#include <type_traits>
 
 namespace ivf {
 using namespace dev;
@@ -266,12 +265,6 @@ struct ReadArgs {
     int64_t n_rows;
     int hkv, d;
 };
-
-// Two e4m3 numbers times a power of two, in T
-template <typename T, bool HIGH> __device__ __forceinline__ uint32_t from_e4m3(uint32_t code, float power) {
-    if constexpr (std::is_same<T, _Float16>::value) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(code, power, HIGH));
-    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, power, HIGH));
-}
 
 // A workgroup reads kReadRows rows: its first lanes find their slots, then all take pieces of 16 elements.
 constexpr int kReadRows = 8;
