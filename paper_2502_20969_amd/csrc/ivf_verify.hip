@@ -29,7 +29,7 @@ struct VerifyArgs {
     int32_t *accepted, *follows, *len_out;
     VerifyTile* tiles;           // [n_tokens][n_tile]
     double* left;                // [n_seq][n_tile] sums of max(w - W d, 0)
-    uint32_t* ticket;            // [n_seq] workgroups that have left theirs
+    VerifyTile* chosen;          // [n_seq] the row that such a sum is formed of, joined, its number in `best`; -1: none
     double rise;                 // scale * log2(e); 0: the largest entry alone counts
     int vocab, n_tile;
 };
@@ -59,6 +59,24 @@ __device__ __forceinline__ double exp2_64(double y) {
     p = __builtin_fma(p, f, c1);
     p = __builtin_fma(p, f, 1.0);
     return __builtin_amdgcn_ldexp(p, (int)n);
+}
+
+// 2^(t / 64) for t from -64000 to 64, from a table of 2^(i / 64): the series around the nearest whole number is off by (0.0055)^5 / 5! = 4e-14.
+// A tile's weights are formed by it, which are the most of all that is to be computed (256 rows of 131,072 entries, by exp2_64 37 us)
+constexpr int kPowers = 64;
+__device__ __forceinline__ double exp2_by(const double* table, double t) {
+    const double shifted = t + 0x1.8p52, f = t - (shifted - 0x1.8p52);      // the whole number is in the low bits
+    const int n = (int)__builtin_bit_cast(long long, shifted);
+    constexpr double kLn2 = 0.693147180559945309417 / kPowers;
+    constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4;
+    double p = __builtin_fma(c4, f, c3);
+    p = __builtin_fma(p, f, c2);
+    p = __builtin_fma(p, f, c1);
+    // n / 64 into the exponent, which stays a normal number's
+    const unsigned long long raw = __builtin_bit_cast(unsigned long long, table[n & (kPowers - 1)]);
+    const uint32_t hi = (uint32_t)(raw >> 32) + ((uint32_t)(n & -kPowers) << 14);
+    const double b = __builtin_bit_cast(double, (unsigned long long)hi << 32 | (uint32_t)raw);
+    return __builtin_fma(b * f, p, b);
 }
 
 template <typename T> __device__ __forceinline__ float entry_of(const void* logits, int64_t at) {
@@ -98,56 +116,74 @@ template <typename T> __device__ __forceinline__ float unpack(const u4_t& v, int
     else return __uint_as_float(e & 1 ? v[e / 2] & 0xFFFF0000u : v[e / 2] << 16);
 }
 
-// A wavefront per tile: its largest entry, then its weights, from registers.  Entry e of load i of a lane is entry (i * 64 + lane) * kPerLoad + e.
-template <typename T>
-__global__ __launch_bounds__(kVerifyWaves * 64) void verify_tiles_kernel(VerifyArgs a) {
+// A lane's kVerifyRun entries of a tile that begins at entry i0 of x, spread so that the lanes' loads lie side by side; `fill` behind the row's end.
+template <typename T> __device__ __forceinline__ int place_in_tile(int i) {
+    constexpr int kPer = kPerLoad<T>;
+    return (i / kPer * 64 + lane_id()) * kPer + i % kPer;
+}
+template <typename T> __device__ __forceinline__ void load_tile(const T* x, int i0, int vocab, float fill, float (&v)[kVerifyRun]) {
     constexpr int kPer = kPerLoad<T>, kLoads = kVerifyRun / kPer;
-    for (int64_t i = (int64_t)blockIdx.x * (kVerifyWaves * 64) + threadIdx.x; i < a.step.n_seq; i += (int64_t)gridDim.x * (kVerifyWaves * 64)) a.ticket[i] = 0;
-    const int lane = lane_id(), per_row = (a.n_tile + kVerifyWaves - 1) / kVerifyWaves;
-    const int row = blockIdx.x / per_row, tile = blockIdx.x % per_row * kVerifyWaves + wave_id();
-    if (tile >= a.n_tile) return;
-    const T* x = (const T*)a.logits + row * a.row_stride;
-    const int i0 = tile * kVerifyTile + lane * kPer;
-    float v[kVerifyRun], top = -INFINITY;
-    u4_t raw[kLoads];
-    if ((tile + 1) * kVerifyTile <= a.vocab) {
+    if (i0 + kVerifyTile <= vocab) {
+        u4_t raw[kLoads];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) raw[i] = *(const u4_any_t*)(x + i0 + i * 64 * kPer);
+        for (int i = 0; i < kLoads; ++i) raw[i] = *(const u4_any_t*)(x + i0 + place_in_tile<T>(i * kPer));
 #pragma unroll
         for (int i = 0; i < kVerifyRun; ++i) v[i] = unpack<T>(raw[i / kPer], i % kPer);
     } else {
 #pragma unroll
         for (int i = 0; i < kVerifyRun; ++i) {
-            const int at = i0 + i / kPer * 64 * kPer + i % kPer;
-            v[i] = at < a.vocab ? (float)x[at] : -INFINITY;
+            const int at = i0 + place_in_tile<T>(i);
+            v[i] = at < vocab ? (float)x[at] : fill;
         }
     }
+}
+
+// A wavefront per tile: its largest entry, then its weights, from registers.
+template <typename T>
+__global__ __launch_bounds__(kVerifyWaves * 64, 6) void verify_tiles_kernel(VerifyArgs a) {
+    const int per_row = (a.n_tile + kVerifyWaves - 1) / kVerifyWaves;
+    const int row = blockIdx.x / per_row, tile = blockIdx.x % per_row * kVerifyWaves + wave_id();
+    float v[kVerifyRun], top = -INFINITY;
+    load_tile((const T*)a.logits + row * a.row_stride, tile * kVerifyTile, a.vocab, -INFINITY, v);
 #pragma unroll
     for (int i = 0; i < kVerifyRun; ++i) top = fmaxf(top, v[i]);          // NaN counts for nothing
     top = lanes_max(top);
     VerifyTile out = {0.0, top, -1};
+    __shared__ double s_powers[kPowers];
+    if (threadIdx.x < kPowers) s_powers[threadIdx.x] = exp2_64(threadIdx.x / (double)kPowers);
+    __syncthreads();
     if (a.rise == 0.0) {
         int best = 0x7FFFFFFF;
 #pragma unroll
         for (int i = kVerifyRun - 1; i >= 0; --i)
-            if (v[i] == top) best = i0 + i / kPer * 64 * kPer + i % kPer;
+            if (v[i] == top) best = min(best, tile * kVerifyTile + place_in_tile<T>(i));
         for (int w = 32; w >= 1; w >>= 1) best = min(best, __shfl_xor(best, w));
         if (top > -INFINITY) out.best = best;
     } else if (top > -INFINITY) {
         double sum = 0.0;
+        if (top == INFINITY) {
 #pragma unroll
-        for (int i = 0; i < kVerifyRun; ++i) sum += weight_of(v[i], top, a.rise);
+            for (int i = 0; i < kVerifyRun; ++i) sum += v[i] == INFINITY ? 1.0 : 0.0;
+        } else {
+            // weights below 2^-1000 are nothing beside the largest's, which is 1: entries there, and NaN, may be what gives that
+            const double by = a.rise * kPowers, less = by * (double)top;
+            const float least = fmaxf((float)((double)top - 990.0 / a.rise), -0x1.fffffep127f);
+#pragma unroll
+            for (int i = 0; i < kVerifyRun; ++i) sum += exp2_by(s_powers, __builtin_fma((double)fmaxf(v[i], least), by, -less));
+        }
         out.sum = lanes_sum(sum);
     }
-    if (lane == 0) a.tiles[(int64_t)row * a.n_tile + tile] = out;
+    if (lane_id() == 0 && tile < a.n_tile) a.tiles[(int64_t)row * a.n_tile + tile] = out;
 }
 
-// A row's tiles joined, by a wavefront
-__device__ __forceinline__ VerifyTile join_tiles(const VerifyArgs& a, int64_t row) {
+// A row's tiles joined, by a wavefront; `t`: the lane's of the first 64, which the caller has requested
+__device__ __forceinline__ VerifyTile tile_of(const VerifyArgs& a, int64_t row, int i) {
+    return i < a.n_tile ? a.tiles[row * a.n_tile + i] : VerifyTile{0.0, -INFINITY, -1};
+}
+__device__ __forceinline__ VerifyTile join_tiles(const VerifyArgs& a, int64_t row, VerifyTile t) {
     VerifyTile all = {0.0, -INFINITY, -1};
-    const VerifyTile* tiles = a.tiles + row * a.n_tile;
     for (int i0 = 0; i0 < a.n_tile; i0 += 64) {
-        const VerifyTile t = i0 + lane_id() < a.n_tile ? tiles[i0 + lane_id()] : VerifyTile{0.0, -INFINITY, -1};
+        if (i0 > 0) t = tile_of(a, row, i0 + lane_id());
         const float top = fmaxf(all.top, lanes_max(t.top));
         if (a.rise == 0.0) {
             if (top > all.top) all.best = __shfl(t.best, __builtin_ctzll(__ballot(t.top == top)));
@@ -162,143 +198,225 @@ __device__ __forceinline__ VerifyTile join_tiles(const VerifyArgs& a, int64_t ro
 
 // The weights that a sequence's next token is drawn from
 template <typename T> struct Weights {
-    const VerifyArgs& a;
-    int64_t logits, draft;                                // where the rows begin; draft -1: none
-    int without;                                          // a token that is left out
+    const T* logits;                                      // the row
+    const float* draft;                                   // its draft's, or NULL
+    int vocab, without;                                   // a token that is left out, or -1
     float top;
-    double whole;
-    __device__ __forceinline__ double operator()(int i) const {
-        const double w = i == without ? 0.0 : weight_of(entry_of<T>(a.logits, logits + i), top, a.rise);
-        if (draft < 0) return w;
-        const float d = a.draft[draft + i];
-        return fmax(w - whole * (double)(d > 0.f ? d : 0.f), 0.0);
+    double whole, rise;
+    // of N entries from i0 on; 0 behind the row's end
+    template <int N> __device__ __forceinline__ void operator()(int i0, double (&w)[N]) const {
+        float x[N], d[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = i0 + i < vocab ? (float)logits[i0 + i] : -INFINITY;
+            d[i] = draft && i0 + i < vocab ? draft[i0 + i] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = i0 + i == without ? 0.0 : one(x[i], d[i]);
+    }
+    __device__ __forceinline__ double one(float x, float d) const {
+        const double w = weight_of(x, top, rise);
+        return draft ? fmax(w - whole * (double)fmaxf(d, 0.f), 0.0) : w;
     }
 };
 
-// By a wavefront: the first of n entries from i0 on at which the running sum, `run` before them, is above `reach`; the last of any weight where
-// rounding lets none be; -1: no weight at all.
-template <typename W> __device__ __forceinline__ int draw_in_tile(const W& weights, int i0, int n, double run, double reach) {
-    const int lane = lane_id();
-    double mine = 0.0;
-    for (int i = lane * kVerifyRun; i < min(n, (lane + 1) * kVerifyRun); ++i) mine += weights(i0 + i);
-    const double upto = run + lanes_prefix(mine);
-    const uint64_t some = __ballot(mine > 0.0);
-    if (!some) return -1;
-    const uint64_t above = __ballot(mine > 0.0 && upto > reach);
-    const int l = above ? __builtin_ctzll(above) : 63 - __builtin_clzll(some);
-    run = __shfl(upto - mine, l);
-    // the lane's run, an entry a lane
-    const int i = l * kVerifyRun + lane;
-    const double w = lane < kVerifyRun && i < n ? weights(i0 + i) : 0.0;
-    const double to = run + lanes_prefix(w);
-    const uint64_t any = __ballot(w > 0.0), over = __ballot(w > 0.0 && to > reach);
-    return i0 + l * kVerifyRun + (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any));
+// A draw by a workgroup of kDrawWaves: sums up to every thread, and the first thread whose sum is above what is to be reached.
+constexpr int kDrawWaves = 8, kDrawThreads = kDrawWaves * 64, kDrawRun = kVerifyTile / kDrawThreads;
+struct DrawShared {
+    double part[kDrawWaves], before;
+    int first, last, token;
+};
+__device__ __forceinline__ double draw_prefix(DrawShared& sh, double x, double& whole) {
+    double upto = lanes_prefix(x), before = 0.0;
+    __syncthreads();
+    if (lane_id() == 63) sh.part[wave_id()] = upto;
+    if (threadIdx.x == 0) { sh.first = 0x7FFFFFFF; sh.last = -1; }
+    __syncthreads();
+    whole = 0.0;
+#pragma unroll
+    for (int w = 0; w < kDrawWaves; ++w) {
+        if (w == wave_id()) before = whole;
+        whole += sh.part[w];
+    }
+    return before + upto;
+}
+// The thread whose `mine` takes the sum above `reach`; the last of any weight where rounding lets none be (none: -1); behind draw_prefix
+__device__ __forceinline__ int draw_thread(DrawShared& sh, double mine, double upto, double reach, double& before) {
+    const uint64_t some = __ballot(mine > 0.0), above = __ballot(mine > 0.0 && upto > reach);
+    if (lane_id() == 0) {
+        if (above) atomicMin(&sh.first, wave_id() * 64 + __builtin_ctzll(above));
+        if (some) atomicMax(&sh.last, wave_id() * 64 + 63 - __builtin_clzll(some));
+    }
+    __syncthreads();
+    const int at = sh.first != 0x7FFFFFFF ? sh.first : sh.last;
+    if ((int)threadIdx.x == at) sh.before = upto - mine;
+    __syncthreads();
+    before = sh.before;
+    return at;
+}
+// The token that follows; left: the tiles' sums where a draft's probabilities are subtracted; row: that of the weights
+template <typename T> __device__ __forceinline__ int draw(const VerifyArgs& a, DrawShared& sh, Weights<T> weights, int64_t row, const double* left, float uniform) {
+    for (int tries = 0; tries < 2; ++tries) {
+        // the tile of a token that is left out is summed anew: less that token's weight its sum may lose all that is left
+        const int at = weights.without < 0 ? -1 : weights.without / kVerifyTile;
+        auto sum_of = [&](int i) {
+            if (weights.draft) return i < a.n_tile ? left[i] : 0.0;
+            const VerifyTile x = tile_of(a, row, i);
+            return x.top == -INFINITY ? 0.0 : x.sum * weight_of(x.top, weights.top, a.rise);
+        };
+        double mine = sum_of(threadIdx.x), anew = 0.0, w[kDrawRun], whole, part;
+        if (at >= 0) {
+            weights(at * kVerifyTile + threadIdx.x * kDrawRun, w);
+            double x = 0.0;
+#pragma unroll
+            for (int i = 0; i < kDrawRun; ++i) x += w[i];
+            draw_prefix(sh, x, anew);
+            if ((int)threadIdx.x == at) mine = anew;
+        }
+        double upto = draw_prefix(sh, mine, whole);
+        for (int i0 = kDrawThreads; i0 < a.n_tile; i0 += kDrawThreads) {
+            const int i = i0 + threadIdx.x;
+            draw_prefix(sh, i == at ? anew : sum_of(i), part);
+            whole += part;
+        }
+        if (whole > 0.0) {
+            const double reach = (double)uniform * whole;
+            double run = 0.0, before = 0.0;
+            int tile = -1;
+            for (int i0 = 0; i0 < a.n_tile; i0 += kDrawThreads) {
+                const int i = i0 + threadIdx.x;
+                if (a.n_tile > kDrawThreads) {
+                    mine = i == at ? anew : sum_of(i);
+                    upto = run + draw_prefix(sh, mine, part);
+                }
+                double from;
+                const int here = draw_thread(sh, mine, upto, reach, from);
+                if (here >= 0) { tile = i0 + here; before = from; }
+                if (sh.first != 0x7FFFFFFF) break;
+                run += part;
+            }
+            weights(tile * kVerifyTile + threadIdx.x * kDrawRun, w);
+            mine = 0.0;
+#pragma unroll
+            for (int i = 0; i < kDrawRun; ++i) mine += w[i];
+            upto = before + draw_prefix(sh, mine, part);
+            double at_run;
+            const int here = draw_thread(sh, mine, upto, reach, at_run);
+            if ((int)threadIdx.x == here) {
+                int found = 0;
+                bool over = false;
+#pragma unroll
+                for (int i = 0; i < kDrawRun; ++i) {
+                    at_run += w[i];
+                    if (!over && w[i] > 0.0) { found = i; over = at_run > reach; }
+                }
+                sh.token = tile * kVerifyTile + here * kDrawRun + found;
+            }
+            __syncthreads();
+            return here < 0 ? -1 : sh.token;
+        }
+        weights.draft = nullptr;                          // nothing is left: from p itself
+        weights.without = -1;
+    }
+    return -1;
 }
 
-// The accepted drafts of a sequence, and the token that follows.  One workgroup, or, where a second pass over a row may be needed, one for every
-// kVerifyWaves tiles, all of which find the same; the last one to leave its sums draws.
+// A workgroup per sequence: the accepted drafts, by a wavefront a row, and the token that follows where no draft's probabilities are to be
+// subtracted; else the row and what is known of it, for the two kernels below.
 template <typename T>
-__global__ __launch_bounds__(kVerifyWaves * 64) void verify_pick_kernel(VerifyArgs a, int parts) {
+__global__ __launch_bounds__(kDrawThreads) void verify_decide_kernel(VerifyArgs a) {
     __shared__ int s_refused;
-    __shared__ uint32_t s_ticket;
     __shared__ VerifyTile s_row[kVerifyRows];
-    const int s = blockIdx.x / parts, part = blockIdx.x % parts, lane = lane_id(), wave = wave_id();
+    __shared__ DrawShared s_draw;
+    const int s = blockIdx.x, lane = lane_id(), wave = wave_id();
     const int t0 = token_of(a.step, s), count = max(0, token_of(a.step, s + 1) - t0);
     if (threadIdx.x == 0) s_refused = max(1, count);
     __syncthreads();
-    for (int i = wave; i < count; i += kVerifyWaves) {
-        const VerifyTile row = join_tiles(a, t0 + i);
-        if (i < kVerifyRows && lane == 0) s_row[i] = row;
+    for (int i = wave; i < count; i += kDrawWaves) {
         const int t = t0 + i + 1;
-        if (i + 1 == count) break;
-        const int token = a.tokens[t];
-        bool ok = token >= 0 && token < a.vocab && row.top > -INFINITY;
-        if (a.rise == 0.0) {
-            ok = ok && token == row.best;
-        } else if (ok) {
-            const float d = a.draft ? a.draft[t * a.draft_stride + token] : 1.f;
-            const double w = weight_of(entry_of<T>(a.logits, (t - 1) * a.row_stride + token), row.top, a.rise);
-            ok = (double)a.uniform[t] * (double)(d > 0.f ? d : 0.f) * row.sum < w;
+        const bool drafted = i + 1 < count;
+        const VerifyTile first = tile_of(a, t - 1, lane);
+        const int token = drafted ? a.tokens[t] : -1;
+        const bool known = token >= 0 && token < a.vocab;
+        float x = 0.f, d = 1.f, u = 0.f;
+        if (known && a.rise != 0.0) {
+            x = entry_of<T>(a.logits, (t - 1) * a.row_stride + token);
+            if (a.draft) d = a.draft[t * a.draft_stride + token];
+            u = a.uniform[t];
         }
-        if (!ok && lane == 0) atomicMin(&s_refused, i + 1);
+        const VerifyTile row = join_tiles(a, t - 1, first);
+        if (i < kVerifyRows && lane == 0) s_row[i] = row;
+        bool ok = known && row.top > -INFINITY;
+        if (a.rise == 0.0) ok = ok && token == row.best;
+        else ok = ok && (double)u * (double)fmaxf(d, 0.f) * row.sum < weight_of(x, row.top, a.rise);
+        if (drafted && !ok && lane == 0) atomicMin(&s_refused, i + 1);
     }
     __syncthreads();
     const int n = s_refused - 1, t = t0 + n;
     const bool refused = n + 1 < count;
-    if (part == 0 && threadIdx.x == 0) {
+    const VerifyTile row = count == 0 ? VerifyTile{0.0, -INFINITY, -1} : n < kVerifyRows ? s_row[n] : join_tiles(a, t, tile_of(a, t, lane));
+    const bool later = refused && a.draft && a.rise != 0.0 && row.top > -INFINITY;
+    if (threadIdx.x == 0) {
         a.accepted[s] = n;
         a.len_out[s] = a.step.len[s] - max(0, count - 1 - n);
+        if (a.draft && a.rise != 0.0) a.chosen[s] = VerifyTile{row.sum, row.top, later ? t : -1};
     }
-    const VerifyTile row = count == 0 ? VerifyTile{0.0, -INFINITY, -1} : n < kVerifyRows ? s_row[n] : join_tiles(a, t);
-    const bool second = refused && a.draft && a.rise != 0.0 && row.top > -INFINITY;
-    if (!second && part > 0) return;
-    Weights<T> weights = {a, t * a.row_stride, -1, -1, row.top, row.sum};
-    double* left = a.left + (int64_t)s * a.n_tile;
-    if (second) {
-        weights.draft = (t + 1) * a.draft_stride;
-        const int tile = part * kVerifyWaves + wave;
-        if (tile < a.n_tile) {
-            double sum = 0.0;
-            for (int i = tile * kVerifyTile + lane; i < min(a.vocab, (tile + 1) * kVerifyTile); i += 64) sum += weights(i);
-            sum = lanes_sum(sum);
-            if (lane == 0) left[tile] = sum;
-        }
-        if (parts > 1) {
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) s_ticket = atomicAdd(&a.ticket[s], 1u);
-            __syncthreads();
-            if (s_ticket != (uint32_t)parts - 1) return;
-            __threadfence();
-        } else {
-            __syncthreads();
-        }
-    }
-    if (wave > 0) return;
+    if (later) return;
     int token = -1;
     if (a.rise == 0.0) {
         token = row.best;
     } else if (row.top > -INFINITY) {
-        const VerifyTile* tiles = a.tiles + (int64_t)t * a.n_tile;
-        if (refused && !second) weights.without = a.tokens[t + 1];
-        if (weights.without >= a.vocab) weights.without = -1;
-        for (int tries = 0; tries < 2 && token < 0; ++tries) {           // where nothing is left, from p itself
-            const bool from_left = second && tries == 0;
-            if (tries == 1) { weights.draft = -1; weights.without = -1; }
-            // the sum of the tile of the token that is left out, anew: less its weight it may lose what is left
-            double anew = 0.0;
-            const int at = weights.without < 0 ? -1 : weights.without / kVerifyTile;
-            if (at >= 0) {
-                for (int i = at * kVerifyTile + lane; i < min(a.vocab, (at + 1) * kVerifyTile); i += 64) anew += weights(i);
-                anew = lanes_sum(anew);
-            }
-            auto sum_of = [&](int i) {
-                if (i >= a.n_tile) return 0.0;
-                if (from_left) return left[i];
-                const VerifyTile x = tiles[i];
-                return i == at ? anew : x.top == -INFINITY ? 0.0 : x.sum * weight_of(x.top, row.top, a.rise);
-            };
-            double whole = 0.0;
-            for (int i0 = 0; i0 < a.n_tile; i0 += 64) whole += __shfl(lanes_prefix(sum_of(i0 + lane)), 63);
-            if (!(whole > 0.0)) continue;
-            const double reach = (double)a.uniform[t0] * whole;
-            double run = 0.0, before = 0.0;
-            int tile = -1;
-            for (int i0 = 0; i0 < a.n_tile; i0 += 64) {
-                const double mine = sum_of(i0 + lane), upto = run + lanes_prefix(mine);
-                const uint64_t some = __ballot(mine > 0.0), above = __ballot(mine > 0.0 && upto > reach);
-                if (some) {
-                    const int l = above ? __builtin_ctzll(above) : 63 - __builtin_clzll(some);
-                    tile = i0 + l;
-                    before = __shfl(upto - mine, l);
-                }
-                if (above) break;
-                run = __shfl(upto, 63);
-            }
-            token = draw_in_tile(weights, tile * kVerifyTile, min(kVerifyTile, a.vocab - tile * kVerifyTile), before, reach);
+        int without = refused ? a.tokens[t + 1] : -1;
+        if (without >= a.vocab) without = -1;
+        const Weights<T> weights = {(const T*)a.logits + t * a.row_stride, nullptr, a.vocab, without, row.top, row.sum, a.rise};
+        token = draw(a, s_draw, weights, t, nullptr, a.uniform[t0]);
+    }
+    if (threadIdx.x == 0) a.follows[s] = token;
+}
+
+template <typename T> __device__ __forceinline__ Weights<T> weights_left(const VerifyArgs& a, const VerifyTile& chosen) {
+    const int64_t t = chosen.best;
+    return {(const T*)a.logits + t * a.row_stride, a.draft + (t + 1) * a.draft_stride, a.vocab, -1, chosen.top, chosen.sum, a.rise};
+}
+
+// A wavefront per tile of the rows whose draft's probabilities are subtracted
+template <typename T>
+__global__ __launch_bounds__(kVerifyWaves * 64) void verify_left_kernel(VerifyArgs a) {
+    const int per_row = (a.n_tile + kVerifyWaves - 1) / kVerifyWaves;
+    const int s = blockIdx.x / per_row, tile = blockIdx.x % per_row * kVerifyWaves + wave_id(), i0 = tile * kVerifyTile;
+    const VerifyTile chosen = a.chosen[s];
+    if (chosen.best < 0 || tile >= a.n_tile) return;
+    const Weights<T> weights = weights_left<T>(a, chosen);
+    float x[kVerifyRun], d[kVerifyRun];
+    load_tile(weights.logits, i0, a.vocab, -INFINITY, x);
+    // the draft's entries in the places of the logits'
+#pragma unroll
+    for (int i = 0; i < kVerifyRun; i += 4) {
+        const int at = i0 + place_in_tile<T>(i);
+        if (i0 + kVerifyTile <= a.vocab) {
+            const u4_t y = *(const u4_any_t*)(weights.draft + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[i + e] = __uint_as_float(y[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[i + e] = at + e < a.vocab ? weights.draft[at + e] : 0.f;
         }
     }
-    if (lane == 0) a.follows[s] = token;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kVerifyRun; ++i) sum += weights.one(x[i], d[i]);
+    sum = lanes_sum(sum);
+    if (lane_id() == 0) a.left[(int64_t)s * a.n_tile + tile] = sum;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyArgs a) {
+    __shared__ DrawShared s_draw;
+    const int s = blockIdx.x;
+    const VerifyTile chosen = a.chosen[s];
+    if (chosen.best < 0) return;
+    const int token = draw(a, s_draw, weights_left<T>(a, chosen), chosen.best, a.left + (int64_t)s * a.n_tile, a.uniform[token_of(a.step, s)]);
+    if (threadIdx.x == 0) a.follows[s] = token;
 }
 
 static int check_verify(int n_seq, int n_tokens, int vocab) {
@@ -312,9 +430,13 @@ static int check_verify(int n_seq, int n_tokens, int vocab) {
 }
 
 template <typename T> static void launch_verify(const VerifyArgs& a, hipStream_t s) {
-    const int per_row = (a.n_tile + kVerifyWaves - 1) / kVerifyWaves, parts = a.draft && a.rise != 0.0 ? per_row : 1;
-    hipLaunchKernelGGL(verify_tiles_kernel<T>, dim3((unsigned)((int64_t)a.step.n_tokens * per_row)), dim3(kVerifyWaves * 64), 0, s, a);
-    hipLaunchKernelGGL(verify_pick_kernel<T>, dim3((unsigned)((int64_t)a.step.n_seq * parts)), dim3(kVerifyWaves * 64), 0, s, a, parts);
+    const int64_t per_row = (a.n_tile + kVerifyWaves - 1) / kVerifyWaves;
+    const dim3 block(kVerifyWaves * 64);
+    hipLaunchKernelGGL(verify_tiles_kernel<T>, dim3((unsigned)(a.step.n_tokens * per_row)), block, 0, s, a);
+    hipLaunchKernelGGL(verify_decide_kernel<T>, dim3(a.step.n_seq), dim3(kDrawThreads), 0, s, a);
+    if (!a.draft || a.rise == 0.0) return;
+    hipLaunchKernelGGL(verify_left_kernel<T>, dim3((unsigned)(a.step.n_seq * per_row)), block, 0, s, a);
+    hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(a.step.n_seq), dim3(kDrawThreads), 0, s, a);
 }
 
 }  // namespace ivf
@@ -326,7 +448,7 @@ extern "C" int ivf_verify_workspace(int32_t n_seq, int32_t n_tokens, int32_t voc
     if (rc) return rc;
     if (!bytes) return fail(IVF_EINVAL, "bytes is NULL");
     const size_t n_tile = ((size_t)vocab + kVerifyTile - 1) / kVerifyTile;
-    *bytes = (size_t)n_tokens * n_tile * sizeof(VerifyTile) + (size_t)n_seq * (n_tile * 8 + 4);
+    *bytes = (size_t)n_tokens * n_tile * sizeof(VerifyTile) + (size_t)n_seq * (n_tile * 8 + sizeof(VerifyTile));
     return IVF_OK;
 }
 
@@ -359,8 +481,8 @@ extern "C" int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int
     a.n_tile = (vocab + kVerifyTile - 1) / kVerifyTile;
     a.rise = (double)scale * 1.44269504088896340736;
     a.tiles = (VerifyTile*)workspace;
-    a.left = (double*)(a.tiles + (size_t)a.step.n_tokens * a.n_tile);
-    a.ticket = (uint32_t*)(a.left + (size_t)a.step.n_seq * a.n_tile);
+    a.chosen = a.tiles + (size_t)a.step.n_tokens * a.n_tile;
+    a.left = (double*)(a.chosen + a.step.n_seq);
     hipStream_t s = (hipStream_t)stream;
     if (dtype == IVF_F32) launch_verify<float>(a, s);
     else if (dtype == IVF_F16) launch_verify<_Float16>(a, s);
