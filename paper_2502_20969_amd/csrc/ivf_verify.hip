@@ -61,22 +61,17 @@ __device__ __forceinline__ double exp2_64(double y) {
     return __builtin_amdgcn_ldexp(p, (int)n);
 }
 
-// 2^(t / 64) for t from -64000 to 64, from a table of 2^(i / 64): the series around the nearest whole number is off by (0.0055)^5 / 5! = 4e-14.
-// A tile's weights are formed by it, which are the most of all that is to be computed (256 rows of 131,072 entries, by exp2_64 37 us)
-constexpr int kPowers = 64;
-__device__ __forceinline__ double exp2_by(const double* table, double t) {
-    const double shifted = t + 0x1.8p52, f = t - (shifted - 0x1.8p52);      // the whole number is in the low bits
+// 2^(t / 256) for t = v by - less, `less` a whole number below 2^40 in size, t from -300,000 on, from a table of 2^(i / 256) in LDS: the series
+// around the nearest whole number is off by (0.00136)^4 / 4! = 1.4e-13.  The weights of all entries are formed by it, in 17 instructions
+// each with what is around it (256 rows of 131,072 entries, by exp2_64 37 us).
+constexpr int kPowers = 256;
+__device__ __forceinline__ double exp2_by(const double* table, double v, double by, double less) {
+    const double whole = 0x1.8p52 - less, shifted = __builtin_fma(v, by, whole);     // the whole number is in the low bits
     const int n = (int)__builtin_bit_cast(long long, shifted);
-    constexpr double kLn2 = 0.693147180559945309417 / kPowers;
-    constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4;
-    double p = __builtin_fma(c4, f, c3);
-    p = __builtin_fma(p, f, c2);
-    p = __builtin_fma(p, f, c1);
-    // n / 64 into the exponent, which stays a normal number's
-    const unsigned long long raw = __builtin_bit_cast(unsigned long long, table[n & (kPowers - 1)]);
-    const uint32_t hi = (uint32_t)(raw >> 32) + ((uint32_t)(n & -kPowers) << 14);
-    const double b = __builtin_bit_cast(double, (unsigned long long)hi << 32 | (uint32_t)raw);
-    return __builtin_fma(b * f, p, b);
+    const double f = __builtin_fma(v, by, whole - shifted);
+    constexpr double c1 = 0.693147180559945309417 / kPowers, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3;
+    const double p = __builtin_fma(__builtin_fma(c3, f, c2), f, c1), b = table[n & (kPowers - 1)];
+    return __builtin_amdgcn_ldexp(__builtin_fma(b * f, p, b), n >> 8);
 }
 
 template <typename T> __device__ __forceinline__ float entry_of(const void* logits, int64_t at) {
@@ -150,7 +145,8 @@ __global__ __launch_bounds__(kVerifyWaves * 64, 6) void verify_tiles_kernel(Veri
     top = lanes_max(top);
     VerifyTile out = {0.0, top, -1};
     __shared__ double s_powers[kPowers];
-    if (threadIdx.x < kPowers) s_powers[threadIdx.x] = exp2_64(threadIdx.x / (double)kPowers);
+    static_assert(kPowers == kVerifyWaves * 64, "a power a thread");
+    s_powers[threadIdx.x] = exp2_64(threadIdx.x / (double)kPowers);
     __syncthreads();
     if (a.rise == 0.0) {
         int best = 0x7FFFFFFF;
@@ -165,11 +161,22 @@ __global__ __launch_bounds__(kVerifyWaves * 64, 6) void verify_tiles_kernel(Veri
 #pragma unroll
             for (int i = 0; i < kVerifyRun; ++i) sum += v[i] == INFINITY ? 1.0 : 0.0;
         } else {
-            // weights below 2^-1000 are nothing beside the largest's, which is 1: entries there, and NaN, may be what gives that
-            const double by = a.rise * kPowers, less = by * (double)top;
-            const float least = fmaxf((float)((double)top - 990.0 / a.rise), -0x1.fffffep127f);
+            const double by = a.rise * kPowers, less = rint(by * (double)top);
+            if (fabs(less) < 0x1p40) {
+                // entries whose weights are below 2^-990 of the largest, and NaN, may count as 2^-990
+                const float least = fmaxf((float)((double)top - 990.0 / a.rise), -0x1.fffffep127f);
 #pragma unroll
-            for (int i = 0; i < kVerifyRun; ++i) sum += exp2_by(s_powers, __builtin_fma((double)fmaxf(v[i], least), by, -less));
+                for (int i = 0; i < kVerifyRun; ++i) sum += exp2_by(s_powers, (double)fmaxf(v[i], least), by, less);
+                sum *= exp2_64(__builtin_fma((double)top, by, -less) * (-1.0 / kPowers));
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < kVerifyRun; ++i) {
+                    float x = v[0];
+#pragma unroll
+                    for (int j = 1; j < kVerifyRun; ++j) x = i == j ? v[j] : x;
+                    sum += weight_of(x, top, a.rise);
+                }
+            }
         }
         out.sum = lanes_sum(sum);
     }
