@@ -84,6 +84,12 @@ __device__ __forceinline__ void fetch4(const void* g, uint32_t to) {
 __device__ __forceinline__ void fetch16(const void* base, uint32_t off, uint32_t to) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(off), "s"(base), "s"(to) : "memory");
 }
+// lane l's byte at g as a word to `to` + 4 l
+__device__ __forceinline__ void fetch_byte(const void* g, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ubyte %0, off" :: "v"(g), "s"(to) : "memory");
+}
+// until at most N of the loads, which arrive in order, are on their way
+template <int N> __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory"); }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -96,6 +102,11 @@ typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s4_t* lds_s4;
 typedef __attribute__((address_space(3))) const s8_t* lds_s8;
 typedef __attribute__((address_space(3))) u4_t* lds_u4;
+typedef int i2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i2_t* lds_i2;
+typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+typedef float f4_t __attribute__((ext_vector_type(4)));
+template <typename V> using lds_ptr = __attribute__((address_space(3))) V*;
 
 template <typename T> struct Half;
 template <> struct Half<_Float16> {
@@ -145,12 +156,15 @@ constexpr float kSlack = 8.f;
 template <int D, int NARROW, bool Q8>
 struct Shape {
     static constexpr int kChunks = D <= 64 ? 8 : D <= 128 ? 16 : 32;       // 16-byte chunks of a staged row
+    // Q8 with few rows: tiles stay codes in LDS and are converted where the products take them; with many rows they are converted on the way
+    static constexpr bool kDirect = Q8 && NARROW;
     static constexpr int kLanes = Q8 ? kChunks / 2 : kChunks;              // lanes that load a row, 16 bytes each
-    static constexpr int kPitch = kChunks * 16;
+    static constexpr int kPitch = (kDirect ? kLanes : kChunks) * 16;
     static constexpr int kKeys = NARROW || D > 128 ? 32 : 64;              // keys of a tile
     static constexpr int kWaves = NARROW ? NARROW : 4;
-    static constexpr int kStages = Q8 && NARROW ? 1 : 2;                   // one tile is on its way while one is worked on (Q8: in registers)
-    static constexpr int kTileBytes = kKeys * kPitch * 2;                  // keys, then values
+    static constexpr int kStages = kDirect && D <= 128 ? 3 : 2;            // one tile is on its way (two) while one is worked on
+    static constexpr int kTileBytes = kKeys * kPitch * 2 + (kDirect ? 256 : 0);      // keys, then values; the bytes of their powers, a word each
+    static constexpr int kPowerBytes = kDirect ? 256 : 0;                  // the values' powers of the tile that is worked on
     static constexpr int kRowsPerLoad = 64 / kLanes;
     static constexpr int kWaveRows = NARROW ? kKeys : kKeys / kWaves;      // rows of a tile that a wavefront fetches
     static constexpr int kLoads = kWaveRows / kRowsPerLoad;                // loads for its keys, and as many for its values
@@ -158,7 +172,7 @@ struct Shape {
     static constexpr int kSets = (kLoads + 3) / 4;
     static constexpr int kEntrySlots = 4;                                  // tiles whose table entries are kept: an entry comes three tiles ahead
     static constexpr int kJoinBytes = NARROW ? kWaves * 32 * (D * 4 + 8) : 0;    // to join the wavefronts, in the same place
-    static constexpr int kStageBytes = std::max((NARROW ? kWaves : 1) * kStages * kTileBytes, kJoinBytes);
+    static constexpr int kStageBytes = std::max((NARROW ? kWaves : 1) * (kStages * kTileBytes + kPowerBytes), kJoinBytes);
     static constexpr int kLds = kStageBytes + kWaves * kEntrySlots * kSets * 256;
 };
 
@@ -171,6 +185,14 @@ __device__ __forceinline__ int again(int x) { asm volatile("" : "+v"(x)); return
 template <int CHUNKS> __device__ __forceinline__ int place_swap(int row) {
     return CHUNKS == 8 ? row & 7 : (row & 3) << 2 | (row >> 2 & 3);
 }
+
+// The same of rows of codes, 4, 8 or 16 chunks, so that eight rows 0 - 3 and 8 - 11, and eight in a row, are spread over the banks
+template <int CHUNKS> __device__ __forceinline__ int code_swap(int row) {
+    return CHUNKS == 4 ? (row >> 1 & 1) | ((row >> 2 ^ row >> 3) & 1) << 1 : (row & 3) | ((row >> 2 ^ row >> 3) & 1) << 2;
+}
+// Q8 with few rows: the key whose scores register r of the lanes' lower half has, and the one that lane l % 32 gives the product
+__device__ __forceinline__ constexpr int direct_key(int r) { return 16 * (r >> 3) + (r & 7); }
+__device__ __forceinline__ int direct_row(int l) { return (l & 16) | (l >> 2 & 1) << 3 | (l & 3) | (l >> 3 & 1) << 2; }
 
 // Registers: two workgroups a compute unit, but of heads of 256 one, whose sums and queries alone take 192 (eight wavefronts: a prompt
 // of 8000 tokens 890 us against 803).  What the edge tiles need where a value is not finite decides how many: without it the kernel of many
@@ -249,7 +271,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
     // the window's first key, of a position that may be below 0
     auto first_of = [&](int p) { return max(0, max(p, 0) - (a.window - 1)); };
 
-    unsigned char* stage = s_mem + (NARROW ? wave * S::kStages * S::kTileBytes : 0);
+    unsigned char* stage = s_mem + (NARROW ? wave * (S::kStages * S::kTileBytes + S::kPowerBytes) : 0);
     const uint32_t stage_at = __builtin_amdgcn_readfirstlane(lds_address(stage));
     const int32_t* entries = (const int32_t*)(s_mem + S::kStageBytes + wave * S::kEntrySlots * S::kSets * 256);
     const uint32_t entries_at = __builtin_amdgcn_readfirstlane(lds_address(entries));
@@ -261,10 +283,15 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
     const int value_row = 4 * half + (lane & 15) / 4;
     const int value_place = (S::kKeys + value_row) * S::kPitch + (((2 * (lane >> 4 & 1) + (lane & 3) / 2) ^ place_swap<S::kChunks>(value_row)) << 4) + (lane & 1) * 8;
     constexpr int kRowBit = S::kChunks == 8 ? 0 : 32;
+    // Q8 with few rows: 16 codes of key direct_row(l % 32), chunk 2 j + l / 32; and of values, which are read transposed, eight rows 16 s + 8 (l / 32) and on by
+    // sixteen lanes, chunk 2 b + l / 16 % 2
+    const int direct_place = S::kDirect ? direct_row(lane & 31) * S::kPitch + ((half ^ code_swap<S::kLanes>(direct_row(lane & 31))) << 4) : 0;
+    const int direct_value = S::kDirect ? (S::kKeys + 8 * half + (lane & 15) / 2) * S::kPitch + (((lane >> 4 & 1) ^ code_swap<S::kLanes>(8 * half + (lane & 15) / 2)) << 4) + (lane & 1) * 8 : 0;
 
     // the chunk of a row that a lane fetches by load 0, in bytes; another load's rows change single bits of it
-    const int chunk_place = Q8 ? lane % S::kLanes * 16 : ((lane % S::kChunks) ^ place_swap<S::kChunks>((NARROW ? 0 : wave * S::kWaveRows) + lane / S::kChunks)) * 16;
+    const int chunk_place = S::kDirect ? ((lane % S::kLanes) ^ code_swap<S::kLanes>(lane / S::kLanes)) * 16 : Q8 ? lane % S::kLanes * 16 : ((lane % S::kChunks) ^ place_swap<S::kChunks>((NARROW ? 0 : wave * S::kWaveRows) + lane / S::kChunks)) * 16;
     auto chunk_bytes = [&](int u) {
+        if (S::kDirect) return (uint32_t)(chunk_place ^ (S::kLanes == 4 ? 0 : S::kLanes == 8 ? (u & 1) << 6 : ((u ^ u >> 1) & 1) << 6));
         return Q8 ? (uint32_t)chunk_place : (uint32_t)(chunk_place ^ (S::kChunks == 8 ? 0 : S::kChunks == 16 ? (u & 3) << 4 : (u & 1) << 7 | (u >> 1 & 3) << 4));
     };
     // in registers: a choice between two of the arguments would otherwise be a load, which waits for the tiles on their way
@@ -341,7 +368,11 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         {
             const T* src = (const T*)a.q.data + tok * a.q.token_stride + head * a.q.head_stride + half * 8;
 #pragma unroll
-            for (int s = 0; s < kKeySteps; ++s) q[s] = mine ? *(const s8_t*)(src + s * 16) : s8_t{};
+            for (int s = 0; s < kKeySteps; ++s) {
+                // (Q8 with few rows: a lane's sixteen codes in a row serve two steps)
+                if constexpr (S::kDirect) q[s] = mine ? *(const s8_t*)(src + (s >> 1) * 32 + half * 8 + (s & 1) * 8) : s8_t{};
+                else q[s] = mine ? *(const s8_t*)(src + s * 16) : s8_t{};
+            }
             // waited for here: in the loops below, a wait for them would be one for the tiles on their way
 #pragma unroll
             for (int s = 0; s < kKeySteps; ++s) asm volatile("" : "+v"(q[s]));
@@ -414,11 +445,33 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                 const int j = pre ? key : key - plen;
                 const int in_page = (e & ((1 << up) - 1)) << shift | (j & ((1 << shift) - 1));
                 place[set] = (int64_t)(e >> up) * a.cache.page_bytes + (int64_t)in_page * a.cache.token_bytes;
-                if constexpr (Q8) scale_place[set] = (int64_t)(e >> up) * (int)a.quant.page_stride + (int64_t)in_page * (int)a.quant.token_stride;
+                if constexpr (Q8 && !S::kDirect) scale_place[set] = (int64_t)(e >> up) * (int)a.quant.page_stride + (int64_t)in_page * (int)a.quant.token_stride;
+            }
+            if constexpr (S::kDirect) {
+                // of key l % 32, whose entry another lane has fetched
+                const int r = lane & 31, from = r / (4 * S::kRowsPerLoad) * 64 + r % S::kRowsPerLoad * S::kLanes + r / S::kRowsPerLoad % 4;
+                const int key = min(first_key(i) + r, ke - 1);
+                const bool pre = key < plen;
+                const int shift = pre ? pre_shift : own_shift, up = page_shift - shift;
+                const int e = min(max(entries[(i & (S::kEntrySlots - 1)) * S::kSets * 64 + from], 0), pre ? pre_last : own_last);
+                const int in_page = (e & ((1 << up) - 1)) << shift | ((pre ? key : key - plen) & ((1 << shift) - 1));
+                scale_place[0] = (int64_t)(e >> up) * (int)a.quant.page_stride + (int64_t)in_page * (int)a.quant.token_stride;
             }
         };
         auto fetch_tile = [&](int i) __attribute__((always_inline)) {
-            if constexpr (Q8) {
+            if constexpr (S::kDirect) {
+                const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes;
+#pragma unroll
+                for (int u = 0; u < S::kLoads; ++u) {
+                    const int64_t at = quad_lane(place[u / 4], u & 3) + chunk_bytes(u);        // by all lanes
+                    if (D % 64 == 0 || chunk_bytes(u) < D) {
+                        fetch16(kbase + at, to + u * 1024);
+                        fetch16(vbase + at, to + S::kKeys * S::kPitch + u * 1024);
+                    }
+                }
+                fetch_byte((half ? vscales : kscales) + scale_place[0], to + 2 * S::kKeys * S::kPitch);
+                return;
+            } else if constexpr (Q8) {
 #pragma unroll
                 for (int set = 0; set < S::kSets; ++set) {
                     kbyte[set] = kscales[scale_place[set]];
@@ -452,7 +505,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         // Q8: the codes that arrived, as numbers of the rows' type, to the place that the tile's products read them from.  A lane's 16 codes are
         // two chunks of a row there
         auto put_tile = [&](int i) __attribute__((always_inline)) {
-            if constexpr (Q8) {
+            if constexpr (Q8 && !S::kDirect) {
                 int kp[S::kSets], vp[S::kSets];
 #pragma unroll
                 for (int set = 0; set < S::kSets; ++set) {
@@ -500,6 +553,37 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             f16v_t x[kKeyTiles];
 #pragma unroll
             for (int t = 0; t < kKeyTiles; ++t) x[t] = f16v_t{};
+            // what register r of tile t's scores is, less what all of a lane have in common
+            auto key_index = [](int t, int r) { return S::kDirect ? direct_key(r) : t * 32 + (r & 3) + 8 * (r >> 2); };
+            const int lane_key = (S::kDirect ? 8 : 4) * half;
+            // Q8 with few rows: the powers of the values, in the order of their keys: of f16 the two that a product of two takes; of bf16, which has no such
+            // products, the weights are multiplied by them
+            u4_t half_powers[2];
+            f4_t powers[4];
+            const uint32_t direct_at = tile_at + direct_value;
+            if constexpr (S::kDirect) {
+                const lds_ptr<const int> bytes = (lds_ptr<const int>)(uintptr_t)(tile_at + 2 * S::kKeys * S::kPitch);
+                const uint32_t table = stage_at + S::kStages * S::kTileBytes;
+                u4_t c[D / 32];
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) c[j] = *(lds_ptr<const u4_t>)(uintptr_t)((tile_at + direct_place) ^ (uint32_t)(j << 5));
+                const float kp = power_of(a.quant, bytes[direct_row(lane & 31)]), vp = power_of(a.quant, bytes[32 + (lane & 31)]);
+                if constexpr (std::is_same<T, _Float16>::value) ((lds_ptr<_Float16>)(uintptr_t)table)[lane & 31] = (_Float16)vp;
+                else ((lds_ptr<float>)(uintptr_t)table)[lane & 31] = vp;
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const u4_t k = {from_e4m3<T, false>(c[j][2 * u], kp), from_e4m3<T, true>(c[j][2 * u], kp), from_e4m3<T, false>(c[j][2 * u + 1], kp),
+                                        from_e4m3<T, true>(c[j][2 * u + 1], kp)};
+                        x[0] = H::mfma(__builtin_bit_cast(s8_t, k), q[2 * j + u], x[0]);
+                    }
+#pragma unroll
+                for (int u = 0; u < (std::is_same<T, _Float16>::value ? 2 : 4); ++u) {
+                    if constexpr (std::is_same<T, _Float16>::value) half_powers[u] = *(lds_ptr<const u4_t>)(uintptr_t)(table + (16 * u + 8 * half) * 2);
+                    else powers[u] = *(lds_ptr<const f4_t>)(uintptr_t)(table + (16 * (u / 2) + 8 * half + 4 * (u & 1)) * 4);
+                }
+            } else {
             // reads of LDS run kBatch products ahead: one wavefront's products then hide their latency
             constexpr int kScores = kKeySteps * kKeyTiles;
             auto key = [&](int c) __attribute__((always_inline)) {
@@ -519,19 +603,20 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                     x[(c + u) % kKeyTiles] = H::mfma(k[c / kBatch & 1][u], q[(c + u) / kKeyTiles], x[(c + u) % kKeyTiles]);
             }
             __builtin_amdgcn_sched_barrier(0);
+            }
             auto sees = [&](int j) { return j <= lim && (j >= low || j < sinks); };
             if (!full) {
-                const int to = lim - j0 - 4 * half, from = low - j0 - 4 * half, sunk = sinks - j0 - 4 * half;
+                const int to = lim - j0 - lane_key, from = low - j0 - lane_key, sunk = sinks - j0 - lane_key;
 #pragma unroll
                 for (int t = 0; t < kKeyTiles; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) x[t][r] = t * 32 + (r & 3) + 8 * (r >> 2) <= to ? x[t][r] : -INFINITY;
+                    for (int r = 0; r < 16; ++r) x[t][r] = key_index(t, r) <= to ? x[t][r] : -INFINITY;
                 if (a.window > 0) {
 #pragma unroll
                     for (int t = 0; t < kKeyTiles; ++t)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            const int j = t * 32 + (r & 3) + 8 * (r >> 2);
+                            const int j = key_index(t, r);
                             x[t][r] = j >= from || j < sunk ? x[t][r] : -INFINITY;
                         }
                 }
@@ -565,13 +650,26 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                     const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r + 1], a.scale_log2, minus));
                     sum[0] += w0;
                     sum[1] += w1;
-                    p[t * 2 + r / 8][r % 8] = __builtin_bit_cast(short, (T)w0);
-                    p[t * 2 + r / 8][r % 8 + 1] = __builtin_bit_cast(short, (T)w1);
+                    constexpr bool by_power = S::kDirect && !std::is_same<T, _Float16>::value;
+                    p[t * 2 + r / 8][r % 8] = __builtin_bit_cast(short, (T)(by_power ? w0 * powers[r / 4][r % 4] : w0));
+                    p[t * 2 + r / 8][r % 8 + 1] = __builtin_bit_cast(short, (T)(by_power ? w1 * powers[r / 4][r % 4 + 1] : w1));
                 }
             l += sum[0] + sum[1];
             // V transposed, the keys in the order of p: lane l, element l % 32 of a block of 32, keys 16 s + 4 (l / 32) .. + 4 and
             // eight behind those
+            auto codes = [&](int s, int b) __attribute__((always_inline)) {
+                return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2)(uintptr_t)((direct_at ^ (uint32_t)(b << 5)) + s * 16 * S::kPitch));
+            };
+            auto of_codes = [&](i2_t c, int s) __attribute__((always_inline)) {
+                u4_t v = {from_e4m3<T, false>(c[0], 1.f), from_e4m3<T, true>(c[0], 1.f), from_e4m3<T, false>(c[1], 1.f), from_e4m3<T, true>(c[1], 1.f)};
+                if constexpr (std::is_same<T, _Float16>::value) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2_t, (uint32_t)v[e]) * __builtin_bit_cast(h2_t, (uint32_t)half_powers[s][e]));
+                }
+                return __builtin_bit_cast(s8_t, v);
+            };
             auto value = [&](int s, int b) __attribute__((always_inline)) {
+                if constexpr (S::kDirect) return of_codes(codes(s, b), s);
                 s8_t v;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -604,7 +702,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                             s8_t v = value(s, b), kind, seen;
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
-                                const int j = j0 + 16 * s + (e & 3) + 8 * (e >> 2) + 4 * half;
+                                const int j = j0 + 16 * s + (S::kDirect ? e : (e & 3) + 8 * (e >> 2)) + lane_key;
                                 const uint32_t bits = (uint16_t)v[e];
                                 const bool finite = (bits & H::kExponent) != H::kExponent;
                                 kind[e] = finite ? (short)0 : (bits & 0x7FFFu) != H::kExponent ? of(16384.f) : bits >> 15 ? of(128.f) : of(1.f);
@@ -625,6 +723,23 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                 return;
             }
             constexpr int kSums = kKeyTiles * 2 * kBlocks;
+            if constexpr (S::kDirect) {
+                i2_t v[2][kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) v[0][u] = codes(u / kBlocks, u % kBlocks);
+#pragma unroll
+                for (int c = 0; c < kSums; c += kBatch) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u)
+                        if (c + kBatch + u < kSums) v[(c / kBatch + 1) & 1][u] = codes((c + kBatch + u) / kBlocks, (c + kBatch + u) % kBlocks);
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u)
+                        o[(c + u) % kBlocks] = H::mfma(of_codes(v[c / kBatch & 1][u], (c + u) / kBlocks), p[(c + u) / kBlocks], o[(c + u) % kBlocks]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                return;
+            }
             s8_t v[2][kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) v[0][u] = value(u / kBlocks, u % kBlocks);
@@ -641,8 +756,24 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         };
 
         // Q8 with many rows: a tile is fetched into registers two tiles ahead, and put into LDS one ahead
-        constexpr int kAhead = Q8 && !NARROW ? 2 : 1;
-        if (kAhead == 2) {
+        constexpr int kAhead = Q8 && !NARROW ? 2 : 1, kLocate = S::kDirect ? S::kStages : kAhead + 1;
+        if constexpr (S::kDirect) {
+            // the entries of a tile come before the tile that is as many stages behind it, so that they are there when that one is
+            if (n > 0) {
+#pragma unroll
+                for (int i = 0; i < S::kStages; ++i)
+                    if (i < n) fetch_entries(i);
+                wait_loads();
+#pragma unroll
+                for (int i = 0; i + 1 < S::kStages; ++i)
+                    if (i < n) {
+                        locate(i);
+                        if (i + S::kStages < n) fetch_entries(i + S::kStages);
+                        fetch_tile(i);
+                    }
+                if (S::kStages - 1 < n) locate(S::kStages - 1);
+            }
+        } else if (kAhead == 2) {
             if (paged) {
                 if (n > 0) { entry = page_entry(0); fetch_paged(0); }
                 if (n > 1) entry = page_entry(1);
@@ -674,6 +805,14 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             if (n > 1) locate(1);
         }
         auto arrive = [&](int i) __attribute__((always_inline)) {
+            if constexpr (S::kDirect) {
+                // tile i has arrived: of the loads behind it, those of one tile may be on their way
+                if (S::kStages == 3 && i + 1 < n) wait_but<S::kLoads * 2 + 1>();
+                else wait_loads();
+                if (i + 2 * S::kStages - 1 < n) fetch_entries(i + 2 * S::kStages - 1);
+                if (i + S::kStages - 1 < n) fetch_tile(i + S::kStages - 1);
+                return;
+            }
             wait_loads();                // tile i has arrived
             if (!NARROW) barrier();      // for every wavefront, and the tile before has been read
             if (Q8 && i + kAhead - 1 < n) put_tile(i + kAhead - 1);
@@ -699,12 +838,12 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         for (int i = 0; i < n_full; ++i) {
             arrive(i);
             if (!idle) compute(i, std::true_type{});
-            if (!paged && i + kAhead + 1 < n) locate(i + kAhead + 1);
+            if (!paged && i + kLocate < n) locate(i + kLocate);
         }
         for (int i = n_full; i < n; ++i) {
             arrive(i);
             if (!idle && !unseen(i)) compute(i, std::false_type{});
-            if (!paged && i + kAhead + 1 < n) locate(i + kAhead + 1);
+            if (!paged && i + kLocate < n) locate(i + kLocate);
         }
         l += other_half(l);
 
