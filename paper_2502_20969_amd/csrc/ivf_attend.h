@@ -88,8 +88,6 @@ __device__ __forceinline__ void fetch16(const void* base, uint32_t off, uint32_t
 __device__ __forceinline__ void fetch_byte(const void* g, uint32_t to) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ubyte %0, off" :: "v"(g), "s"(to) : "memory");
 }
-// until at most N of the loads, which arrive in order, are on their way
-template <int N> __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory"); }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -162,7 +160,7 @@ struct Shape {
     static constexpr int kPitch = (kDirect ? kLanes : kChunks) * 16;
     static constexpr int kKeys = NARROW || D > 128 ? 32 : 64;              // keys of a tile
     static constexpr int kWaves = NARROW ? NARROW : 4;
-    static constexpr int kStages = kDirect && D <= 128 ? 3 : 2;            // one tile is on its way (two) while one is worked on
+    static constexpr int kStages = 2;                                      // one tile is on its way while one is worked on
     static constexpr int kTileBytes = kKeys * kPitch * 2 + (kDirect ? 256 : 0);      // keys, then values; the bytes of their powers, a word each
     static constexpr int kPowerBytes = kDirect ? 256 : 0;                  // the values' powers of the tile that is worked on
     static constexpr int kRowsPerLoad = 64 / kLanes;
@@ -199,7 +197,7 @@ __device__ __forceinline__ int direct_row(int l) { return (l & 16) | (l >> 2 & 1
 // rows would take 189 of heads of 128 and 133 of heads of 64, with it 256 and some 200 in scratch memory, and 202.  The loop over inner tiles
 // uses no scratch memory, an edge tile stores and reloads about ten values and waits for the tile on its way each time.
 template <typename T, int D, int NARROW, bool Q8>
-__global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (NARROW && !Q8) ? 1 : 2)) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (NARROW && !Q8) ? 1 : NARROW && D == 64 ? 3 : 2)) void attend_kernel(AttendArgs a) {
     using S = Shape<D, NARROW, Q8>;
     using H = Half<T>;
     constexpr int kKeySteps = D / 16, kBlocks = D / 32, kKeyTiles = S::kKeys / 32;
@@ -210,7 +208,23 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
     const bool second = at >= a.first_blocks;
     const AttendArgs::Pass& pass = a.pass[second];
     if (second) at -= a.first_blocks;
-    const int kvh = at % a.hkv; at /= a.hkv;
+    int kvh;
+    if constexpr (Q8) {
+        // The key heads of a unit's piece to one XCD, to which every eighth workgroup goes: a row of codes of one head, or its powers, may be less
+        // than a line of the L2 cache (heads of 64, tokens one after the other: every line was fetched twice)
+        const int pieces = (second ? (int)gridDim.x - a.first_blocks : a.first_blocks) / a.hkv, whole = pieces & ~7;
+        if (at < whole * a.hkv) {
+            const int x = at & 7, i = at >> 3;
+            kvh = i % a.hkv;
+            at = i / a.hkv * 8 + x;
+        } else {
+            at -= whole * a.hkv;
+            kvh = at % a.hkv;
+            at = whole + at / a.hkv;
+        }
+    } else {
+        kvh = at % a.hkv; at /= a.hkv;
+    }
     int tile0 = 0, split, unit;
     if (pass.n_tile > 0) {
         tile0 = pass.n_tile - 1 - at % pass.n_tile; at /= pass.n_tile;     // the rows that see most first
@@ -268,6 +282,18 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         }
         return plen + own_len(a.step, lo) - (token_of(a.step, lo + 1) - t);
     };
+    // Q8: the same of a group of up to 64 sequences by all lanes, which have read the sequences' tokens and lengths at once
+    const bool by_lanes = Q8 && by_group && s1 - s0 <= 64;
+    const int lane_token = by_lanes ? token_of(a.step, min(s0 + lane, s1)) : 0, lane_end = by_lanes ? token_of(a.step, min(s0 + lane + 1, s1)) : 0;
+    const int lane_len = by_lanes && s0 + lane < s1 ? own_len(a.step, s0 + lane) : 0;
+    auto lane_position = [&](int t) {
+        int at = 0;
+        for (int w = 32; w >= 1; w >>= 1) {
+            const int next = at + w;
+            if (__shfl(lane_token, next & 63) <= t && next < s1 - s0) at = next;
+        }
+        return plen + __shfl(lane_len, at) - (__shfl(lane_end, at) - t);
+    };
     // the window's first key, of a position that may be below 0
     auto first_of = [&](int p) { return max(0, max(p, 0) - (a.window - 1)); };
 
@@ -320,12 +346,25 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         const int row = row_first + (NARROW ? 0 : wave * 32) + (lane & 31);
         const bool mine = row < rows;
         const int tok = t0 + (mine ? row : rows - 1) / G, head = kvh * G + (mine ? row : rows - 1) % G;
-        const int pos = mine ? position(tok) : -1;
+        int pos;
+        if (by_lanes) {
+            pos = lane_position(tok);
+            pos = mine ? pos : -1;
+        } else {
+            pos = mine ? position(tok) : -1;
+        }
         const int lim = min(pos, ke - 1);                                  // sees keys up to lim that are at or above low, or sinks
         const int low = a.window > 0 ? first_of(pos) : 0;
         // over the workgroup's rows (positions rise inside a sequence; over a group, all rows are looked at)
         int most = -1, least = 0x7FFFFFFF;
-        if (by_group) {
+        if (by_lanes) {
+            for (int r0 = row_first; r0 <= row_last; r0 += 64) {
+                const int p = lane_position(t0 + min(r0 + lane, row_last) / G);
+                most = max(most, p);
+                least = min(least, p);
+            }
+            for (int w = 32; w >= 1; w >>= 1) { most = max(most, __shfl_xor(most, w)); least = min(least, __shfl_xor(least, w)); }
+        } else if (by_group) {
             for (int r = row_first + lane; r <= row_last; r += 64) {
                 const int p = position(t0 + r / G);
                 most = max(most, p);
@@ -806,9 +845,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         }
         auto arrive = [&](int i) __attribute__((always_inline)) {
             if constexpr (S::kDirect) {
-                // tile i has arrived: of the loads behind it, those of one tile may be on their way
-                if (S::kStages == 3 && i + 1 < n) wait_but<S::kLoads * 2 + 1>();
-                else wait_loads();
+                wait_loads();
                 if (i + 2 * S::kStages - 1 < n) fetch_entries(i + 2 * S::kStages - 1);
                 if (i + S::kStages - 1 < n) fetch_tile(i + S::kStages - 1);
                 return;
