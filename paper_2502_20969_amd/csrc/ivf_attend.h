@@ -555,11 +555,15 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
 #pragma unroll
                 for (int u = 0; u < S::kLoads; ++u) {
                     const int r = (NARROW ? 0 : wave * S::kWaveRows) + u * S::kRowsPerLoad + lane / S::kLanes;
-                    const uint32_t at = to + r * S::kPitch + ((lane % S::kLanes * 2 ^ place_swap<S::kChunks>(r)) << 4);
+                    const uint32_t at = to + r * S::kPitch + (((lane % S::kLanes * 2 + (S::kLanes > 4 ? lane >> 2 & 1 : 0)) ^ place_swap<S::kChunks>(r)) << 4);
+                    // rows of 8 chunks and more: every other four lanes write their second chunk first, so that eight lanes side by side, whose
+                    // chunks are two apart, do not meet in half of the banks
+                    const bool turn = S::kLanes > 4 && (lane & 4);
                     auto put = [&](const uint4& c, int power, uint32_t at) __attribute__((always_inline)) {
                         const float p = __int_as_float(power);
-                        *(lds_u4)(uintptr_t)at = u4_t{from_e4m3<T, false>(c.x, p), from_e4m3<T, true>(c.x, p), from_e4m3<T, false>(c.y, p), from_e4m3<T, true>(c.y, p)};
-                        *(lds_u4)(uintptr_t)(at ^ 16) = u4_t{from_e4m3<T, false>(c.z, p), from_e4m3<T, true>(c.z, p), from_e4m3<T, false>(c.w, p), from_e4m3<T, true>(c.w, p)};
+                        const uint32_t a0 = turn ? c.z : c.x, a1 = turn ? c.w : c.y, b0 = turn ? c.x : c.z, b1 = turn ? c.y : c.w;
+                        *(lds_u4)(uintptr_t)at = u4_t{from_e4m3<T, false>(a0, p), from_e4m3<T, true>(a0, p), from_e4m3<T, false>(a1, p), from_e4m3<T, true>(a1, p)};
+                        *(lds_u4)(uintptr_t)(at ^ 16) = u4_t{from_e4m3<T, false>(b0, p), from_e4m3<T, true>(b0, p), from_e4m3<T, false>(b1, p), from_e4m3<T, true>(b1, p)};
                     };
                     const int pk = quad_lane(kp[u / 4], u & 3), pv = quad_lane(vp[u / 4], u & 3);
                     if (D % 64 == 0 || chunk_place < D) {
