@@ -209,9 +209,11 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
     const AttendArgs::Pass& pass = a.pass[second];
     if (second) at -= a.first_blocks;
     int kvh;
-    if constexpr (Q8) {
+    if constexpr (S::kDirect) {
         // The key heads of a unit's piece to one XCD, to which every eighth workgroup goes: a row of codes of one head, or its powers, may be less
-        // than a line of the L2 cache (heads of 64, tokens one after the other: every line was fetched twice)
+        // than a line of the L2 cache (heads of 64, tokens one after the other: every line was fetched twice, 40 windows of 4096 keys 67 us, now 55).
+        // Many rows read their keys again and again: there an XCD that has one head of eight keeps it in its cache (a prompt of 8000 tokens: 858 us, by
+        // this 900)
         const int pieces = (second ? (int)gridDim.x - a.first_blocks : a.first_blocks) / a.hkv, whole = pieces & ~7;
         if (at < whole * a.hkv) {
             const int x = at & 7, i = at >> 3;
@@ -282,18 +284,6 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         }
         return plen + own_len(a.step, lo) - (token_of(a.step, lo + 1) - t);
     };
-    // Q8: the same of a group of up to 64 sequences by all lanes, which have read the sequences' tokens and lengths at once
-    const bool by_lanes = Q8 && by_group && s1 - s0 <= 64;
-    const int lane_token = by_lanes ? token_of(a.step, min(s0 + lane, s1)) : 0, lane_end = by_lanes ? token_of(a.step, min(s0 + lane + 1, s1)) : 0;
-    const int lane_len = by_lanes && s0 + lane < s1 ? own_len(a.step, s0 + lane) : 0;
-    auto lane_position = [&](int t) {
-        int at = 0;
-        for (int w = 32; w >= 1; w >>= 1) {
-            const int next = at + w;
-            if (__shfl(lane_token, next & 63) <= t && next < s1 - s0) at = next;
-        }
-        return plen + __shfl(lane_len, at) - (__shfl(lane_end, at) - t);
-    };
     // the window's first key, of a position that may be below 0
     auto first_of = [&](int p) { return max(0, max(p, 0) - (a.window - 1)); };
 
@@ -346,25 +336,12 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         const int row = row_first + (NARROW ? 0 : wave * 32) + (lane & 31);
         const bool mine = row < rows;
         const int tok = t0 + (mine ? row : rows - 1) / G, head = kvh * G + (mine ? row : rows - 1) % G;
-        int pos;
-        if (by_lanes) {
-            pos = lane_position(tok);
-            pos = mine ? pos : -1;
-        } else {
-            pos = mine ? position(tok) : -1;
-        }
+        const int pos = mine ? position(tok) : -1;
         const int lim = min(pos, ke - 1);                                  // sees keys up to lim that are at or above low, or sinks
         const int low = a.window > 0 ? first_of(pos) : 0;
         // over the workgroup's rows (positions rise inside a sequence; over a group, all rows are looked at)
         int most = -1, least = 0x7FFFFFFF;
-        if (by_lanes) {
-            for (int r0 = row_first; r0 <= row_last; r0 += 64) {
-                const int p = lane_position(t0 + min(r0 + lane, row_last) / G);
-                most = max(most, p);
-                least = min(least, p);
-            }
-            for (int w = 32; w >= 1; w >>= 1) { most = max(most, __shfl_xor(most, w)); least = min(least, __shfl_xor(least, w)); }
-        } else if (by_group) {
+        if (by_group) {
             for (int r = row_first + lane; r <= row_last; r += 64) {
                 const int p = position(t0 + r / G);
                 most = max(most, p);
@@ -444,26 +421,18 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         // Q8: the codes of a tile on its way, of the rows that a lane's loads bring, and the powers' bytes of the row whose place it keeps
         uint4 kcode[Q8 ? S::kLoads : 1], vcode[Q8 ? S::kLoads : 1];
         int kbyte[Q8 ? S::kSets : 1], vbyte[Q8 ? S::kSets : 1];
-        auto fetch_paged = [&](int i) __attribute__((always_inline)) {
+        // bytes from the cache's begin (and from that of the powers), of the wavefront's rows of a tile
+        auto page_at = [&](int i, int64_t* scale) __attribute__((always_inline)) {
             const int key = page_key(i);
             const bool pre = key < plen;
             const int shift = pre ? pre_shift : own_shift, up = page_shift - shift, j = pre ? key : key - plen;
             const int e = min(max(entry, 0), pre ? pre_last : own_last);
             const int in_page = (e & ((1 << up) - 1)) << shift | (j & ((1 << shift) - 1));
-            const int64_t at = (int64_t)(e >> up) * a.cache.page_bytes + (int64_t)in_page * a.cache.token_bytes;
-            if constexpr (Q8) {
-                const int64_t sc = (e >> up) * a.quant.page_stride + in_page * a.quant.token_stride + page_scale;
-                static_assert(NARROW || S::kSets == 1, "one set of loads");
-                kbyte[0] = kscales[sc];
-                vbyte[0] = vscales[sc];
-#pragma unroll
-                for (int u = 0; u < S::kLoads; ++u)
-                    if (D % 64 == 0 || chunk_place < D) {
-                        kcode[u] = *(const uint4*)(kbase + at + page_place[u % (NARROW ? 1 : S::kLoads)]);
-                        vcode[u] = *(const uint4*)(vbase + at + page_place[u % (NARROW ? 1 : S::kLoads)]);
-                    }
-                return;
-            }
+            if (Q8) *scale = (int64_t)(e >> up) * (int)a.quant.page_stride + (int64_t)in_page * (int)a.quant.token_stride;
+            return (int64_t)(e >> up) * a.cache.page_bytes + (int64_t)in_page * a.cache.token_bytes;
+        };
+        auto fetch_paged = [&](int i) __attribute__((always_inline)) {
+            const int64_t at = page_at(i, nullptr);
             const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes + wave * S::kWaveRows * S::kPitch;
 #pragma unroll
             for (int u = 0; u < S::kLoads; ++u)
@@ -498,7 +467,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             }
         };
         auto fetch_tile = [&](int i) __attribute__((always_inline)) {
-            if constexpr (S::kDirect) {
+            if constexpr (Q8) {
                 const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes;
 #pragma unroll
                 for (int u = 0; u < S::kLoads; ++u) {
@@ -509,21 +478,6 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                     }
                 }
                 fetch_byte((half ? vscales : kscales) + scale_place[0], to + 2 * S::kKeys * S::kPitch);
-                return;
-            } else if constexpr (Q8) {
-#pragma unroll
-                for (int set = 0; set < S::kSets; ++set) {
-                    kbyte[set] = kscales[scale_place[set]];
-                    vbyte[set] = vscales[scale_place[set]];
-                }
-#pragma unroll
-                for (int u = 0; u < S::kLoads; ++u) {
-                    const int64_t at = quad_lane(place[u / 4], u & 3) + chunk_place;
-                    if (D % 64 == 0 || chunk_place < D) {
-                        kcode[u] = *(const uint4*)(kbase + at);
-                        vcode[u] = *(const uint4*)(vbase + at);
-                    }
-                }
                 return;
             }
             const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes + (NARROW ? 0 : wave * S::kWaveRows * S::kPitch);
@@ -541,37 +495,51 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             }
         };
 
-        // Q8: the codes that arrived, as numbers of the rows' type, to the place that the tile's products read them from.  A lane's 16 codes are
-        // two chunks of a row there
-        auto put_tile = [&](int i) __attribute__((always_inline)) {
+        // Q8 with many rows: a tile's codes on their way to registers.  (One place for both ways to find them: two would each load into registers of their
+        // own, and wait, to copy them)
+        auto fetch_codes = [&](int i) __attribute__((always_inline)) {
             if constexpr (Q8 && !S::kDirect) {
-                int kp[S::kSets], vp[S::kSets];
+                static_assert(S::kSets == 1, "one set of loads");
+                int64_t at[S::kLoads], scale;
+                if (paged) {
+                    const int64_t first = page_at(i, &scale);
+                    scale += page_scale;
 #pragma unroll
-                for (int set = 0; set < S::kSets; ++set) {
-                    kp[set] = __float_as_int(power_of(a.quant, kbyte[set]));
-                    vp[set] = __float_as_int(power_of(a.quant, vbyte[set]));
+                    for (int u = 0; u < S::kLoads; ++u) at[u] = first + page_place[u];
+                } else {
+                    scale = scale_place[0];
+#pragma unroll
+                    for (int u = 0; u < S::kLoads; ++u) at[u] = quad_lane(place[0], u & 3) + chunk_place;       // by all lanes
                 }
-                const uint32_t to = stage_at + (i % S::kStages) * S::kTileBytes;
+                kbyte[0] = kscales[scale];
+                vbyte[0] = vscales[scale];
 #pragma unroll
-                for (int u = 0; u < S::kLoads; ++u) {
-                    const int r = (NARROW ? 0 : wave * S::kWaveRows) + u * S::kRowsPerLoad + lane / S::kLanes;
-                    const uint32_t at = to + r * S::kPitch + (((lane % S::kLanes * 2 + (S::kLanes > 4 ? lane >> 2 & 1 : 0)) ^ place_swap<S::kChunks>(r)) << 4);
-                    // rows of 8 chunks and more: every other four lanes write their second chunk first, so that eight lanes side by side, whose
-                    // chunks are two apart, do not meet in half of the banks
-                    const bool turn = S::kLanes > 4 && (lane & 4);
-                    auto put = [&](const uint4& c, int power, uint32_t at) __attribute__((always_inline)) {
-                        const float p = __int_as_float(power);
-                        const uint32_t a0 = turn ? c.z : c.x, a1 = turn ? c.w : c.y, b0 = turn ? c.x : c.z, b1 = turn ? c.y : c.w;
-                        *(lds_u4)(uintptr_t)at = u4_t{from_e4m3<T, false>(a0, p), from_e4m3<T, true>(a0, p), from_e4m3<T, false>(a1, p), from_e4m3<T, true>(a1, p)};
-                        *(lds_u4)(uintptr_t)(at ^ 16) = u4_t{from_e4m3<T, false>(b0, p), from_e4m3<T, true>(b0, p), from_e4m3<T, false>(b1, p), from_e4m3<T, true>(b1, p)};
-                    };
-                    const int pk = quad_lane(kp[u / 4], u & 3), pv = quad_lane(vp[u / 4], u & 3);
+                for (int u = 0; u < S::kLoads; ++u)
                     if (D % 64 == 0 || chunk_place < D) {
-                        put(kcode[u], pk, at);
-                        put(vcode[u], pv, at + S::kKeys * S::kPitch);
+                        kcode[u] = *(const uint4*)(kbase + at[u]);
+                        vcode[u] = *(const uint4*)(vbase + at[u]);
                     }
+            }
+        };
+        // Q8 with many rows: the codes that arrived by load c (of keys, then of values), as numbers of the rows' type, to the place that the tile's
+        // products read them from.  A lane's 16 codes are two chunks of a row there
+        auto put_codes = [&](int i, int c) __attribute__((always_inline)) {
+            if constexpr (Q8 && !S::kDirect) {
+                const int u = c % S::kLoads, r = wave * S::kWaveRows + u * S::kRowsPerLoad + lane / S::kLanes;
+                const uint32_t at = stage_at + (i % S::kStages) * S::kTileBytes + (c < S::kLoads ? 0 : S::kKeys * S::kPitch) + r * S::kPitch +
+                                    ((lane % S::kLanes * 2 ^ place_swap<S::kChunks>(r)) << 4);
+                const float p = __int_as_float(quad_lane(__float_as_int(power_of(a.quant, c < S::kLoads ? kbyte[0] : vbyte[0])), u & 3));      // by all lanes
+                const uint4 x = c < S::kLoads ? kcode[u] : vcode[u];
+                if (D % 64 == 0 || chunk_place < D) {
+                    *(lds_u4)(uintptr_t)at = u4_t{from_e4m3<T, false>(x.x, p), from_e4m3<T, true>(x.x, p), from_e4m3<T, false>(x.y, p), from_e4m3<T, true>(x.y, p)};
+                    *(lds_u4)(uintptr_t)(at ^ 16) = u4_t{from_e4m3<T, false>(x.z, p), from_e4m3<T, true>(x.z, p), from_e4m3<T, false>(x.w, p), from_e4m3<T, true>(x.w, p)};
                 }
             }
+        };
+        constexpr int kPuts = Q8 && !S::kDirect ? 2 * S::kLoads : 0;
+        auto put_tile = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < kPuts; ++c) put_codes(i, c);
         };
 
         f16v_t o[kBlocks] = {};
@@ -587,7 +555,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         };
 
         // one tile: scores, weights, products; `full`: every row sees all its keys
-        auto compute = [&](int i, auto full_tag) __attribute__((always_inline)) {
+        auto compute = [&](int i, auto full_tag, auto between) __attribute__((always_inline)) {
             constexpr bool full = decltype(full_tag)::value;
             const int j0 = first_key(i);
             const uint32_t tile_at = stage_at + (i % S::kStages) * S::kTileBytes;
@@ -644,6 +612,14 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u)
                     x[(c + u) % kKeyTiles] = H::mfma(k[c / kBatch & 1][u], q[(c + u) / kKeyTiles], x[(c + u) % kKeyTiles]);
+                between(c / kBatch);
+                if constexpr (Q8 && !S::kDirect) {
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) {
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);        // a product,
+                        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);        // and what fits beside it
+                    }
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
             }
@@ -798,8 +774,10 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             __builtin_amdgcn_sched_barrier(0);
         };
 
-        // Q8 with many rows: a tile is fetched into registers two tiles ahead, and put into LDS one ahead
-        constexpr int kAhead = Q8 && !NARROW ? 2 : 1, kLocate = S::kDirect ? S::kStages : kAhead + 1;
+        // Q8 with many rows: a tile is fetched into registers two tiles ahead, and put into LDS one ahead, beside the products of scores, which leave the
+        // vector units free
+        constexpr bool kConvert = Q8 && !S::kDirect;
+        constexpr int kLocate = S::kDirect ? S::kStages : kConvert ? 3 : 2;
         if constexpr (S::kDirect) {
             // the entries of a tile come before the tile that is as many stages behind it, so that they are there when that one is
             if (n > 0) {
@@ -816,24 +794,30 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                     }
                 if (S::kStages - 1 < n) locate(S::kStages - 1);
             }
-        } else if (kAhead == 2) {
-            if (paged) {
-                if (n > 0) { entry = page_entry(0); fetch_paged(0); }
-                if (n > 1) entry = page_entry(1);
-                if (n > 0) put_tile(0);
-                if (n > 1) fetch_paged(1);
-                if (n > 2) entry = page_entry(2);
-            } else if (n > 0) {
+        } else if constexpr (kConvert) {
+            if (n > 0) {
+                if (paged) {
+                    entry = page_entry(0);
+                } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < n) fetch_entries(i);
-                wait_loads();
-                locate(0);
-                fetch_tile(0);
-                if (n > 1) locate(1);
+                    for (int i = 0; i < 4; ++i)
+                        if (i < n) fetch_entries(i);
+                    wait_loads();
+                    locate(0);
+                }
+                fetch_codes(0);
+                if (paged) {
+                    if (n > 1) entry = page_entry(1);
+                } else if (n > 1) {
+                    locate(1);
+                }
                 put_tile(0);
-                if (n > 1) fetch_tile(1);
-                if (n > 2) locate(2);
+                if (n > 1) fetch_codes(1);
+                if (paged) {
+                    if (n > 2) entry = page_entry(2);
+                } else if (n > 2) {
+                    locate(2);
+                }
             }
         } else if (paged) {
             if (n > 0) { entry = page_entry(0); fetch_paged(0); }
@@ -854,16 +838,38 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                 if (i + S::kStages - 1 < n) fetch_tile(i + S::kStages - 1);
                 return;
             }
-            wait_loads();                // tile i has arrived
-            if (!NARROW) barrier();      // for every wavefront, and the tile before has been read
-            if (Q8 && i + kAhead - 1 < n) put_tile(i + kAhead - 1);
-            if (paged) {
-                if (i + kAhead < n) fetch_paged(i + kAhead);
-                if (i + kAhead + 1 < n) entry = page_entry(i + kAhead + 1);
+            if constexpr (kConvert) {
+                barrier();               // for every wavefront: tile i is in LDS, and the tile before has been read
                 return;
             }
-            if (i + kAhead < n) fetch_tile(i + kAhead);
-            if (i + kAhead + 2 < n) fetch_entries(i + kAhead + 2);
+            wait_loads();                // tile i has arrived
+            if (!NARROW) barrier();      // for every wavefront, and the tile before has been read
+            if (paged) {
+                if (i + 1 < n) fetch_paged(i + 1);
+                if (i + 2 < n) entry = page_entry(i + 2);
+                return;
+            }
+            if (i + 1 < n) fetch_tile(i + 1);
+            if (i + 3 < n) fetch_entries(i + 3);
+        };
+        // the next tile, between the products of tile i's scores: piece c of kPuts; then the one behind it, on its way.  (Entries before codes: where these
+        // have arrived those have)
+        auto next_tile = [&](int i, int c) __attribute__((always_inline)) {
+            if constexpr (kConvert) {
+                put_codes(i + 1, c);     // (behind the last tile, what nobody reads: without a choice products and conversions stay in one block)
+                if (c < kPuts - 1) return;
+                if (!paged && i + 4 < n) fetch_entries(i + 4);
+                if (i + 2 < n) fetch_codes(i + 2);
+                if (paged && i + 3 < n) entry = page_entry(i + 3);
+            }
+        };
+        auto work = [&](int i, auto full, bool skip) __attribute__((always_inline)) {
+            if (!skip) {
+                compute(i, full, [&](int c) __attribute__((always_inline)) { next_tile(i, c); });
+            } else {
+#pragma unroll
+                for (int c = 0; c < kPuts; ++c) next_tile(i, c);
+            }
         };
         const bool idle = !NARROW && row_first + wave * 32 >= rows;        // no rows: this wavefront only fetches
         // the keys that some row of the wavefront sees: [0, wave_sinks) and [wave_low, wave_lim]
@@ -878,12 +884,12 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         // two loops, so that what the tiles at the edges need takes no registers from the others
         for (int i = 0; i < n_full; ++i) {
             arrive(i);
-            if (!idle) compute(i, std::true_type{});
+            work(i, std::true_type{}, idle);
             if (!paged && i + kLocate < n) locate(i + kLocate);
         }
         for (int i = n_full; i < n; ++i) {
             arrive(i);
-            if (!idle && !unseen(i)) compute(i, std::false_type{});
+            work(i, std::false_type{}, idle || unseen(i));
             if (!paged && i + kLocate < n) locate(i + kLocate);
         }
         l += other_half(l);
