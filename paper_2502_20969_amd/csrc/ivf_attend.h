@@ -537,6 +537,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             }
         };
         constexpr int kPuts = Q8 && !S::kDirect ? 2 * S::kLoads : 0;
+        static_assert(kPuts == 0 || kPuts == (kKeySteps * kKeyTiles + kBatch - 1) / kBatch, "a piece for each batch of products");
         auto put_tile = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int c = 0; c < kPuts; ++c) put_codes(i, c);
