@@ -63,7 +63,7 @@ __device__ __forceinline__ double exp2_64(double y) {
 
 // 2^(t / 256) for t = v by - less, `less` a whole number below 2^40 in size, t from -300,000 on, from a table of 2^(i / 256) in LDS: the series
 // around the nearest whole number is off by (0.00136)^4 / 4! = 1.4e-13.  The weights of all entries are formed by it, in 17 instructions
-// each with what is around it (256 rows of 131,072 entries, by exp2_64 37 us).
+// each with what is around it (225 rows of 131,072 entries, by exp2_64 37 us, so 23).
 constexpr int kPowers = 256;
 __device__ __forceinline__ double exp2_by(const double* table, double v, double by, double less) {
     const double whole = 0x1.8p52 - less, shifted = __builtin_fma(v, by, whole);     // the whole number is in the low bits
@@ -392,26 +392,45 @@ __global__ __launch_bounds__(kVerifyWaves * 64) void verify_left_kernel(VerifyAr
     const int per_row = (a.n_tile + kVerifyWaves - 1) / kVerifyWaves;
     const int s = blockIdx.x / per_row, tile = blockIdx.x % per_row * kVerifyWaves + wave_id(), i0 = tile * kVerifyTile;
     const VerifyTile chosen = a.chosen[s];
-    if (chosen.best < 0 || tile >= a.n_tile) return;
+    if (chosen.best < 0) return;                          // all wavefronts
     const Weights<T> weights = weights_left<T>(a, chosen);
     float x[kVerifyRun], d[kVerifyRun];
-    load_tile(weights.logits, i0, a.vocab, -INFINITY, x);
-    // the draft's entries in the places of the logits'
+    if (tile < a.n_tile) {
+        load_tile(weights.logits, i0, a.vocab, -INFINITY, x);
+        // the draft's entries in the places of the logits'
 #pragma unroll
-    for (int i = 0; i < kVerifyRun; i += 4) {
-        const int at = i0 + place_in_tile<T>(i);
-        if (i0 + kVerifyTile <= a.vocab) {
-            const u4_t y = *(const u4_any_t*)(weights.draft + at);
+        for (int i = 0; i < kVerifyRun; i += 4) {
+            const int at = i0 + place_in_tile<T>(i);
+            if (i0 + kVerifyTile <= a.vocab) {
+                const u4_t y = *(const u4_any_t*)(weights.draft + at);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[i + e] = __uint_as_float(y[e]);
-        } else {
+                for (int e = 0; e < 4; ++e) d[i + e] = __uint_as_float(y[e]);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[i + e] = at + e < a.vocab ? weights.draft[at + e] : 0.f;
+                for (int e = 0; e < 4; ++e) d[i + e] = at + e < a.vocab ? weights.draft[at + e] : 0.f;
+            }
         }
     }
+    __shared__ double s_powers[kPowers];
+    s_powers[threadIdx.x] = exp2_64(threadIdx.x / (double)kPowers);
+    __syncthreads();
+    if (tile >= a.n_tile) return;
     double sum = 0.0;
+    const double by = a.rise * kPowers, less = rint(by * (double)chosen.top);
+    if (fabs(less) < 0x1p40) {
+        // w and W relative to a power of two near the largest weight; an entry that has no weight must leave nothing
+        const float least = fmaxf((float)((double)chosen.top - 990.0 / a.rise), -0x1.fffffep127f);
+        const double back = exp2_64(__builtin_fma((double)chosen.top, by, -less) * (-1.0 / kPowers)), whole = chosen.sum / back;
 #pragma unroll
-    for (int i = 0; i < kVerifyRun; ++i) sum += weights.one(x[i], d[i]);
+        for (int i = 0; i < kVerifyRun; ++i) {
+            const double w = x[i] > least ? exp2_by(s_powers, (double)fmaxf(x[i], least), by, less) : 0.0;
+            sum += fmax(w - whole * (double)fmaxf(d[i], 0.f), 0.0);
+        }
+        sum *= back;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVerifyRun; ++i) sum += weights.one(x[i], d[i]);
+    }
     sum = lanes_sum(sum);
     if (lane_id() == 0) a.left[(int64_t)s * a.n_tile + tile] = sum;
 }
