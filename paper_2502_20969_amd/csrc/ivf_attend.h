@@ -23,6 +23,14 @@
 // tokens, 32 query and 8 key heads of 128, in 2.04 ms, 1030 TFLOP/s, the matrix units are busy for 52 % of the SIMDs' cycles, vector
 // instructions (those that start products among them) for 47 %; LDS for 26 % of a compute unit's, without bank conflicts.  Heads of 64: 35 % and 56 %, LDS
 // 35 %, half of that by bank conflicts (three prompts, 4250 tokens, behind 6000 keys: 375 us, 650 TFLOP/s).
+//
+// Quantised caches (Q8).  What a key or value stands for, an e4m3 number times the power of two of its token and head, is exact in T, so nothing
+// else changes.  Few rows: tiles are codes in LDS.  A lane reads sixteen codes of a key, which serve two products (the order of elements inside a product is
+// free too), and converts them with the key's power; eight codes of one element of eight values, read transposed, it converts as they are, and the
+// weights (bf16) or the numbers (f16) are multiplied by the values' powers.  LDS carries a third of what it does with tiles of T, and memory bounds it: 24 sequences of
+// up to 60,000 keys as above in 291 us, 5.0 TB/s, the loads alone in 286.  Many rows: every wavefront converts its share of a tile once, between the products of scores, and
+// writes it into LDS, a tile ahead: 8000 tokens behind 2001, 32 query and 8 key heads of 128, in 858 to 925 us (of 16-bit keys and values 824), 850 to 920 TFLOP/s: the
+// conversions are 10 % more vector instructions, and the writes double what LDS does.
 #pragma once
 #include "ivf_answer.h"
 #include "ivf_device.h"

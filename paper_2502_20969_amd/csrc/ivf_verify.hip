@@ -7,6 +7,9 @@
 // the tile's largest entry and its sum of weights relative to that; a row's (top, W) are those of its tiles joined.  A draw looks for the
 // tile, the run of entries inside it, and the entry in turn.  Only a refused draft that was drawn from probabilities needs a second pass
 // over its row, for the sums of max(w - W d, 0).
+//
+// What bounds it: the weights' 64-bit vector instructions (86 % of the SIMDs' cycles).  225 rows of 131,072 bf16 logits: tiles 23 us, the decision 7.6 (a chain of loads: tokens,
+// entries, tiles), what the drafts leave of 64 rows 10, the draw 6.3 (again a chain: sums, a tile).  Five rows of 50,001: 5.3 and 7.1.
 #include "ivf_answer.h"
 #include "ivf_device.h"
 #include <math.h>
@@ -133,7 +136,8 @@ template <typename T> __device__ __forceinline__ void load_tile(const T* x, int 
     }
 }
 
-// A wavefront per tile: its largest entry, then its weights, from registers.
+// A wavefront per tile: its largest entry, then its weights, from registers.  (Two tiles a wavefront, the second on its way meanwhile: 26 us against 23, for the registers leave
+// four wavefronts a SIMD.)
 template <typename T>
 __global__ __launch_bounds__(kVerifyWaves * 64, 6) void verify_tiles_kernel(VerifyArgs a) {
     const int per_row = (a.n_tile + kVerifyWaves - 1) / kVerifyWaves;
