@@ -170,7 +170,32 @@ def test_drawn_tokens_follow_the_target():
         assert ((share - target).abs() <= 5.5 * (target * (1 - target) / n).sqrt()).all()
 
 
-@pytest.mark.parametrize("new,vocab", [([6] * 40, 131072), ([2], 160001), ([9], 1000003)])
+@pytest.mark.parametrize("scale", [1e-20, 1e-3, 50.0, 1e9, 9e29])
+@pytest.mark.parametrize("size", [1.0, 1e4, 1e30])
+def test_scales_and_sizes(scale, size):
+    """Probabilities that are nearly alike, and such of which the largest takes all."""
+    new = [4, 2, 5]
+    logits, tokens, uniform, probs = _problem(new, 5000, "f32", False, 21)
+    logits = logits * size
+    logits[3, 7], logits[8, 9] = 3e38, -3e38
+    logits[5, 100:103] = logits[5].max()
+    _run(new, logits, tokens, uniform, scale=scale)
+    _run(new, logits, tokens, uniform, draft=torch.softmax(torch.randn(11, 5000, generator=torch.Generator().manual_seed(3)), -1), scale=scale)
+
+
+@pytest.mark.parametrize("refused", [2, 31, 32, 33, 69, None])
+def test_many_drafts(refused):
+    """A sequence of more drafts than a workgroup keeps the rows of."""
+    g = torch.Generator().manual_seed(8)
+    logits, tokens = torch.randn(73, 300, generator=g), torch.randint(0, 300, (73,), generator=g)
+    logits[:-1].scatter_(1, tokens[1:, None], 40.0)
+    if refused is not None:
+        logits[1 + refused, tokens[2 + refused]] = -40.0
+    got = _run([1, 70, 2], logits, tokens, torch.rand(73, generator=g))
+    assert got[0].tolist() == [0, 69 if refused in (None, 69) else refused, 1]
+
+
+@pytest.mark.parametrize("new,vocab", [([6] * 40, 131072), ([2], 160001), ([9], 1000003), ([3, 2], 2300001)])
 @pytest.mark.parametrize("draft", [False, True])
 def test_large_vocabularies(new, vocab, draft):
     if draft and vocab == 131072:
