@@ -545,7 +545,6 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             }
         };
         constexpr int kPuts = Q8 && !S::kDirect ? 2 * S::kLoads : 0;
-        static_assert(kPuts == 0 || kPuts == (kKeySteps * kKeyTiles + kBatch - 1) / kBatch, "a piece for each batch of products");
         auto put_tile = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int c = 0; c < kPuts; ++c) put_codes(i, c);
@@ -564,7 +563,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         };
 
         // one tile: scores, weights, products; `full`: every row sees all its keys
-        auto compute = [&](int i, auto full_tag, auto between) __attribute__((always_inline)) {
+        auto compute = [&](int i, auto full_tag) __attribute__((always_inline)) {
             constexpr bool full = decltype(full_tag)::value;
             const int j0 = first_key(i);
             const uint32_t tile_at = stage_at + (i % S::kStages) * S::kTileBytes;
@@ -621,14 +620,6 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u)
                     x[(c + u) % kKeyTiles] = H::mfma(k[c / kBatch & 1][u], q[(c + u) / kKeyTiles], x[(c + u) % kKeyTiles]);
-                between(c / kBatch);
-                if constexpr (Q8 && !S::kDirect) {
-#pragma unroll
-                    for (int u = 0; u < kBatch; ++u) {
-                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);        // a product,
-                        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);        // and what fits beside it
-                    }
-                }
             }
             __builtin_amdgcn_sched_barrier(0);
             }
@@ -783,8 +774,9 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             __builtin_amdgcn_sched_barrier(0);
         };
 
-        // Q8 with many rows: a tile is fetched into registers two tiles ahead, and put into LDS one ahead, beside the products of scores, which leave the
-        // vector units free
+        // Q8 with many rows: a tile is fetched into registers two tiles ahead, and put into LDS one ahead.  (Put piece by piece between the products of
+        // scores a prompt of 8000 tokens took 962 us against 985, but what the edge tiles then stored in scratch memory cost more: windows of 1024 284 against
+        // 239, a prompt of 4000 tokens with heads of 256 481 against 235)
         constexpr bool kConvert = Q8 && !S::kDirect;
         constexpr int kLocate = S::kDirect ? S::kStages : kConvert ? 3 : 2;
         if constexpr (S::kDirect) {
@@ -848,7 +840,12 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                 return;
             }
             if constexpr (kConvert) {
+                wait_loads();            // the codes of tile i + 1 have arrived, and the entries that the next places come from
                 barrier();               // for every wavefront: tile i is in LDS, and the tile before has been read
+                if (i + 1 < n) put_tile(i + 1);
+                if (!paged && i + 4 < n) fetch_entries(i + 4);
+                if (i + 2 < n) fetch_codes(i + 2);
+                if (paged && i + 3 < n) entry = page_entry(i + 3);
                 return;
             }
             wait_loads();                // tile i has arrived
@@ -860,25 +857,6 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             }
             if (i + 1 < n) fetch_tile(i + 1);
             if (i + 3 < n) fetch_entries(i + 3);
-        };
-        // the next tile, between the products of tile i's scores: piece c of kPuts; then the one behind it, on its way.  (Entries before codes: where these
-        // have arrived those have)
-        auto next_tile = [&](int i, int c) __attribute__((always_inline)) {
-            if constexpr (kConvert) {
-                put_codes(i + 1, c);     // (behind the last tile, what nobody reads: without a choice products and conversions stay in one block)
-                if (c < kPuts - 1) return;
-                if (!paged && i + 4 < n) fetch_entries(i + 4);
-                if (i + 2 < n) fetch_codes(i + 2);
-                if (paged && i + 3 < n) entry = page_entry(i + 3);
-            }
-        };
-        auto work = [&](int i, auto full, bool skip) __attribute__((always_inline)) {
-            if (!skip) {
-                compute(i, full, [&](int c) __attribute__((always_inline)) { next_tile(i, c); });
-            } else {
-#pragma unroll
-                for (int c = 0; c < kPuts; ++c) next_tile(i, c);
-            }
         };
         const bool idle = !NARROW && row_first + wave * 32 >= rows;        // no rows: this wavefront only fetches
         // the keys that some row of the wavefront sees: [0, wave_sinks) and [wave_low, wave_lim]
@@ -893,12 +871,12 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
         // two loops, so that what the tiles at the edges need takes no registers from the others
         for (int i = 0; i < n_full; ++i) {
             arrive(i);
-            work(i, std::true_type{}, idle);
+            if (!idle) compute(i, std::true_type{});
             if (!paged && i + kLocate < n) locate(i + kLocate);
         }
         for (int i = n_full; i < n; ++i) {
             arrive(i);
-            work(i, std::false_type{}, idle || unseen(i));
+            if (!idle && !unseen(i)) compute(i, std::false_type{});
             if (!paged && i + kLocate < n) locate(i + kLocate);
         }
         l += other_half(l);
