@@ -28,9 +28,9 @@
 // else changes.  Few rows: tiles are codes in LDS.  A lane reads sixteen codes of a key, which serve two products (the order of elements inside a product is
 // free too), and converts them with the key's power; eight codes of one element of eight values, read transposed, it converts as they are, and the
 // weights (bf16) or the numbers (f16) are multiplied by the values' powers.  LDS carries a third of what it does with tiles of T, and memory bounds it: 24 sequences of
-// up to 60,000 keys as above in 291 us, 5.0 TB/s, the loads alone in 286.  Many rows: every wavefront converts its share of a tile once, between the products of scores, and
-// writes it into LDS, a tile ahead: 8000 tokens behind 2001, 32 query and 8 key heads of 128, in 858 to 925 us (of 16-bit keys and values 824), 850 to 920 TFLOP/s: the
-// conversions are 10 % more vector instructions, and the writes double what LDS does.
+// up to 60,000 keys as above in 291 us, 5.0 TB/s, the loads alone in 286.  Many rows: every wavefront converts its share of a tile once and writes it
+// into LDS, a tile ahead: 8000 tokens behind 2001, 32 query and 8 key heads of 128, in 870 to 985 us where 16-bit keys and values take 800 to 865: the
+// conversions are 10 % more vector instructions, the writes double what LDS does, and the clock falls with the power of both.
 #pragma once
 #include "ivf_answer.h"
 #include "ivf_device.h"

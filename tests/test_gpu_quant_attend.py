@@ -112,6 +112,38 @@ def test_a_value_that_is_no_number_reaches_those_who_see_it(new):
     assert torch.isfinite(out[:, [i for i in range(64) if i != e]]).all()
 
 
+@pytest.mark.parametrize("new,own,hints", [(1, 40, {}), (1, 5000, dict(max_q=1, max_len=5000)), (90, 300, {}), (3, 900, dict(max_q=3, max_len=900))])
+def test_a_query_that_is_no_number(new, own, hints):
+    """NaN in every element of its head and in lse, however the keys are cut; the other heads and tokens keep their results."""
+    pr = Problem8([new, 1], [own, 30], hkv=2, d=128, seed=own)
+    q = pr.rows(4)
+    want, wl, tol = pr.attend(q, pr.d ** -0.5)
+    q[0, 1, 7] = float("nan")
+    lse = torch.zeros(pr.tokens, 4).cuda()
+    out = P.ivf_attend(pr.step(P, **hints), pr.cache(P), q.cuda(), lse=lse).double().cpu().numpy()
+    assert np.isnan(out[0, 1]).all() and bool(torch.isnan(lse[0, 1]))
+    rest = np.ones(out.shape[:2], bool)
+    rest[0, 1] = False
+    assert (np.abs(out - want) <= tol)[rest].all()
+
+
+def test_what_the_cache_holds_is_what_is_read():
+    """Attention over a quantised cache, and over a 16-bit one that holds what ivf_kv_read brings back: of the same numbers, within both's roundings."""
+    for new in (1, 80):
+        pr = Problem8([new, 2], [new + 400, 90], hkv=2, d=64, page=32, dtype="f16", seed=new)
+        q, cache, step = pr.rows(4).cuda(), pr.cache(P), pr.step(P)
+        n = [new + 400, 90]
+        rows = [torch.zeros(sum(n), 2, 64, dtype=torch.float16, device="cuda") for _ in range(2)]
+        P.ivf_kv_read(step, cache, torch.tensor([0, n[0], sum(n)], dtype=torch.int32).cuda(), *rows)
+        flat = P.KvCache(*(x.view(-1, 1, 2, 64) for x in rows))
+        table = torch.zeros(2, n[0], dtype=torch.int32)
+        table[0], table[1, :90] = torch.arange(n[0]), n[0] + torch.arange(90)
+        plain = P.KvStep(step._keep[0], step._keep[1], table.cuda(), page=1, n_tokens=pr.tokens)
+        a, b = (P.ivf_attend(s, c, q).double().cpu().numpy() for s, c in ((step, cache), (plain, flat)))
+        _, _, tol = pr.attend(q.cpu(), 64 ** -0.5)
+        assert (np.abs(a - b) <= 2 * tol).all()
+
+
 def test_rows_that_see_nothing():
     """Fewer own keys than new tokens, and none at all: zeros and -inf."""
     pr = Problem8([3, 40, 2, 1], [3, 40, 2, 5], hkv=1, d=64, seed=6)
