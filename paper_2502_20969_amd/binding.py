@@ -784,22 +784,24 @@ def ivf_verify_draft(step, logits, tokens, uniform=None, draft=None, scale=1.0, 
         if draft.dtype is not t.float32 or draft.get_device() != dev or draft.shape[-1] != vocab:
             raise ValueError("draft must be a float32 tensor [tokens, vocab] on the step's device")
         by_draft, dp = _matrix(draft, n, "draft"), draft.data_ptr()
+    # what comes back is one allocation
     s = step.arg.n_seq
-    out = _new(stream, (2 if lens_out is not None else 3, s), t.int32)
+    out = _new(stream, (3 if lens_out is None else 2, s), t.int32)
+    at = out.data_ptr()
     if lens_out is None:
-        lens_out = out[2]
-    lp = _i32(lens_out, (s,), dev, "lens_out")
+        (accepted, follows, lens_out), lp = out.unbind(0), at + 8 * s
+    else:
+        (accepted, follows), lp = out.unbind(0), _i32(lens_out, (s,), dev, "lens_out")
     need = ivf_verify_workspace(s, n, vocab)
     if workspace is None:
         workspace = _workspace(need, stream)
         wp, wn = workspace.data_ptr(), need
     else:
         wp, wn = _room(workspace, dev)
-    at = out.data_ptr()
     status = load().ivf_verify_draft(step.ref, logits.data_ptr(), stride, dtype, vocab, scale, tp, up, dp, by_draft, at, at + 4 * s, lp, wp, wn, on)
     if status != 0:
         _check(status)
-    return out[0], out[1], lens_out
+    return accepted, follows, lens_out
 
 
 @functools.lru_cache(maxsize=64)             # a function of the sizes alone

@@ -34,8 +34,6 @@ struct QuantView {
 
 // Checks the caller's structures and fills the views; a status, with the error text set.  `qv`: filled for a quantised cache.
 int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv, StepView* sv, QuantView* qv);
-// The type of the rows that go into a cache and come out of it
-inline int row_type(const ivf_kv_cache* cache) { return cache->dtype == IVF_E4M3 ? cache->row_dtype : cache->dtype; }
 // Checks the rows of `what`: pointer, alignment and strides.
 int check_rows(const ivf_rows* r, const char* what);
 

@@ -204,6 +204,7 @@ __device__ __forceinline__ int direct_row(int l) { return (l & 16) | (l >> 2 & 1
 // of 8000 tokens 890 us against 803).  What the edge tiles need where a value is not finite decides how many: without it the kernel of many
 // rows would take 189 of heads of 128 and 133 of heads of 64, with it 256 and some 200 in scratch memory, and 202.  The loop over inner tiles
 // uses no scratch memory, an edge tile stores and reloads about ten values and waits for the tile on its way each time.
+// Q8 with few rows: two wavefronts a SIMD, of heads of 64 three (40 windows of 4096 keys: 58 us by two with three tiles in LDS, 48 by three with two), else one.
 template <typename T, int D, int NARROW, bool Q8>
 __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (NARROW && !Q8) ? 1 : NARROW && D == 64 ? 3 : 2)) void attend_kernel(AttendArgs a) {
     using S = Shape<D, NARROW, Q8>;
