@@ -544,7 +544,7 @@ int ivf_kv_read(const ivf_kv_step* step, const ivf_kv_cache* cache, const int32_
  *   step       q_off, len, n_seq and n_tokens are used
  *   logits     row t at t * row_stride (elements of dtype: IVF_F32, IVF_F16 or IVF_BF16), `vocab` entries.  -INF and NaN have
  *              probability zero; where entries are +INF, these alone have one, and share it
- *   scale      >= 0, the inverse of a temperature.  0: a draft is accepted if it is the largest entry's token, and that of the largest
+ *   scale      from 0 to 1e30, the inverse of a temperature.  0: a draft is accepted if it is the largest entry's token, and that of the largest
  *              entry follows (of equal ones the first); uniform and draft are not looked at
  *   tokens     [n_tokens] the tokens; a draft outside the vocabulary is refused (the first of a sequence is not looked at)
  *   uniform    [n_tokens] numbers from 0 to below 1
@@ -556,7 +556,7 @@ int ivf_kv_read(const ivf_kv_step* step, const ivf_kv_cache* cache, const int32_
  * vocab is at most 2^30.
  */
 int ivf_verify_workspace(int32_t n_seq, int32_t n_tokens, int32_t vocab, size_t* bytes);
-int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int64_t row_stride, int dtype, int32_t vocab, float scale,
+int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int64_t row_stride, int dtype, int32_t vocab, double scale,
                      const int32_t* tokens, const float* uniform, const float* draft, int64_t draft_stride, int32_t* accepted,
                      int32_t* follows, int32_t* len_out, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -131,7 +131,7 @@ def load():
     L.ivf_attend.argtypes = [step, cache, rows, i32, rows, vp, C.c_float, i32, i32, vp, sz, vp]
     L.ivf_kv_read.argtypes = [step, cache, vp, vp, i64, rows, rows, vp]
     L.ivf_verify_workspace.argtypes = [i32, i32, i32, C.POINTER(sz)]
-    L.ivf_verify_draft.argtypes = [step, vp, i64, ci, i32, C.c_float, vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]
+    L.ivf_verify_draft.argtypes = [step, vp, i64, ci, i32, C.c_double, vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]
     L.ivf_beam_workspace.argtypes = [i32, i32, i32, i32, C.POINTER(sz)]
     L.ivf_beam_step.argtypes = [vp, i64, ci, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, C.POINTER(BeamStateArg), i32, vp, sz, vp]
     L.ivf_strerror.argtypes = [ci]

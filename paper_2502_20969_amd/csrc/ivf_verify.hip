@@ -482,7 +482,7 @@ extern "C" int ivf_verify_workspace(int32_t n_seq, int32_t n_tokens, int32_t voc
     return IVF_OK;
 }
 
-extern "C" int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int64_t row_stride, int dtype, int32_t vocab, float scale,
+extern "C" int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int64_t row_stride, int dtype, int32_t vocab, double scale,
                                 const int32_t* tokens, const float* uniform, const float* draft, int64_t draft_stride, int32_t* accepted,
                                 int32_t* follows, int32_t* len_out, void* workspace, size_t workspace_bytes, void* stream) {
     if (!step) return fail(IVF_EINVAL, "step is NULL");
@@ -492,8 +492,8 @@ extern "C" int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int
     if (rc) return rc;
     if (!logits || !tokens || !accepted || !follows || !len_out) return fail(IVF_EINVAL, "logits, tokens or an output is NULL");
     if (dtype != IVF_F32 && dtype != IVF_F16 && dtype != IVF_BF16) return fail(IVF_EINVAL, "unknown dtype %d", dtype);
-    if (!(scale >= 0.f) || scale > 1e30f) return fail(IVF_EINVAL, "scale must not be negative");
-    if (scale > 0.f && !uniform) return fail(IVF_EINVAL, "uniform is NULL");
+    if (!(scale >= 0.0) || scale > 1e30) return fail(IVF_EINVAL, "scale must be from 0 to 1e30");
+    if (scale > 0.0 && !uniform) return fail(IVF_EINVAL, "uniform is NULL");
     if (row_stride < vocab) return fail(IVF_EINVAL, "row_stride (%lld) is below vocab (%d)", (long long)row_stride, vocab);
     if (draft && draft_stride < vocab) return fail(IVF_EINVAL, "draft_stride (%lld) is below vocab (%d)", (long long)draft_stride, vocab);
     if (((uintptr_t)logits & (dtype == IVF_F32 ? 3u : 1u)) != 0 || ((uintptr_t)draft & 3u) != 0)
@@ -509,7 +509,7 @@ extern "C" int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int
     a.logits = logits; a.row_stride = row_stride; a.draft = draft; a.draft_stride = draft_stride; a.tokens = tokens; a.uniform = uniform;
     a.accepted = accepted; a.follows = follows; a.len_out = len_out; a.vocab = vocab;
     a.n_tile = (vocab + kVerifyTile - 1) / kVerifyTile;
-    a.rise = (double)scale * 1.44269504088896340736;
+    a.rise = scale * 1.44269504088896340736;
     a.tiles = (VerifyTile*)workspace;
     a.chosen = a.tiles + (size_t)a.step.n_tokens * a.n_tile;
     a.left = (double*)(a.chosen + a.step.n_seq);

@@ -91,7 +91,7 @@ def verify(logits, tokens, uniform, q_off, lens, draft=None, scale=1.0):
         if top == np.inf:
             w = (row == np.inf).astype(np.float64)
         else:
-            w = np.exp(float(np.float32(scale)) * (row - top))
+            w = np.exp(scale * (row - top))
         return w / w.sum()
 
     for s in range(len(q_off) - 1):

@@ -183,6 +183,24 @@ def test_scales_and_sizes(scale, size):
     _run(new, logits, tokens, uniform, draft=torch.softmax(torch.randn(11, 5000, generator=torch.Generator().manual_seed(3)), -1), scale=scale)
 
 
+def test_a_temperature_that_32_bits_round():
+    """scale counts as it is given: random numbers that lie between the running sums by 0.7 and by what 32 bits make of it."""
+    logits = torch.randn(60, 60001, generator=torch.Generator().manual_seed(6)) * 3
+    uniform, want = np.zeros(60, np.float32), []
+    for t in range(60):
+        x = logits[t].double().numpy()
+        by, rounded = (np.cumsum(np.exp(s * (x - x.max()))) for s in (0.7, float(np.float32(0.7))))
+        by, rounded = by / by[-1], rounded / rounded[-1]
+        u = ((by + rounded) / 2).astype(np.float32).astype(np.float64)
+        between = (np.abs(u - by) + np.abs(u - rounded) < np.abs(by - rounded) * (1 + 1e-6)) & (np.minimum(np.abs(u - by), np.abs(u - rounded)) > 1e-10)
+        uniform[t] = u[np.flatnonzero(between)[len(np.flatnonzero(between)) // 2]]
+        want.append(int(np.argmax(by > float(uniform[t]))))
+        assert want[-1] != int(np.argmax(rounded > float(uniform[t])))
+    step, _ = _step([1] * 60, [5] * 60)
+    got = P.ivf_verify_draft(step, logits.cuda(), torch.zeros(60, dtype=torch.int32).cuda(), torch.from_numpy(uniform).cuda(), scale=0.7)[1].tolist()
+    assert got == want
+
+
 @pytest.mark.parametrize("refused", [2, 31, 32, 33, 69, None])
 def test_many_drafts(refused):
     """A sequence of more drafts than a workgroup keeps the rows of."""
