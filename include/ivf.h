@@ -538,9 +538,9 @@ int ivf_kv_read(const ivf_kv_step* step, const ivf_kv_cache* cache, const int32_
  * it, drafts (copied from a passage, or drawn by a smaller model); row t of logits is what the target says behind token t, p_t =
  * softmax(scale * row t) in 64 bits.  Token t, a draft, is accepted if all drafts before it are and uniform[t] * d < p_(t-1)(token),
  * d = draft[t][token], or 1 without `draft`.  Behind the last accepted one, token a, a token follows that is drawn by uniform[q_off[s]]:
- * from p_a if a is the sequence's last; else from max(p_a - draft[a + 1], 0), or without `draft` from p_a less the refused token (from
- * p_a where that leaves nothing).  To draw by u from weights: the first token at which their running sum, in order, is above u times
- * their sum.
+ * from p_a if a is the sequence's last; else from max(p_a - draft[a + 1], 0), of which less than 2^-40 p_a is nothing, or without `draft`
+ * from p_a less the refused token (from p_a where that leaves nothing).  To draw by u from weights: the first token at which their running
+ * sum, in order, is above u times their sum.
  *   step       q_off, len, n_seq and n_tokens are used
  *   logits     row t at t * row_stride (elements of dtype: IVF_F32, IVF_F16 or IVF_BF16), `vocab` entries.  -INF and NaN have
  *              probability zero; where entries are +INF, these alone have one, and share it

@@ -207,13 +207,41 @@ __device__ __forceinline__ VerifyTile join_tiles(const VerifyArgs& a, int64_t ro
     return all;
 }
 
+// What a draft's probability d leaves of a weight w, max(w - W d, 0).  w and W are off by 1.5e-13 of themselves: where target and draft say the same,
+// what their difference comes out as is of either sign.  Less than 2^-40 of w is therefore nothing.
+__device__ __forceinline__ double left_of(double w, double whole, float d) {
+    const double x = __builtin_fma(-whole, (double)fmaxf(d, 0.f), w);
+    return x > w * 0x1p-40 ? x : 0.0;
+}
+// The same of the entries of one row, whose tiles' sums and entries are formed by this alone: a tile has a sum above zero exactly where one of its
+// entries has.  In units of 2^(less / kPowers) by the table of powers, else of the largest entry's weight.
+struct Left {
+    const double* table;
+    double rise, by, less, whole;
+    float top, least;
+    bool by_table;
+    __device__ __forceinline__ Left(const double* powers, double rise_, float top_, double sum) : table(powers), rise(rise_), top(top_) {
+        by = rise * kPowers;
+        less = rint(by * (double)top);
+        by_table = fabs(less) < 0x1p40;
+        least = fmaxf((float)((double)top - 990.0 / rise), -0x1.fffffep127f);
+        whole = by_table ? sum / exp2_64(__builtin_fma((double)top, by, -less) * (-1.0 / kPowers)) : sum;
+    }
+    template <bool TABLE> __device__ __forceinline__ double of(float x, float d) const {
+        if (!TABLE) return left_of(weight_of(x, top, rise), whole, d);
+        // an entry that has no weight must leave nothing
+        return x > least ? left_of(exp2_by(table, (double)x, by, less), whole, d) : 0.0;
+    }
+};
+
 // The weights that a sequence's next token is drawn from
 template <typename T> struct Weights {
     const T* logits;                                      // the row
     const float* draft;                                   // its draft's, or NULL
+    const Left* left;                                     // with `draft`
     int vocab, without;                                   // a token that is left out, or -1
     float top;
-    double whole, rise;
+    double rise;
     // of N entries from i0 on; 0 behind the row's end
     template <int N> __device__ __forceinline__ void operator()(int i0, double (&w)[N]) const {
         float x[N], d[N];
@@ -223,11 +251,8 @@ template <typename T> struct Weights {
             d[i] = draft && i0 + i < vocab ? draft[i0 + i] : 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = i0 + i == without ? 0.0 : one(x[i], d[i]);
-    }
-    __device__ __forceinline__ double one(float x, float d) const {
-        const double w = weight_of(x, top, rise);
-        return draft ? fmax(w - whole * (double)fmaxf(d, 0.f), 0.0) : w;
+        for (int i = 0; i < N; ++i)
+            w[i] = i0 + i == without ? 0.0 : !draft ? weight_of(x[i], top, rise) : left->by_table ? left->of<true>(x[i], d[i]) : left->of<false>(x[i], d[i]);
     }
 };
 
@@ -324,7 +349,7 @@ template <typename T> __device__ __forceinline__ int draw(const VerifyArgs& a, D
                 sh.token = tile * kVerifyTile + here * kDrawRun + found;
             }
             __syncthreads();
-            return here < 0 ? -1 : sh.token;
+            if (here >= 0) return sh.token;
         }
         weights.draft = nullptr;                          // nothing is left: from p itself
         weights.without = -1;
@@ -379,15 +404,10 @@ __global__ __launch_bounds__(kDrawThreads) void verify_decide_kernel(VerifyArgs 
     } else if (row.top > -INFINITY) {
         int without = refused ? a.tokens[t + 1] : -1;
         if (without >= a.vocab) without = -1;
-        const Weights<T> weights = {(const T*)a.logits + t * a.row_stride, nullptr, a.vocab, without, row.top, row.sum, a.rise};
+        const Weights<T> weights = {(const T*)a.logits + t * a.row_stride, nullptr, nullptr, a.vocab, without, row.top, a.rise};
         token = draw(a, s_draw, weights, t, nullptr, a.uniform[t0]);
     }
     if (threadIdx.x == 0) a.follows[s] = token;
-}
-
-template <typename T> __device__ __forceinline__ Weights<T> weights_left(const VerifyArgs& a, const VerifyTile& chosen) {
-    const int64_t t = chosen.best;
-    return {(const T*)a.logits + t * a.row_stride, a.draft + (t + 1) * a.draft_stride, a.vocab, -1, chosen.top, chosen.sum, a.rise};
 }
 
 // A wavefront per tile of the rows whose draft's probabilities are subtracted
@@ -397,21 +417,22 @@ __global__ __launch_bounds__(kVerifyWaves * 64) void verify_left_kernel(VerifyAr
     const int s = blockIdx.x / per_row, tile = blockIdx.x % per_row * kVerifyWaves + wave_id(), i0 = tile * kVerifyTile;
     const VerifyTile chosen = a.chosen[s];
     if (chosen.best < 0) return;                          // all wavefronts
-    const Weights<T> weights = weights_left<T>(a, chosen);
+    const int64_t t = chosen.best;
+    const float* draft = a.draft + (t + 1) * a.draft_stride;
     float x[kVerifyRun], d[kVerifyRun];
     if (tile < a.n_tile) {
-        load_tile(weights.logits, i0, a.vocab, -INFINITY, x);
+        load_tile((const T*)a.logits + t * a.row_stride, i0, a.vocab, -INFINITY, x);
         // the draft's entries in the places of the logits'
 #pragma unroll
         for (int i = 0; i < kVerifyRun; i += 4) {
             const int at = i0 + place_in_tile<T>(i);
             if (i0 + kVerifyTile <= a.vocab) {
-                const u4_t y = *(const u4_any_t*)(weights.draft + at);
+                const u4_t y = *(const u4_any_t*)(draft + at);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) d[i + e] = __uint_as_float(y[e]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d[i + e] = at + e < a.vocab ? weights.draft[at + e] : 0.f;
+                for (int e = 0; e < 4; ++e) d[i + e] = at + e < a.vocab ? draft[at + e] : 0.f;
             }
         }
     }
@@ -419,21 +440,14 @@ __global__ __launch_bounds__(kVerifyWaves * 64) void verify_left_kernel(VerifyAr
     s_powers[threadIdx.x] = exp2_64(threadIdx.x / (double)kPowers);
     __syncthreads();
     if (tile >= a.n_tile) return;
+    const Left left(s_powers, a.rise, chosen.top, chosen.sum);
     double sum = 0.0;
-    const double by = a.rise * kPowers, less = rint(by * (double)chosen.top);
-    if (fabs(less) < 0x1p40) {
-        // w and W relative to a power of two near the largest weight; an entry that has no weight must leave nothing
-        const float least = fmaxf((float)((double)chosen.top - 990.0 / a.rise), -0x1.fffffep127f);
-        const double back = exp2_64(__builtin_fma((double)chosen.top, by, -less) * (-1.0 / kPowers)), whole = chosen.sum / back;
+    if (left.by_table) {
 #pragma unroll
-        for (int i = 0; i < kVerifyRun; ++i) {
-            const double w = x[i] > least ? exp2_by(s_powers, (double)fmaxf(x[i], least), by, less) : 0.0;
-            sum += fmax(w - whole * (double)fmaxf(d[i], 0.f), 0.0);
-        }
-        sum *= back;
+        for (int i = 0; i < kVerifyRun; ++i) sum += left.of<true>(x[i], d[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < kVerifyRun; ++i) sum += weights.one(x[i], d[i]);
+        for (int i = 0; i < kVerifyRun; ++i) sum += left.of<false>(x[i], d[i]);
     }
     sum = lanes_sum(sum);
     if (lane_id() == 0) a.left[(int64_t)s * a.n_tile + tile] = sum;
@@ -442,10 +456,16 @@ __global__ __launch_bounds__(kVerifyWaves * 64) void verify_left_kernel(VerifyAr
 template <typename T>
 __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyArgs a) {
     __shared__ DrawShared s_draw;
+    __shared__ double s_powers[kPowers];
     const int s = blockIdx.x;
     const VerifyTile chosen = a.chosen[s];
     if (chosen.best < 0) return;
-    const int token = draw(a, s_draw, weights_left<T>(a, chosen), chosen.best, a.left + (int64_t)s * a.n_tile, a.uniform[token_of(a.step, s)]);
+    if (threadIdx.x < kPowers) s_powers[threadIdx.x] = exp2_64(threadIdx.x / (double)kPowers);
+    __syncthreads();
+    const int64_t t = chosen.best;
+    const Left left(s_powers, a.rise, chosen.top, chosen.sum);
+    const Weights<T> weights = {(const T*)a.logits + t * a.row_stride, a.draft + (t + 1) * a.draft_stride, &left, a.vocab, -1, chosen.top, a.rise};
+    const int token = draw(a, s_draw, weights, t, a.left + (int64_t)s * a.n_tile, a.uniform[token_of(a.step, s)]);
     if (threadIdx.x == 0) a.follows[s] = token;
 }
 

@@ -137,6 +137,57 @@ def test_nothing_left():
     assert got[0].tolist() == [0]
 
 
+def _equal_entries(k, vocab, scale, seed=0):
+    """1000 sequences of a settled token and one refused draft.  The row in front of the draft has k equal entries, all others are -inf, at places
+    all over the vocabulary; their value is another in every sequence, of both signs and from next to nothing to 23.  Random numbers
+    between the multiples of 1 / 1024, which the running sums are."""
+    g = torch.Generator().manual_seed(1000 * k + vocab + seed)
+    n = 1000
+    value = torch.cat([torch.arange(-500, 0), torch.arange(1, 501)]).float() * (6 / 128)
+    value += torch.randint(0, 6, (n,), generator=g) / 128
+    places = torch.stack([torch.randperm(vocab, generator=g)[:k].sort()[0] for _ in range(n)])
+    logits = torch.full((2 * n, vocab), -float("inf"))
+    logits[torch.arange(0, 2 * n, 2)[:, None], places] = (value / scale)[:, None] if scale < 1e-3 else value[:, None]
+    logits[1::2] = torch.randn(n, vocab, generator=g)
+    uniform = (torch.randint(0, 1024, (2 * n,), generator=g) * 2 + 1) / 2048
+    return [2] * n, logits, torch.full((2 * n,), -1), uniform, places
+
+
+@pytest.mark.parametrize("k,vocab", [(1, 1), (1, 40), (1, 5000), (2, 40), (2, 5000), (3, 300), (4, 5000), (8, 64), (64, 64), (64, 5000)])
+@pytest.mark.parametrize("scale", [1.0, 0.7, 1.25, 1.6, 1e-4])
+def test_drafts_that_equal_the_target(k, vocab, scale):
+    """One allowed token, or several alike, by target and draft: max(p - q, 0) leaves nothing (1 / 3 in 32 bits is above a third), and the
+    target's own say what follows a draft that cannot be accepted, outside the vocabulary or without probability in both."""
+    new, logits, tokens, uniform, places = _equal_entries(k, vocab, scale)
+    draft = torch.zeros(logits.shape)
+    draft[torch.arange(1, len(tokens), 2)[:, None], places] = 1.0 / k
+    got = _run(new, logits, tokens, uniform, draft=draft, scale=scale)
+    assert not any(got[0].tolist()) and min(got[1].tolist()) >= 0
+    if vocab > k:
+        for s in range(1000):
+            other = set(range(k + 1)) - set(places[s].tolist())
+            tokens[2 * s + 1] = min(other)
+        got = _run(new, logits, tokens, uniform, draft=draft, scale=scale)
+        assert not any(got[0].tolist()) and min(got[1].tolist()) >= 0
+
+
+@pytest.mark.parametrize("vocab", [40, 30000])
+@pytest.mark.parametrize("scale", [1.0, 0.7, 1.6])
+def test_what_is_left_beside_equal_entries(vocab, scale):
+    """Of eight equal entries the draft has the target's probability, but of one none and of one twice it: only the first can follow, by
+    whatever random number, 0 and the largest below 1 among them."""
+    new, logits, tokens, uniform, places = _equal_entries(8, vocab, scale, 5)
+    draft = torch.zeros(logits.shape)
+    rows, at = torch.arange(1, len(tokens), 2), torch.arange(1000) % 8
+    draft[rows[:, None], places] = 0.125
+    draft[rows, places[torch.arange(1000), at]] = 0.0
+    draft[rows, places[torch.arange(1000), (at + 3) % 8]] = 0.25
+    uniform[0::4] = 0.0
+    uniform[2::8] = 1.0 - 2.0 ** -24
+    got = _run(new, logits, tokens, uniform, draft=draft, scale=scale)
+    assert got[1].tolist() == places[torch.arange(1000), at].tolist()
+
+
 def test_drafts_outside_the_vocabulary():
     logits, tokens, uniform, probs = _problem([4, 4, 3], 200, "f16", True, 9)
     tokens[2], tokens[5], tokens[8] = -1, 200, 2 ** 31 - 1
