@@ -64,7 +64,7 @@ __device__ __forceinline__ double exp2_64(double y) {
     return __builtin_amdgcn_ldexp(p, (int)n);
 }
 
-// 2^(t / 256) for t = v by - less, `less` a whole number below 2^40 in size, t from -300,000 on, from a table of 2^(i / 256) in LDS: the series
+// 2^(t / 256) for t = v by - less, `less` a whole number below 2^40 in size, t from -330,000 on, from a table of 2^(i / 256) in LDS: the series
 // around the nearest whole number is off by (0.00136)^4 / 4! = 1.4e-13.  The weights of all entries are formed by it, in 17 instructions
 // each with what is around it (225 rows of 131,072 entries, by exp2_64 37 us, so 23).
 constexpr int kPowers = 256;
@@ -76,6 +76,12 @@ __device__ __forceinline__ double exp2_by(const double* table, double v, double 
     const double p = __builtin_fma(__builtin_fma(c3, f, c2), f, c1), b = table[n & (kPowers - 1)];
     return __builtin_amdgcn_ldexp(__builtin_fma(b * f, p, b), n >> 8);
 }
+
+// Whether a row's weights are formed by it, and the entry that whatever lies below it (-inf and NaN among that) counts as: 990 / rise below the
+// largest.  rise |top| is below 2^32 then, and the entry's rounding to 32 bits below 2^8 / rise, so that its weight is below 2^-730 of the largest.  With
+// rise at 2^-90 or below it could lie under the lowest number of 32 bits, which may have any weight.
+__device__ __forceinline__ bool by_table(double rise, double less) { return fabs(less) < 0x1p40 && rise > 0x1p-90; }
+__device__ __forceinline__ float least_entry(double rise, float top) { return (float)((double)top - 990.0 / rise); }
 
 template <typename T> __device__ __forceinline__ float entry_of(const void* logits, int64_t at) {
     const float x = (float)((const T*)logits)[at];
@@ -166,9 +172,8 @@ __global__ __launch_bounds__(kVerifyWaves * 64, 6) void verify_tiles_kernel(Veri
             for (int i = 0; i < kVerifyRun; ++i) sum += v[i] == INFINITY ? 1.0 : 0.0;
         } else {
             const double by = a.rise * kPowers, less = rint(by * (double)top);
-            if (fabs(less) < 0x1p40) {
-                // entries whose weights are below 2^-990 of the largest, and NaN, may count as 2^-990
-                const float least = fmaxf((float)((double)top - 990.0 / a.rise), -0x1.fffffep127f);
+            if (by_table(a.rise, less)) {
+                const float least = least_entry(a.rise, top);
 #pragma unroll
                 for (int i = 0; i < kVerifyRun; ++i) sum += exp2_by(s_powers, (double)fmaxf(v[i], least), by, less);
                 sum *= exp2_64(__builtin_fma((double)top, by, -less) * (-1.0 / kPowers));
@@ -219,13 +224,13 @@ struct Left {
     const double* table;
     double rise, by, less, whole;
     float top, least;
-    bool by_table;
+    bool tabled;
     __device__ __forceinline__ Left(const double* powers, double rise_, float top_, double sum) : table(powers), rise(rise_), top(top_) {
         by = rise * kPowers;
         less = rint(by * (double)top);
-        by_table = fabs(less) < 0x1p40;
-        least = fmaxf((float)((double)top - 990.0 / rise), -0x1.fffffep127f);
-        whole = by_table ? sum / exp2_64(__builtin_fma((double)top, by, -less) * (-1.0 / kPowers)) : sum;
+        tabled = by_table(rise, less);
+        least = least_entry(rise, top);
+        whole = tabled ? sum / exp2_64(__builtin_fma((double)top, by, -less) * (-1.0 / kPowers)) : sum;
     }
     template <bool TABLE> __device__ __forceinline__ double of(float x, float d) const {
         if (!TABLE) return left_of(weight_of(x, top, rise), whole, d);
@@ -252,7 +257,7 @@ template <typename T> struct Weights {
         }
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            w[i] = i0 + i == without ? 0.0 : !draft ? weight_of(x[i], top, rise) : left->by_table ? left->of<true>(x[i], d[i]) : left->of<false>(x[i], d[i]);
+            w[i] = i0 + i == without ? 0.0 : !draft ? weight_of(x[i], top, rise) : left->tabled ? left->of<true>(x[i], d[i]) : left->of<false>(x[i], d[i]);
     }
 };
 
@@ -442,7 +447,7 @@ __global__ __launch_bounds__(kVerifyWaves * 64) void verify_left_kernel(VerifyAr
     if (tile >= a.n_tile) return;
     const Left left(s_powers, a.rise, chosen.top, chosen.sum);
     double sum = 0.0;
-    if (left.by_table) {
+    if (left.tabled) {
 #pragma unroll
         for (int i = 0; i < kVerifyRun; ++i) sum += left.of<true>(x[i], d[i]);
     } else {

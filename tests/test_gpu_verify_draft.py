@@ -234,6 +234,32 @@ def test_scales_and_sizes(scale, size):
     _run(new, logits, tokens, uniform, draft=torch.softmax(torch.randn(11, 5000, generator=torch.Generator().manual_seed(3)), -1), scale=scale)
 
 
+@pytest.mark.parametrize("scale", [1e-28, 1e-31, 1e-36, 1e-37, 1e-38, 1e-40, 1e-45, 1e-300])
+@pytest.mark.parametrize("vocab", [50, 2048, 5001])
+def test_scales_near_zero(scale, vocab):
+    """All that is allowed is nearly alike, and what is not (-inf, NaN, what lies behind the vocabulary's end) still has no probability."""
+    new = [3, 2, 4]
+    logits, tokens, uniform, _ = _problem(new, vocab, "f32", False, 31)
+    g = torch.Generator().manual_seed(vocab)
+    for t in range(9):
+        allowed = torch.randperm(vocab, generator=g)[:2 + 4 * t]
+        row = torch.full((vocab,), -float("inf"))
+        row[::3] = float("nan")
+        row[allowed] = logits[t, allowed] * 1e3
+        logits[t] = row
+        if t < 8:
+            tokens[t + 1] = allowed[0]
+    logits[1, tokens[2]], logits[4, tokens[5] - 1] = 3.4e38, -3.4e38
+    logits[6] = -float("inf")
+    logits[6, :2] = torch.finfo(torch.float32).min
+    uniform[1] = 0.3
+    _run(new, logits, tokens, uniform, scale=scale)
+    draft = torch.softmax(torch.randn(9, vocab, generator=g), -1)
+    _run(new, logits, tokens, uniform, draft=draft, scale=scale)
+    uniform[1:] = 1.0 - 2.0 ** -24
+    _run(new, logits, tokens, uniform, draft=draft * 20, scale=scale)
+
+
 def test_a_temperature_that_32_bits_round():
     """scale counts as it is given: random numbers that lie between the running sums by 0.7 and by what 32 bits make of it."""
     logits = torch.randn(60, 60001, generator=torch.Generator().manual_seed(6)) * 3
