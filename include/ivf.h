@@ -493,7 +493,7 @@ typedef struct ivf_rows {
  *              positions in their sequences
  *   q, q_out   n_tokens x n_q_heads x d each, or both NULL with n_q_heads = 0; q_out may be q
  * d is a multiple of 16 of at most 1024.  Tokens whose place is not in the table or whose entry is not in the
- * cache are not written (their queries are rotated).  Two tokens must not share a slot.
+ * cache are not written (their queries are rotated).  Two tokens must not share a slot.  n_tokens is below 2^24.
  * A quantised cache gets the rotated numbers as they are in 32 bits (the two products and their sum rounded one by one), taken
  * into +-240 * 2^8 (f16) or +-240 * 2^120 (bf16): e is the least of its range with 448 * 2^e at or above the head's largest, and each
  * number x 2^-e goes to the nearest e4m3 number, ties to even.  What is not finite becomes NaN and counts for nothing in e.
@@ -528,7 +528,7 @@ int ivf_attend(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_row
  *   first      [n_seq] device, or NULL: 0
  *   k, v       n_rows x cache->n_heads x d, of which rows outside all sequences, and those of keys that a sequence does not
  *              have, are left as they were
- * d is a multiple of 16.  The step's new tokens are keys like the others.
+ * d is a multiple of 16, n_rows below 2^28.  The step's new tokens are keys like the others.
  */
 int ivf_kv_read(const ivf_kv_step* step, const ivf_kv_cache* cache, const int32_t* out_off, const int32_t* first, int64_t n_rows,
                 const ivf_rows* k, const ivf_rows* v, void* stream);
@@ -553,7 +553,7 @@ int ivf_kv_read(const ivf_kv_step* step, const ivf_kv_cache* cache, const int32_
  *   accepted, follows, len_out   [n_seq] the accepted drafts; the token that follows, -1 where a row has no entry of a probability
  *              and for sequences without new tokens; len less the drafts that were not accepted.  len_out may be step->len
  *   workspace  as in ivf_attend; its size is ivf_verify_workspace()
- * vocab is at most 2^30.
+ * vocab is at most 2^30, n_seq below 2^23, and n_seq and n_tokens, each times the vocabulary's pieces of 8192 entries, below 2^24.
  */
 int ivf_verify_workspace(int32_t n_seq, int32_t n_tokens, int32_t vocab, size_t* bytes);
 int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int64_t row_stride, int dtype, int32_t vocab, double scale,

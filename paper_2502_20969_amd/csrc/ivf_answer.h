@@ -36,6 +36,8 @@ struct QuantView {
 int make_views(const ivf_kv_step* step, const ivf_kv_cache* cache, CacheView* cv, StepView* sv, QuantView* qv);
 // Checks the rows of `what`: pointer, alignment and strides.
 int check_rows(const ivf_rows* r, const char* what);
+// A launch has fewer than 2^32 threads.
+inline bool too_many_threads(int64_t workgroups, int threads) { return workgroups > (int64_t)UINT32_MAX / threads; }
 
 namespace dev {
 

@@ -356,6 +356,7 @@ extern "C" int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache,
     if (rot < 0 || rot % 16 != 0 || rot > cache->d) return fail(IVF_EINVAL, "rot must be a multiple of 16 of at most d (got %d)", rot);
     if ((rot > 0) != (rotary != nullptr)) return fail(IVF_EINVAL, "rotary and rot go together");
     if (rot > 0 && n_positions < 1) return fail(IVF_EINVAL, "n_positions must be at least 1");
+    if (too_many_threads(step->n_tokens, 256)) return fail(IVF_ELIMIT, "%d tokens", step->n_tokens);
     a.k = *k; a.v = *v;
     if (q) { a.q = *q; a.q_out = *q_out; }
     a.rotary = rotary; a.positions = positions; a.n_positions = n_positions; a.rot = rot;
@@ -388,7 +389,7 @@ extern "C" int ivf_kv_read(const ivf_kv_step* step, const ivf_kv_cache* cache, c
     if ((rc = check_rows(k, "k")) || (rc = check_rows(v, "v"))) return rc;
     if (cache->d % 16 != 0) return fail(IVF_EINVAL, "d must be a multiple of 16 (got %d)", cache->d);
     if (n_rows < 1) return fail(IVF_EINVAL, "n_rows must be at least 1");
-    if (n_rows > INT32_MAX) return fail(IVF_ELIMIT, "%lld rows", (long long)n_rows);
+    if (too_many_threads((n_rows - 1) / kReadRows + 1, 256)) return fail(IVF_ELIMIT, "%lld rows", (long long)n_rows);
     if ((int64_t)2 * cache->n_heads * (cache->d / 8) > 1 << 30) return fail(IVF_ELIMIT, "%d heads of %d", cache->n_heads, cache->d);
     a.k = *k; a.v = *v; a.out_off = out_off; a.first = first; a.n_rows = n_rows; a.hkv = cache->n_heads; a.d = cache->d;
     a.rows_wg = n_rows >= kReadRows * 1024 ? kReadRows : 4;

@@ -477,21 +477,26 @@ __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyArgs a)
 static int check_verify(int n_seq, int n_tokens, int vocab) {
     if (n_seq < 1 || n_tokens < 1 || vocab < 1) return fail(IVF_EINVAL, "n_seq, n_tokens and vocab must be at least 1");
     if (vocab > 1 << 30) return fail(IVF_ELIMIT, "vocab = %d is above 2^30", vocab);
-    if (n_seq > 1 << 24 || n_tokens > 1 << 24) return fail(IVF_ELIMIT, "%d sequences, %d tokens: at most 2^24", n_seq, n_tokens);
+    // launches of kDrawThreads a sequence, and kVerifyWaves * 64 for as many tiles of a row
     const int64_t blocks = (vocab + (int64_t)kVerifyTile * kVerifyWaves - 1) / (kVerifyTile * kVerifyWaves);
-    if (blocks * n_seq > INT32_MAX || blocks * n_tokens > INT32_MAX)
+    if (too_many_threads(n_seq, kDrawThreads) || too_many_threads(blocks * n_seq, kVerifyWaves * 64) || too_many_threads(blocks * n_tokens, kVerifyWaves * 64))
         return fail(IVF_ELIMIT, "%d sequences, %d tokens over %d entries", n_seq, n_tokens, vocab);
     return IVF_OK;
 }
 
-template <typename T> static void launch_verify(const VerifyArgs& a, hipStream_t s) {
+// (a kernel that is not launched leaves to the next ones what its workspace held before)
+template <typename T> static hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
     const int64_t per_row = (a.n_tile + kVerifyWaves - 1) / kVerifyWaves;
     const dim3 block(kVerifyWaves * 64);
+    hipError_t e;
     hipLaunchKernelGGL(verify_tiles_kernel<T>, dim3((unsigned)(a.step.n_tokens * per_row)), block, 0, s, a);
+    if ((e = hipGetLastError())) return e;
     hipLaunchKernelGGL(verify_decide_kernel<T>, dim3(a.step.n_seq), dim3(kDrawThreads), 0, s, a);
-    if (!a.draft || a.rise == 0.0) return;
+    if ((e = hipGetLastError()) || !a.draft || a.rise == 0.0) return e;
     hipLaunchKernelGGL(verify_left_kernel<T>, dim3((unsigned)(a.step.n_seq * per_row)), block, 0, s, a);
+    if ((e = hipGetLastError())) return e;
     hipLaunchKernelGGL(verify_draw_kernel<T>, dim3(a.step.n_seq), dim3(kDrawThreads), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace ivf
@@ -539,9 +544,6 @@ extern "C" int ivf_verify_draft(const ivf_kv_step* step, const void* logits, int
     a.chosen = a.tiles + (size_t)a.step.n_tokens * a.n_tile;
     a.left = (double*)(a.chosen + a.step.n_seq);
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == IVF_F32) launch_verify<float>(a, s);
-    else if (dtype == IVF_F16) launch_verify<_Float16>(a, s);
-    else launch_verify<__bf16>(a, s);
-    HIP_TRY(hipGetLastError());
+    HIP_TRY(dtype == IVF_F32 ? launch_verify<float>(a, s) : dtype == IVF_F16 ? launch_verify<_Float16>(a, s) : launch_verify<__bf16>(a, s));
     return IVF_OK;
 }

@@ -107,6 +107,18 @@ def test_verifications():
     assert L.ivf_verify_draft(None, OK, 100, 1, 100, 1.0, OK, OK, None, 0, OK, OK, OK, OK, 1 << 40, None) == -1
 
 
+def test_launches_beyond_the_limits():
+    """A launch has fewer than 2^32 threads: 512 a sequence, 256 for four tiles of 2048 entries of a row, 256 for sixteen rows that are read back, 256 a token
+    that is appended."""
+    L, n = P.load(), C.c_size_t()
+    for sizes, want in (((2 ** 23, 2, 10), -5), ((2 ** 23 - 1, 2, 10), 0), ((2, 2 ** 24, 10), -5), ((2, 2 ** 24 - 1, 10), 0), ((2, 2 ** 23, 8193), -5),
+                        ((2, 2 ** 23 - 1, 8193), 0), ((2 ** 22, 2, 3 * 8192 + 1), -5), ((2 ** 22 - 1, 2, 4 * 8192), 0), ((2, 127, 2 ** 30), 0), ((2, 128, 2 ** 30), -5)):
+        assert L.ivf_verify_workspace(*sizes, C.byref(n)) == want, sizes
+    for step in (_step(n_seq=2 ** 23), _step(n_tokens=2 ** 24)):
+        assert _verify(step=step) == -5 and _verify(step=step, draft=7 * OK) == -5
+    assert _read(rows=2 ** 28) == -5 and _read(rows=2 ** 63 - 1) == -5 and _append(step=_step(n_tokens=2 ** 24)) == -5
+
+
 def test_what_is_read_is_not_written():
     """Outputs in the place of inputs that other workgroups may still read, and of each other; only the lengths may be taken back in place."""
     for kw in (dict(accepted=5 * OK), dict(follows=6 * OK), dict(lens=4 * OK), dict(accepted=2 * OK), dict(follows=3 * OK), dict(lens=2 * OK), dict(accepted=OK),
