@@ -514,7 +514,8 @@ int ivf_kv_append(const ivf_kv_step* step, const ivf_kv_cache* cache, const ivf_
  *   workspace  device, 16-byte aligned, at least what ivf_attend_workspace() says for the same arguments; its
  *              contents need not be kept, and calls that may overlap need one each
  * d is 64, 96, 128 or 256.  Keys and values in slots that a token does not see never reach its result, whatever
- * they hold; probabilities are rounded to the rows' type before the product with the values.
+ * they hold; probabilities are rounded to the rows' type before the product with the values.  Sums of values are formed with weights of
+ * up to 2^8 and divided in the end: where such a sum passes the largest 32-bit number the result is infinite.
  */
 int ivf_attend_workspace(const ivf_kv_step* step, const ivf_kv_cache* cache, int32_t n_q_heads, int32_t window, int32_t sinks,
                          size_t* bytes);

@@ -563,7 +563,10 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             }
         };
 
-        // one tile: scores, weights, products; `full`: every row sees all its keys
+        // Q8 with few rows, bf16: the weights are multiplied by the values' powers
+        constexpr bool kByPower = S::kDirect && !std::is_same<T, _Float16>::value;
+        // one tile: scores, weights, products; `full`: every row sees all its keys.  False: nothing is done, it is one for the other
+        // kind, which is right for all
         auto compute = [&](int i, auto full_tag) __attribute__((always_inline)) {
             constexpr bool full = decltype(full_tag)::value;
             const int j0 = first_key(i);
@@ -577,7 +580,12 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             auto key_index = [](int t, int r) { return S::kDirect ? direct_key(r) : t * 32 + (r & 3) + 8 * (r >> 2); };
             const int lane_key = (S::kDirect ? 8 : 4) * half;
             // Q8 with few rows: the powers of the values, in the order of their keys: of f16 the two that a product of two takes; of bf16, which has no such
-            // products, the weights are multiplied by them
+            // products, those that the weights are multiplied by.  That changes nothing but exponents unless a power is near the ends of what bf16 holds: weights
+            // are up to 2^8, and times 2^119 below 2^128; what rounding takes from w 2^-60 because it is below 2^-126 is below 2^-66 of the largest weight.
+            // From a tile with other powers on, and in edge tiles, every value is converted by its own: two at a time by the first's power and by the
+            // second's.  (All tiles so: 24 sequences of up to 60,000 keys as above 373 us, not 297.  24 of up to 20,000 of which many heads are all zeros,
+            // under 2^-117: 122 us, not 117)
+            constexpr int kEndLow = 127 - 60, kEndHigh = 127 + 119;
             u4_t half_powers[2];
             f4_t powers[4];
             const uint32_t direct_at = tile_at + direct_value;
@@ -587,9 +595,10 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                 u4_t c[D / 32];
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j) c[j] = *(lds_ptr<const u4_t>)(uintptr_t)((tile_at + direct_place) ^ (uint32_t)(j << 5));
-                const float kp = power_of(a.quant, bytes[direct_row(lane & 31)]), vp = power_of(a.quant, bytes[32 + (lane & 31)]);
-                if constexpr (std::is_same<T, _Float16>::value) ((lds_ptr<_Float16>)(uintptr_t)table)[lane & 31] = (_Float16)vp;
-                else ((lds_ptr<float>)(uintptr_t)table)[lane & 31] = vp;
+                const int vbyte = bytes[32 + (lane & 31)];
+                const float kp = power_of(a.quant, bytes[direct_row(lane & 31)]), vp = power_of(a.quant, vbyte);
+                if constexpr (kByPower) ((lds_ptr<float>)(uintptr_t)table)[lane & 31] = vp;
+                else ((lds_ptr<_Float16>)(uintptr_t)table)[lane & 31] = (_Float16)vp;
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j)
 #pragma unroll
@@ -599,10 +608,11 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                         x[0] = H::mfma(__builtin_bit_cast(s8_t, k), q[2 * j + u], x[0]);
                     }
 #pragma unroll
-                for (int u = 0; u < (std::is_same<T, _Float16>::value ? 2 : 4); ++u) {
-                    if constexpr (std::is_same<T, _Float16>::value) half_powers[u] = *(lds_ptr<const u4_t>)(uintptr_t)(table + (16 * u + 8 * half) * 2);
+                for (int u = 0; u < (kByPower ? full ? 4 : 0 : 2); ++u) {
+                    if constexpr (!kByPower) half_powers[u] = *(lds_ptr<const u4_t>)(uintptr_t)(table + (16 * u + 8 * half) * 2);
                     else powers[u] = *(lds_ptr<const f4_t>)(uintptr_t)(table + (16 * (u / 2) + 8 * half + 4 * (u & 1)) * 4);
                 }
+                if (kByPower && full && __ballot((uint32_t)(vbyte - kEndLow) > kEndHigh - kEndLow) != 0) return false;
             } else {
             // reads of LDS run kBatch products ahead: one wavefront's products then hide their latency
             constexpr int kScores = kKeySteps * kKeyTiles;
@@ -670,9 +680,8 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                     const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r + 1], a.scale_log2, minus));
                     sum[0] += w0;
                     sum[1] += w1;
-                    constexpr bool by_power = S::kDirect && !std::is_same<T, _Float16>::value;
-                    p[t * 2 + r / 8][r % 8] = __builtin_bit_cast(short, (T)(by_power ? w0 * powers[r / 4][r % 4] : w0));
-                    p[t * 2 + r / 8][r % 8 + 1] = __builtin_bit_cast(short, (T)(by_power ? w1 * powers[r / 4][r % 4 + 1] : w1));
+                    p[t * 2 + r / 8][r % 8] = __builtin_bit_cast(short, (T)(kByPower && full ? w0 * powers[r / 4][r % 4] : w0));
+                    p[t * 2 + r / 8][r % 8 + 1] = __builtin_bit_cast(short, (T)(kByPower && full ? w1 * powers[r / 4][r % 4 + 1] : w1));
                 }
             l += sum[0] + sum[1];
             // V transposed, the keys in the order of p: lane l, element l % 32 of a block of 32, keys 16 s + 4 (l / 32) .. + 4 and
@@ -682,13 +691,29 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             };
             auto of_codes = [&](i2_t c, int s) __attribute__((always_inline)) {
                 u4_t v = {from_e4m3<T, false>(c[0], 1.f), from_e4m3<T, true>(c[0], 1.f), from_e4m3<T, false>(c[1], 1.f), from_e4m3<T, true>(c[1], 1.f)};
-                if constexpr (std::is_same<T, _Float16>::value) {
+                if constexpr (!kByPower) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2_t, (uint32_t)v[e]) * __builtin_bit_cast(h2_t, (uint32_t)half_powers[s][e]));
                 }
                 return __builtin_bit_cast(s8_t, v);
             };
+            // bf16, each by its own power
+            auto by_powers = [&](i2_t c, f4_t first, f4_t second) __attribute__((always_inline)) {
+                u4_t v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f4_t power = e < 2 ? first : second;
+                    const uint32_t low = e & 1 ? from_e4m3<T, true>(c[e / 2], power[2]) : from_e4m3<T, false>(c[e / 2], power[0]);
+                    const uint32_t high = e & 1 ? from_e4m3<T, true>(c[e / 2], power[3]) : from_e4m3<T, false>(c[e / 2], power[1]);
+                    v[e] = __builtin_amdgcn_perm(high, low, 0x07060100u);
+                }
+                return __builtin_bit_cast(s8_t, v);
+            };
             auto value = [&](int s, int b) __attribute__((always_inline)) {
+                if constexpr (kByPower) {
+                    const uint32_t at = stage_at + S::kStages * S::kTileBytes + (16 * s + 8 * half) * 4;
+                    return by_powers(codes(s, b), *(lds_ptr<const f4_t>)(uintptr_t)at, *(lds_ptr<const f4_t>)(uintptr_t)(at + 16));
+                }
                 if constexpr (S::kDirect) return of_codes(codes(s, b), s);
                 s8_t v;
 #pragma unroll
@@ -740,7 +765,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                     }
                     o[b] += y;
                 }
-                return;
+                return true;
             }
             constexpr int kSums = kKeyTiles * 2 * kBlocks;
             if constexpr (S::kDirect) {
@@ -758,7 +783,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                         o[(c + u) % kBlocks] = H::mfma(of_codes(v[c / kBatch & 1][u], (c + u) / kBlocks), p[(c + u) / kBlocks], o[(c + u) % kBlocks]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                return;
+                return true;
             }
             s8_t v[2][kBatch];
 #pragma unroll
@@ -773,6 +798,7 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
                 for (int u = 0; u < kBatch; ++u) o[(c + u) % kBlocks] = H::mfma(v[c / kBatch & 1][u], p[(c + u) / kBlocks], o[(c + u) % kBlocks]);
             }
             __builtin_amdgcn_sched_barrier(0);
+            return true;
         };
 
         // Q8 with many rows: a tile is fetched into registers two tiles ahead, and put into LDS one ahead.  (Put piece by piece between the products of
@@ -870,15 +896,31 @@ __global__ __launch_bounds__((Shape<D, NARROW, Q8>::kWaves * 64), (D > 128 || (N
             return j > wave_lim || (j + S::kKeys <= wave_low && j >= sinks);
         };
         // two loops, so that what the tiles at the edges need takes no registers from the others
-        for (int i = 0; i < n_full; ++i) {
-            arrive(i);
-            if (!idle) compute(i, std::true_type{});
-            if (!paged && i + kLocate < n) locate(i + kLocate);
-        }
-        for (int i = n_full; i < n; ++i) {
-            arrive(i);
-            if (!idle && !unseen(i)) compute(i, std::false_type{});
-            if (!paged && i + kLocate < n) locate(i + kLocate);
+        if constexpr (kByPower) {
+            int i = 0;
+            bool here = false;             // tile i has arrived
+            for (; i < n_full; ++i) {
+                arrive(i);
+                if (!idle && !compute(i, std::true_type{})) { here = true; break; }
+                if (!paged && i + kLocate < n) locate(i + kLocate);
+            }
+            for (; i < n; ++i) {
+                if (!here) arrive(i);
+                here = false;
+                if (!idle && !unseen(i)) compute(i, std::false_type{});
+                if (!paged && i + kLocate < n) locate(i + kLocate);
+            }
+        } else {
+            for (int i = 0; i < n_full; ++i) {
+                arrive(i);
+                if (!idle) compute(i, std::true_type{});
+                if (!paged && i + kLocate < n) locate(i + kLocate);
+            }
+            for (int i = n_full; i < n; ++i) {
+                arrive(i);
+                if (!idle && !unseen(i)) compute(i, std::false_type{});
+                if (!paged && i + kLocate < n) locate(i + kLocate);
+            }
         }
         l += other_half(l);
 

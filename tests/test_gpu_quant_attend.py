@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2502_20969_amd as P
-from quant import Problem8
+from quant import LEAST, MOST, Problem8, VALUES, to_codes, values
 from test_gpu_attend import _run
 
 pytestmark = pytest.mark.gpu
@@ -165,6 +165,63 @@ def test_powers_far_apart(dtype, new):
     """Tokens whose powers of two differ by up to 2^18 (f16) or 2^42: each has its own."""
     pr = Problem8([new, 1], [new + 200, 90], hkv=2, d=128, dtype=dtype, loud=3.0 if dtype == "f16" else 7.0, seed=new)
     _run(pr, 4, scale=2.0 ** (-12 if dtype == "f16" else -26), hints=dict(max_q=new, max_len=new + 200))
+
+
+def _at_the_ends(dtype, d, new, n, x, codes, powers):
+    """new tokens of one head, alike, over n keys of which key j has score x[j] (nearly base 2) against each; codes and powers [n, d] and [n] of
+    the values.  Compared with the sums in 64 bits; no absolute tolerance but f16's own, for what is tiny here counts."""
+    t, u = {"f16": (torch.float16, 2.0 ** -11), "bf16": (torch.bfloat16, 2.0 ** -8)}[dtype]
+    page = 32
+    pages = -(-n // page)
+    flat = lambda a, fill: np.concatenate([a, np.full((pages * page - n,) + a.shape[1:], fill, np.uint8)]).reshape(pages, page, 1, *a.shape[1:])
+    k = np.zeros((n, d), np.uint8)
+    k[:, 0] = to_codes(x)
+    assert np.array_equal(VALUES[k[:, 0]], x)
+    q = torch.zeros(new, 1, d, dtype=t)
+    q[:, 0, 0] = 1.0
+    scale = float(np.float32(np.log(2.0) * (1 - 2.0 ** -12)))
+    cache = P.KvCache(*(torch.from_numpy(a).cuda() for a in (flat(k, 0x7F), flat(codes, 0x7F), flat(np.full(n, 127, np.uint8), 255), flat(powers, 255))), dtype=t)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32).cuda()
+    step = P.KvStep(i32([0, new]), i32([n]), i32([list(range(pages))]), page=page, n_tokens=new)
+    out = P.ivf_attend(step, cache, q.cuda(), scale=scale).double().cpu().numpy()[:, 0]
+    v = values(codes, powers.astype(int) - 127)
+    for i in range(new):
+        w = np.exp(scale * (x[:n - new + 1 + i] - x[:n - new + 1 + i].max()))
+        want = w @ v[:len(w)] / w.sum()
+        # weights and result are rounded once each; a score of at most 12 is off by 2 roundings of 32 bits, its power of 2 by as much, sums of
+        # 600 terms by 600 at most.  Half a step of the type's numbers near zero: 2^-25 (f16), 2^-134 (bf16); f16: weights to 2^-33 of the largest
+        tol = (2 * u + 640 * 2.0 ** -24) * (w @ np.abs(v[:len(w)]) / w.sum())
+        tol += 2.0 ** -134 if dtype == "bf16" else len(w) * 2.0 ** -31 * np.abs(v[:len(w)]).max(0) + 2.0 ** -25
+        bad = ~(np.abs(out[i] - want) <= tol)
+        assert not bad.any(), (i, np.flatnonzero(bad)[:4], out[i][bad][:4], want[bad][:4])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+@pytest.mark.parametrize("new", [1, 5, 70])
+@pytest.mark.parametrize("ends", ["high", "low", "both"])
+def test_powers_at_their_ends(dtype, d, new, ends):
+    """Values under the largest and the least power that the rows' type allows, of keys whose weights are up to 2^8 above those of the keys before
+    them, or far below the largest."""
+    n, least, most = 600, 127 + LEAST[dtype], 127 + MOST[dtype]
+    rng = np.random.default_rng(d + new)
+    # small numbers, zeros among them, of one sign.  Sums are 32 bits wide: 2 * 2^-9 * 2^120 times the weight 2^8 of 90 keys, and 1 of the others, is below 2^127
+    codes = np.where(rng.random((n, d)) < 0.5, 0, rng.integers(1, 3, (n, d))).astype(np.uint8)
+    codes[:, ::5] = 0
+    x, powers = np.zeros(n), np.full(n, most)
+    if ends == "high":
+        x[64::6] = 8.0
+    else:
+        # one key before the others, without a value; their weights are no powers of two
+        x[0], x[1:] = 12.0, rng.integers(0, 16, n - 1) / 16
+        codes[0] = 0
+        codes[1:, 1::5] = 0x38 + rng.integers(0, 8, (n - 1, len(range(1, d, 5))))
+        powers[:] = least
+        if ends == "both":
+            # under the largest power too, of which some elements have nothing but zeros
+            powers[3::7] = most
+            codes[3::7, 1::5] = 0
+    _at_the_ends(dtype, d, new, n, x, codes, powers.astype(np.uint8))
 
 
 def test_strides_streams_and_hints():
