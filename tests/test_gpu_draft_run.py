@@ -24,6 +24,15 @@ def test_drafts_change_nothing_but_the_steps():
         assert again == texts and n <= steps, kw
 
 
+@pytest.mark.parametrize("seed", [0, 3, 5])
+def test_drafts_save_steps(seed):
+    """The model repeats itself: some of the drafts are what it says, more of four than of one, and its text stays the same.  (A verification that
+    refused them all would take as many steps as tokens by themselves.)"""
+    import answer_with_drafts as E
+    (plain, steps), (one, n1), (four, n4) = (E.answer(drafts=d, seed=seed) for d in (0, 1, 4))
+    assert one == plain and four == plain and n4 < n1 < steps == 39
+
+
 def test_a_step_in_a_graph():
     """Append, attention, verification and reading back, captured once and replayed with other contents of the same tensors, eager work and waits
     between; two graphs with workspaces of their own in turn.  Every replay gives what the eager calls give."""
