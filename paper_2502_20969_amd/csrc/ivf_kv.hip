@@ -271,7 +271,7 @@ struct ReadArgs {
 
 // A workgroup reads a.rows_wg rows: its first lanes find their slots, then a thread takes a piece of 8 elements of a head, of one row after the
 // other, kReadAtOnce of them at a time: a wavefront's stores are 1 KB in a row (with 16 elements a thread, whose stores are two halves, 64,900 rows
-// of 8 heads of 128 took 89 us instead of 60: 5.5 TB/s).  Sixteen rows a workgroup where that fills the chip, else four (1391 rows: 5.4 and 4.0 us).
+// of 8 heads of 128 took 89 us instead of 60: 5.5 TB/s; out of a 16-bit cache 81: 5.1).  Sixteen rows a workgroup where that fills the chip, else four (1391 rows: 5.4 and 4.0 us).
 constexpr int kReadRows = 16, kReadAtOnce = 4;
 template <typename T, bool QUANT>
 __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {

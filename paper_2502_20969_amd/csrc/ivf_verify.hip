@@ -8,8 +8,9 @@
 // tile, the run of entries inside it, and the entry in turn.  Only a refused draft that was drawn from probabilities needs a second pass
 // over its row, for the sums of max(w - W d, 0).
 //
-// What bounds it: the weights' 64-bit vector instructions (86 % of the SIMDs' cycles).  225 rows of 131,072 bf16 logits: tiles 23 us, the decision 7.6 (a chain of loads: tokens,
-// entries, tiles), what the drafts leave of 64 rows 10, the draw 6.3 (again a chain: sums, a tile).  Five rows of 50,001: 5.3 and 7.1.
+// What bounds it: half of a call the weights' 64-bit vector instructions (86 % of the SIMDs' cycles in the tiles), half kernels of few workgroups that
+// wait for each other.  225 rows of 131,072 bf16 logits: tiles 23 us, the decision 7.5 (a chain of loads: tokens, entries, tiles), what the drafts leave
+// of 64 rows 10.4, the draw 6.1 (again a chain: sums, a tile); by the largest entry alone 12 and 4.  Five rows of 50,001: 5.3 and 7.1.
 #include "ivf_answer.h"
 #include "ivf_device.h"
 #include <math.h>
