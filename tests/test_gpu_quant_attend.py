@@ -224,6 +224,20 @@ def test_powers_at_their_ends(dtype, d, new, ends):
     _at_the_ends(dtype, d, new, n, x, codes, powers.astype(np.uint8))
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 3)])
+@pytest.mark.parametrize("first", [0, 1, 5])
+def test_zeros_under_the_largest_power(dtype, d, window, sinks, first):
+    """Values of zero under the largest power there is, from the `first`th page on every seventh: in prefixes, windows, pieces and tiles at the edges."""
+    pr = Problem8([1, 2, 1, 1, 3], [300, 90, 1, 1500, 40], groups=[(3, 700), (1, 33)], hkv=2, d=d, dtype=dtype, seed=d + first)
+    for s in range(len(pr.new)):
+        for slots in (pr.own_slots(s), pr.prefix_slots(pr.group(s)) if pr.prefix(s) else pr.own_slots(s)[:0]):
+            at = slots[first * pr.page::7]
+            pr.v[at], pr.codes[1][at], pr.powers[1][at] = 0.0, 0, 255
+    _run(pr, 4, window, sinks, hints=dict(max_q=3, max_len=1500, max_prefix=700))
+
+
 def test_strides_streams_and_hints():
     pr = Problem8([1, 90, 2], [700, 300, 60], groups=[(2, 600)], hkv=2, d=128, page=32, major="head", scales="head", seed=12)
     _run(pr, 8, strided=True, stream=torch.cuda.Stream())
